@@ -14,7 +14,9 @@
  *   - the Poincare RGB mapping of Eq. 4 (Sec. III-A);
  *   - the separable form of Eq. 7 and its backward pass (Eq. 8-10), and the backward
  *     pass of the full form (input and weight gradients before the epilogue);
- *   - IQBN in training mode: batch statistics (Eq. 11) and normalisation (Eq. 12).
+ *   - IQBN in training mode: batch statistics (Eq. 11) and normalisation (Eq. 12);
+ *   - the parts of a residual block of pointwise layers beside its convolutions: the join of
+ *     branch and stream with its norms, gate and dropout, and its gradients.
  *
  * Conventions shared by every entry point
  *   Layout      x is NHWC [N][H][W][C_in]; the C_in real channels are four
@@ -418,6 +420,83 @@ quan_status_t quan_qconv2d_maxpool_rgb_fwd(const float* rgb, const void* wr, con
  */
 quan_status_t quan_maxpool2d_fwd(const void* x, int N, int H, int W, int C, int k, int stride,
                                  int pad, void* out, quan_stream_t stream);
+
+/* Element type of a tensor argument of the calls below. */
+typedef enum { QUAN_DTYPE_BF16 = 0, QUAN_DTYPE_F32 = 1 } quan_dtype_t;
+
+/*
+ * Dropout with a mask that is never stored: element i of x [n] is kept, and multiplied by
+ * 1 / (1 - p), when its 16 random bits are >= p 2^16, else it becomes 0 (whatever it was, an
+ * infinity or NaN too).  The bits are a function of the arguments alone (Philox4x32-10 of
+ * Salmon et al., SC 2011): the block with the 64-bit counter offset + *counter + i / 8 and the
+ * key seed, 32-bit words w0..w3, gives element i bits 16 (i mod 2) and up of word
+ * (i mod 8) / 2.  So the same call on dy is the backward pass, and calls that must differ take
+ * seeds or ranges of ceil(n / 8) counters that do not overlap.
+ *   x, out    [n], dtype quan_dtype_t (device); out may be x itself, else must not overlap it
+ *   p         0 <= p <= 1, rounded to a multiple of 2^-16 (the factor is that p's)
+ *   counter   one 64-bit word (device, 8-byte aligned) added to offset when the kernel runs, or
+ *             NULL: a captured graph draws a new mask at each replay when the word is advanced
+ *             between replays
+ * n = 0 is a no-op.
+ */
+quan_status_t quan_dropout(const void* x, long long n, int dtype, float p,
+                           unsigned long long seed, unsigned long long offset,
+                           const unsigned long long* counter, void* out, quan_stream_t stream);
+
+/*
+ * The join of a residual branch with its stream, and the norm that feeds the next branch, on
+ * rows (pixels) of C channels:
+ *   u = h / rms(h) * post      d = dropout(u)      y = x + alpha * gate * d
+ *   n = y / rms(y) * pre       rms(v)^2 = mean(v^2) + eps
+ * with the mean over the row (groups = 1) or over each quaternion component by itself
+ * (groups = 4: four statistics a row).  Arithmetic is fp32; y and n are rounded once each, and
+ * n is taken of y before its rounding.
+ *   x, h      [rows][C] of dtype (device).  h NULL: only the norm, n of x (y must be NULL)
+ *   post      fp32 [C] or NULL: no norm of the branch, u = h
+ *   gate      fp32 [images][C] or NULL (1): row r takes gate row r / (rows / images); images = 1
+ *             is a gate for each channel, rows must be a multiple of images
+ *   pre       fp32 [C] or NULL: no n (n must be NULL then)
+ *   p, seed, offset, counter
+ *             as quan_dropout on the tensor u [rows * C]; p = 0: no dropout
+ *   y, n      [rows][C] of dtype; y may be x and n may be h (in place); no other overlap
+ * C up to 8192 (a multiple of groups); larger returns QUAN_ERR_UNSUPPORTED.  eps must be finite
+ * and > 0, alpha finite.  rows = 0 is a no-op.
+ */
+quan_status_t quan_residual_join_fwd(const void* x, const void* h, const float* post,
+                                     const float* gate, const float* pre, long long rows, int C,
+                                     int groups, long long images, int dtype, float alpha,
+                                     float eps, float p, unsigned long long seed,
+                                     unsigned long long offset,
+                                     const unsigned long long* counter, void* y, void* n,
+                                     quan_stream_t stream);
+
+/*
+ * Gradients of quan_residual_join_fwd from dy = dL/dy (as the stream's next reader has it) and
+ * dn = dL/dn; nothing is kept from the forward call but its tensors h and y.
+ *   dy        [rows][C] of dtype, or NULL for 0
+ *   dn, y     [rows][C] of dtype; both NULL exactly when pre is NULL
+ *   h         the forward's branch; NULL exactly when the forward had none (post, gate, dh, dpost
+ *             and dgate NULL too)
+ *   workspace device scratch of quan_residual_join_bwd_workspace_size bytes, 4-byte aligned,
+ *             overwritten (may be NULL when that is 0)
+ *   dx        [rows][C] of dtype; may be dy or dn (in place).  NULL allowed when pre is NULL:
+ *             dL/dx is dy itself then
+ *   dh        [rows][C] of dtype; may be dn or h (in place)
+ *   dpost, dgate, dpre
+ *             fp32 [C], [images][C] and [C]: each given exactly when its vector is.  Sums of
+ *             fp32 partial sums in a fixed order: the same call gives the same bits
+ * rows = 0 sets dpost, dgate and dpre to 0.
+ */
+size_t quan_residual_join_bwd_workspace_size(long long rows, int C, int groups,
+                                             long long images);
+quan_status_t quan_residual_join_bwd(const void* dy, const void* dn, const void* y,
+                                     const void* h, const float* post, const float* gate,
+                                     const float* pre, long long rows, int C, int groups,
+                                     long long images, int dtype, float alpha, float eps,
+                                     float p, unsigned long long seed, unsigned long long offset,
+                                     const unsigned long long* counter, void* workspace,
+                                     size_t workspace_bytes, void* dx, void* dh, float* dpost,
+                                     float* dgate, float* dpre, quan_stream_t stream);
 
 /* Select the path of later quan_qconv2d_fwd / _res calls in this process (default AUTO). */
 quan_status_t quan_set_path(int path);

@@ -198,6 +198,38 @@ cudaError_t launch_qconv_stem_pool_rgb(const ConvShape& s, const float* rgb,
                                        const TcOptions& opt, int num_sms, cudaStream_t stream,
                                        char* err, size_t errlen);
 
+// Dropout (philox.cuh): the mask of one call.
+struct DropoutArgs {
+    uint32_t threshold;  // an element is kept when its 16 bits are >= threshold (0: all kept)
+    float factor;        // 2^16 / (2^16 - threshold); 0 when everything is dropped
+    uint32_t key0, key1;
+    unsigned long long offset;
+    const unsigned long long* counter;  // device word added to offset, or null
+};
+// p in [0, 1] rounded to a step of 2^-16.
+DropoutArgs dropout_args(float p, unsigned long long seed, unsigned long long offset,
+                         const unsigned long long* counter);
+cudaError_t launch_dropout(const void* x, long long n, bool f32, const DropoutArgs& d, void* out,
+                           int num_sms, cudaStream_t stream);
+
+// The residual join and its gradients (residual.cu).  Forward: x, h, out_y (y), out_n (n);
+// backward: h, y, dy, dn, out_y (dx), out_n (dh).  Absent tensors and vectors are null.
+struct JoinArgs {
+    const void *x, *h, *y, *dy, *dn;
+    const float *post, *gate, *pre;  // [C], [images][C], [C]
+    void *out_y, *out_n;
+    long long rows, images;
+    int C, groups;
+    bool f32;
+    float alpha, eps;
+    DropoutArgs drop;
+};
+bool join_supported(int C, int groups);
+cudaError_t launch_join_fwd(const JoinArgs& a, int num_sms, cudaStream_t stream);
+size_t join_bwd_workspace_bytes(long long rows, int C, int groups, long long images, int num_sms);
+cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, float* dgate,
+                            float* dpre, int num_sms, cudaStream_t stream);
+
 // Per-real-channel max pooling, bf16 NHWC.
 cudaError_t launch_maxpool_bf16(const void* x, int N, int H, int W, int C, int k, int stride,
                                 int pad, void* out, int num_sms, cudaStream_t stream);

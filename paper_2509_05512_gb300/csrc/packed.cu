@@ -46,6 +46,31 @@ struct Conv {
     c.x, c.w[0], c.w[1], c.w[2], c.w[3], c.bias, c.scale, c.shift, c.v[0], c.v[1], c.v[2],  \
         c.v[3], c.v[4], c.v[5], c.v[6], c.v[7], c.v[8], c.v[9]
 
+// The random numbers of a dropout, and the arguments both directions of a join share.
+struct Draw {
+    unsigned long long seed, offset;
+    const unsigned long long* counter;
+    explicit Draw(Args& g) {
+        seed = static_cast<unsigned long long>(g.next());
+        offset = static_cast<unsigned long long>(g.next());
+        counter = static_cast<const unsigned long long*>(g.ptr());
+    }
+};
+struct Join {
+    float *post, *gate, *pre;
+    long long rows, images;
+    int C, groups, dtype;
+    float alpha, eps, p;
+    Draw d;
+    explicit Join(Args& g)
+        : post(g.f32()), gate(g.f32()), pre(g.f32()), rows(g.next()), images(g.next()),
+          C(g.num()), groups(g.num()), dtype(g.num()), alpha(g.real()), eps(g.real()),
+          p(g.real()), d(g) {}
+};
+#define QUAN_JOIN_ARGS                                                                       \
+    j.post, j.gate, j.pre, j.rows, j.C, j.groups, j.images, j.dtype, j.alpha, j.eps, j.p,    \
+        j.d.seed, j.d.offset, j.d.counter
+
 }  // namespace
 
 extern "C" int quan_packed_call(int op, const long long* words) {
@@ -148,6 +173,36 @@ extern "C" int quan_packed_call(int op, const long long* words) {
             const size_t bytes = static_cast<size_t>(g.next());
             void* out = g.ptr();
             return quan_qconv2d_maxpool_fwd(QUAN_CONV_ARGS, ws, bytes, out, g.stream());
+        }
+        case 13: {
+            void* x = g.ptr();
+            const long long n = g.next();
+            const int dtype = g.num();
+            const float p = g.real();
+            const Draw d(g);
+            void* out = g.ptr();
+            return quan_dropout(x, n, dtype, p, d.seed, d.offset, d.counter, out, g.stream());
+        }
+        case 14: {
+            void* x = g.ptr();
+            void* h = g.ptr();
+            const Join j(g);
+            void* y = g.ptr();
+            void* n = g.ptr();
+            return quan_residual_join_fwd(x, h, QUAN_JOIN_ARGS, y, n, g.stream());
+        }
+        case 15: {
+            void* t[4];
+            for (auto& p : t) p = g.ptr();
+            const Join j(g);
+            void* ws = g.ptr();
+            const size_t bytes = static_cast<size_t>(g.next());
+            void* dx = g.ptr();
+            void* dh = g.ptr();
+            float* d[3];
+            for (auto& p : d) p = g.f32();
+            return quan_residual_join_bwd(t[0], t[1], t[2], t[3], QUAN_JOIN_ARGS, ws, bytes, dx,
+                                          dh, d[0], d[1], d[2], g.stream());
         }
         default:
             return QUAN_ERR_INVALID_ARG;

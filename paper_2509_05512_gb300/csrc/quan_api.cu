@@ -353,6 +353,72 @@ quan_status_t run_bwd_weight(const void* x, const void* dy, int N, int H, int W,
     return QUAN_OK;
 }
 
+// ------------------------------------------------------------------ residual block parts
+
+quan_status_t check_dropout(float p, const unsigned long long* counter) {
+    if (!(p >= 0.0f && p <= 1.0f))
+        return fail(QUAN_ERR_INVALID_ARG, "p must be between 0 and 1 (got %g)", p);
+    if (reinterpret_cast<uintptr_t>(counter) % 8 != 0)
+        return fail(QUAN_ERR_INVALID_ARG, "counter must be 8-byte aligned");
+    return QUAN_OK;
+}
+
+// Sizes and scalars of a residual join; fills what both directions share.
+quan_status_t check_join(quan::JoinArgs* a, long long rows, int C, int groups, long long images,
+                         int dtype, float alpha, float eps, float p, unsigned long long seed,
+                         unsigned long long offset, const unsigned long long* counter) {
+    if (dtype != QUAN_DTYPE_BF16 && dtype != QUAN_DTYPE_F32)
+        return fail(QUAN_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (groups != 1 && groups != 4)
+        return fail(QUAN_ERR_INVALID_ARG, "groups must be 1 or 4 (got %d)", groups);
+    if (rows < 0 || C < 1 || C % groups != 0 || images < 1 || rows % images != 0)
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "rows=%lld must be >= 0 and a multiple of images=%lld >= 1, C=%d a positive "
+                    "multiple of groups=%d",
+                    rows, images, C, groups);
+    if (!std::isfinite(alpha) || !std::isfinite(eps) || eps <= 0.0f)
+        return fail(QUAN_ERR_INVALID_ARG, "alpha must be finite, eps finite and > 0");
+    const quan_status_t st = check_dropout(p, counter);
+    if (st != QUAN_OK) return st;
+    if (rows >= (1LL << 40) / C || images >= (1LL << 40) / C)
+        return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
+    if (!quan::join_supported(C, groups))
+        return fail(QUAN_ERR_UNSUPPORTED, "C=%d is above the widest row (8192 channels)", C);
+    a->rows = rows;
+    a->images = images;
+    a->C = C;
+    a->groups = groups;
+    a->f32 = dtype == QUAN_DTYPE_F32;
+    a->alpha = alpha;
+    a->eps = eps;
+    a->drop = quan::dropout_args(p, seed, offset, counter);
+    return QUAN_OK;
+}
+
+// True when an output overlaps another output, or an input that it may not equal (bit i of
+// may_equal[o]: output o may be input i itself).
+struct Span {
+    const void* p;
+    size_t n;
+};
+bool clash(const Span* outs, int no, const Span* ins, int ni, const unsigned* may_equal) {
+    for (int o = 0; o < no; ++o) {
+        for (int k = 0; k < o; ++k)
+            if (overlaps(outs[o].p, outs[o].n, outs[k].p, outs[k].n)) return true;
+        for (int i = 0; i < ni; ++i)
+            if (overlaps(outs[o].p, outs[o].n, ins[i].p, ins[i].n) &&
+                !(((may_equal[o] >> i) & 1u) && outs[o].p == ins[i].p))
+                return true;
+    }
+    return false;
+}
+
+bool misaligned(const void* const* t, int n, size_t align) {
+    for (int i = 0; i < n; ++i)
+        if (reinterpret_cast<uintptr_t>(t[i]) % align != 0) return true;
+    return false;
+}
+
 }  // namespace
 
 thread_local const char* quan::last_variant = "";
@@ -812,6 +878,147 @@ quan_status_t quan_maxpool2d_fwd(const void* x, int N, int H, int W, int C, int 
     e = quan::launch_maxpool_bf16(x, N, H, W, C, k, stride, pad, out, num_sms,
                                   reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "maxpool launch");
+    return QUAN_OK;
+}
+
+quan_status_t quan_dropout(const void* x, long long n, int dtype, float p,
+                           unsigned long long seed, unsigned long long offset,
+                           const unsigned long long* counter, void* out, quan_stream_t stream) {
+    if (dtype != QUAN_DTYPE_BF16 && dtype != QUAN_DTYPE_F32)
+        return fail(QUAN_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (n < 0) return fail(QUAN_ERR_INVALID_ARG, "n must be >= 0 (got %lld)", n);
+    if (n >= (1LL << 40)) return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
+    const quan_status_t st = check_dropout(p, counter);
+    if (st != QUAN_OK) return st;
+    if (n == 0) return QUAN_OK;
+    const size_t e = dtype == QUAN_DTYPE_F32 ? 4 : 2;
+    if (!x || !out) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    const void* tensors[] = {x, out};
+    if (misaligned(tensors, 2, e))
+        return fail(QUAN_ERR_INVALID_ARG, "tensors must be aligned to their elements");
+    if ((x != out && overlaps(x, n * e, out, n * e)) || overlaps(out, n * e, counter, 8))
+        return fail(QUAN_ERR_INVALID_ARG, "out overlaps x without being x, or the counter");
+    int num_sms = 0, cc = 0;
+    cudaError_t ce;
+    if (!device_info(&num_sms, &cc, &ce)) return cuda_fail(ce, "device query");
+    ce = quan::launch_dropout(x, n, dtype == QUAN_DTYPE_F32,
+                              quan::dropout_args(p, seed, offset, counter), out, num_sms,
+                              reinterpret_cast<cudaStream_t>(stream));
+    if (ce != cudaSuccess) return cuda_fail(ce, "dropout launch");
+    return QUAN_OK;
+}
+
+quan_status_t quan_residual_join_fwd(const void* x, const void* h, const float* post,
+                                     const float* gate, const float* pre, long long rows, int C,
+                                     int groups, long long images, int dtype, float alpha,
+                                     float eps, float p, unsigned long long seed,
+                                     unsigned long long offset,
+                                     const unsigned long long* counter, void* y, void* n,
+                                     quan_stream_t stream) {
+    quan::JoinArgs a = {};
+    const quan_status_t st = check_join(&a, rows, C, groups, images, dtype, alpha, eps, p, seed,
+                                        offset, counter);
+    if (st != QUAN_OK) return st;
+    if (rows == 0) return QUAN_OK;
+    if (!x || (h != nullptr) != (y != nullptr) || (pre != nullptr) != (n != nullptr) ||
+        (!h && (post || gate)) || (!y && !n))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "x is needed, y exactly with h, n exactly with pre, post and gate only with "
+                    "h, and y or n");
+    const size_t e = a.f32 ? 4 : 2, t = static_cast<size_t>(rows) * C * e;
+    const void* tensors[] = {x, h, y, n};
+    const void* vectors[] = {post, gate, pre};
+    if (misaligned(tensors, 4, e) || misaligned(vectors, 3, 4))
+        return fail(QUAN_ERR_INVALID_ARG, "tensors must be aligned to their elements");
+    const size_t cb = static_cast<size_t>(C) * 4;
+    const Span outs[] = {{y, t}, {n, t}};
+    const Span ins[] = {{x, t}, {h, t}, {post, cb}, {gate, cb * images}, {pre, cb}, {counter, 8}};
+    const unsigned equal[] = {1u, 2u};
+    if (clash(outs, 2, ins, 6, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "an output overlaps another tensor");
+    int num_sms = 0, cc = 0;
+    cudaError_t ce;
+    if (!device_info(&num_sms, &cc, &ce)) return cuda_fail(ce, "device query");
+    a.x = x;
+    a.h = h;
+    a.post = post;
+    a.gate = gate;
+    a.pre = pre;
+    a.out_y = y;
+    a.out_n = n;
+    ce = quan::launch_join_fwd(a, num_sms, reinterpret_cast<cudaStream_t>(stream));
+    if (ce != cudaSuccess) return cuda_fail(ce, "residual join launch");
+    return QUAN_OK;
+}
+
+size_t quan_residual_join_bwd_workspace_size(long long rows, int C, int groups,
+                                             long long images) {
+    if (rows < 0 || C < 1 || (groups != 1 && groups != 4) || C % groups != 0 || images < 1 ||
+        rows % images != 0)
+        return 0;
+    int num_sms = 0, cc = 0;
+    cudaError_t ce;
+    if (!device_info(&num_sms, &cc, &ce)) return 0;
+    return quan::join_bwd_workspace_bytes(rows, C, groups, images, num_sms);
+}
+
+quan_status_t quan_residual_join_bwd(const void* dy, const void* dn, const void* y,
+                                     const void* h, const float* post, const float* gate,
+                                     const float* pre, long long rows, int C, int groups,
+                                     long long images, int dtype, float alpha, float eps,
+                                     float p, unsigned long long seed, unsigned long long offset,
+                                     const unsigned long long* counter, void* workspace,
+                                     size_t workspace_bytes, void* dx, void* dh, float* dpost,
+                                     float* dgate, float* dpre, quan_stream_t stream) {
+    quan::JoinArgs a = {};
+    const quan_status_t st = check_join(&a, rows, C, groups, images, dtype, alpha, eps, p, seed,
+                                        offset, counter);
+    if (st != QUAN_OK) return st;
+    if ((post != nullptr) != (dpost != nullptr) || (gate != nullptr) != (dgate != nullptr) ||
+        (pre != nullptr) != (dpre != nullptr))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "dpost, dgate and dpre are given exactly with post, gate and pre");
+    if (rows > 0 &&
+        ((pre != nullptr) != (dn != nullptr) || (pre != nullptr) != (y != nullptr) ||
+         (h != nullptr) != (dh != nullptr) || (!h && (post || gate)) || (!dy && !dn) ||
+         (pre && !dx) || (!dx && !dh)))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "dn and y are given exactly with pre, dh exactly with h, post and gate only "
+                    "with h, dy or dn, dx with pre, dx or dh");
+    const size_t e = a.f32 ? 4 : 2, t = static_cast<size_t>(rows) * C * e;
+    const void* tensors[] = {dy, dn, y, h, dx, dh};
+    const void* vectors[] = {post, gate, pre, dpost, dgate, dpre};
+    if (misaligned(tensors, 6, e) || misaligned(vectors, 6, 4))
+        return fail(QUAN_ERR_INVALID_ARG, "tensors must be aligned to their elements");
+    int num_sms = 0, cc = 0;
+    cudaError_t ce;
+    if (!device_info(&num_sms, &cc, &ce)) return cuda_fail(ce, "device query");
+    const size_t need = quan::join_bwd_workspace_bytes(rows, C, groups, images, num_sms);
+    if (need > 0 && (!workspace || workspace_bytes < need ||
+                     reinterpret_cast<uintptr_t>(workspace) % 4 != 0))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "workspace must hold %zu bytes, 4-byte aligned (got %zu)", need,
+                    workspace_bytes);
+    const size_t cb = static_cast<size_t>(C) * 4;
+    const Span outs[] = {{dx, t},   {dh, t},           {dpost, cb}, {dgate, cb * images},
+                         {dpre, cb}, {need ? workspace : nullptr, need}};
+    const Span ins[] = {{dy, t},    {dn, t},             {y, t},    {h, t},
+                        {post, cb}, {gate, cb * images}, {pre, cb}, {counter, 8}};
+    const unsigned equal[] = {1u | 2u, 2u | 8u, 0u, 0u, 0u, 0u};
+    if (clash(outs, 6, ins, 8, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "an output or the workspace overlaps another tensor");
+    a.dy = dy;
+    a.dn = dn;
+    a.y = y;
+    a.h = h;
+    a.post = post;
+    a.gate = gate;
+    a.pre = pre;
+    a.out_y = dx;
+    a.out_n = dh;
+    ce = quan::launch_join_bwd(a, static_cast<float*>(workspace), dpost, dgate, dpre, num_sms,
+                               reinterpret_cast<cudaStream_t>(stream));
+    if (ce != cudaSuccess) return cuda_fail(ce, "residual join gradient launch");
     return QUAN_OK;
 }
 

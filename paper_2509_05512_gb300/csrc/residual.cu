@@ -1,0 +1,688 @@
+// residual.cu -- the join of a residual block's branch with its stream, its gradients, and
+// dropout.  Rows are pixels, C channels each; the norms are root-mean-square norms over the
+// whole row (groups = 1) or over each quaternion component by itself (groups = 4), S = C / groups
+// channels wide:
+//   u = h / rms(h) * post            (post-norm of the branch; u = h without one)
+//   d = dropout(u),  y = x + alpha * gate * d
+//   n = y / rms(y) * pre             (the next branch's pre-norm), rms(v)^2 = mean(v^2) + eps
+// and, from dy = dL/dy (the stream's) and dn = dL/dn, with r1 = 1 / rms(h), r2 = 1 / rms(y),
+// t = dn * pre:
+//   dx = dy + r2 (t - y r2^2 mean(t y)),     dpre  = sum of dn y r2
+//   s = alpha dropout'(dx), v = s gate,      dgate = sum of s u,  dpost = sum of v h r1
+//   w = v post,  dh = r1 (w - h r1^2 mean(w h))
+// (dropout' = the same mask and factor).  All arithmetic and every sum is fp32; a tensor element
+// is rounded once, on its way out, and n is taken of y before that rounding.  The gradients need
+// no statistics kept from the forward call: they read h and y whole anyway.
+//
+// Both directions are bound by HBM: one pass, each tensor read or written once.  A row stays in
+// registers between its two reductions: tps threads (a power of two) hold a group, eight
+// consecutive channels a thread (chunks of two at most), so that narrow rows share a warp and
+// reduce with shuffles, wide ones a block of up to 512 threads (8192 channels at most).  Column sums stay in each
+// thread's registers for all of its block's rows; blocks leave one row of partial sums each,
+// added in a fixed order by a second launch, so that repeated calls give the same bits.
+#include <cuda_bf16.h>
+
+#include "internal.h"
+#include "philox.cuh"
+#include "ptx.cuh"
+#include "vec_io.cuh"
+
+namespace quan {
+namespace {
+
+// ------------------------------------------------------------------ dropout
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) dropout_kernel(const T* x, long long n, DropoutArgs d,
+                                                      T* out) {
+    griddep_launch_dependents();
+    griddep_wait();
+    const unsigned long long base = dropout_base(d);
+    const long long groups = (n + 7) / 8, step = static_cast<long long>(gridDim.x) * blockDim.x;
+    for (long long g = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; g < groups;
+         g += step) {
+        const uint32_t keep = d.threshold ? dropout_keep8(d, base + g) : 0xFFu;
+        float v[8];
+        if (VEC && 8 * g + 8 <= n) {
+            Raw<T, 8> r;
+            r.load(x + 8 * g);
+            r.values(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * d.factor : 0.0f;
+            r.set(v);
+            r.store(out + 8 * g);
+        } else {
+            const int left = static_cast<int>(n - 8 * g < 8 ? n - 8 * g : 8);
+            for (int j = 0; j < left; ++j) {
+                Raw<T, 1> r;
+                float w[1];
+                r.load(x + 8 * g + j);
+                r.values(w);
+                w[0] = (keep >> j) & 1u ? w[0] * d.factor : 0.0f;
+                r.set(w);
+                r.store(out + 8 * g + j);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the join
+
+// Eight consecutive channels of a thread, loaded LV at a time; `left` of them exist.
+template <typename T, int LV>
+struct Chunk {
+    Raw<T, LV> r[8 / LV];
+    __device__ __forceinline__ void load(const T* p, int left) {
+#pragma unroll
+        for (int i = 0; i < 8 / LV; ++i) {
+            if (i * LV < left)
+                r[i].load(p + i * LV);
+            else
+                r[i].zero();
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < 8 / LV; ++i) r[i].zero();
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8 / LV; ++i) {
+            float w[LV];
+            r[i].values(w);
+#pragma unroll
+            for (int j = 0; j < LV; ++j) v[i * LV + j] = w[j];
+        }
+    }
+    __device__ __forceinline__ void set_store(const float (&v)[8], T* p, int left) {
+#pragma unroll
+        for (int i = 0; i < 8 / LV; ++i) {
+            if (i * LV < left) {
+                float w[LV];
+#pragma unroll
+                for (int j = 0; j < LV; ++j) w[j] = v[i * LV + j];
+                r[i].set(w);
+                r[i].store(p + i * LV);
+            }
+        }
+    }
+};
+
+struct JoinParams {
+    const void *x, *h, *y, *dy, *dn;  // forward: x, h; backward: h, y, dy, dn
+    const float *post, *gate, *pre;
+    void *out_y, *out_n;               // forward: y, n; backward: dx, dh
+    float *part_gate;                  // backward: sums of dgate, a row a unit
+    float *part_post, *part_pre;       // and of dpost and dpre, a row a block
+    long long rows, rows_per_image;
+    int C, S, groups, tps, slots;
+    long long units, chunk_rows;       // backward: units of chunk_rows rows within an image
+    int chunks;                        // units of an image
+    long long part_stride;             // between the rows of two blocks
+    float alpha, eps, inv_s;
+    DropoutArgs drop;
+};
+
+// Where a thread stands: its slot (row of the block's rows), group and chunks.
+struct Place {
+    int slot, seg, ts;
+};
+__device__ __forceinline__ Place place_of(const JoinParams& p) {
+    const int tpr = p.groups * p.tps;
+    Place q;
+    q.slot = threadIdx.x / tpr;
+    const int t = threadIdx.x - q.slot * tpr;
+    q.seg = t / p.tps;
+    q.ts = t - q.seg * p.tps;
+    return q;
+}
+
+// Sum of v over the tps threads of a group.  Every thread of the block calls it together.
+// CROSS (tps > 32): through shared memory, one word a warp, two buffers in turn: who writes a
+// buffer has passed the other one's barrier, which every reader of this one reached after it.
+template <bool CROSS, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], int tps, float (&both)[2][96],
+                                          int& turn) {
+    if constexpr (!CROSS) {
+        for (int o = tps >> 1; o > 0; o >>= 1) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
+    } else {
+        float* sm = both[turn];
+        turn ^= 1;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int wps = tps >> 5, first = warp & ~(wps - 1);
+        if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) sm[32 * k + warp] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = lane < wps ? sm[32 * k + first + lane] : 0.0f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
+    }
+}
+
+// A thread's share of a per-channel vector (1 without one).
+template <int NC>
+__device__ __forceinline__ void load_columns(const float* v, const JoinParams& p, const Place& q,
+                                             float scale, float (&out)[NC][8]) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int col = (q.ts + c * p.tps) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            out[c][j] = (v && col + j < p.S) ? scale * __ldg(v + q.seg * p.S + col + j) : scale;
+    }
+}
+
+// Bits of the eight elements from linear index i on.
+__device__ __forceinline__ uint32_t keep_from(const DropoutArgs& d, unsigned long long base,
+                                              long long i) {
+    const int s = static_cast<int>(i & 7);
+    const uint32_t lo = dropout_keep8(d, base + (static_cast<unsigned long long>(i) >> 3));
+    if (s == 0) return lo;
+    return (lo >> s) |
+           (dropout_keep8(d, base + (static_cast<unsigned long long>(i) >> 3) + 1) << (8 - s));
+}
+
+template <typename T, int LV, int NC, bool CROSS>
+__global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinParams p) {
+    __shared__ float sm[2][96];
+    int turn = 0;
+    griddep_launch_dependents();
+    griddep_wait();
+    const Place q = place_of(p);
+    float post[NC][8], pre[NC][8], gate[NC][8];
+    load_columns<NC>(p.post, p, q, 1.0f, post);
+    load_columns<NC>(p.pre, p, q, 1.0f, pre);
+    load_columns<NC>(p.gate, p, q, p.alpha, gate);
+    const unsigned long long base = p.drop.threshold ? dropout_base(p.drop) : 0ull;
+    const T *x = static_cast<const T*>(p.x), *h = static_cast<const T*>(p.h);
+    T *y = static_cast<T*>(p.out_y), *n = static_cast<T*>(p.out_n);
+    long long image = 0;
+    const long long step = static_cast<long long>(gridDim.x) * p.slots;
+    for (long long r0 = static_cast<long long>(blockIdx.x) * p.slots; r0 < p.rows; r0 += step) {
+        const long long row = r0 + q.slot;
+        const bool active = row < p.rows && q.slot < p.slots;
+        const long long at = row * p.C + q.seg * p.S;
+        Chunk<T, LV> cx[NC], ch[NC];
+        int left[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (q.ts + c * p.tps) * 8;
+            left[c] = active ? p.S - col : 0;
+            cx[c].load(x + at + col, left[c]);
+            if (h) ch[c].load(h + at + col, left[c]);
+        }
+        float v[NC][8];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) cx[c].values(v[c]);
+        if (h) {
+            if (active && p.gate && row / p.rows_per_image != image) {
+                image = row / p.rows_per_image;
+                load_columns<NC>(p.gate + image * p.C, p, q, p.alpha, gate);
+            }
+            float u[NC][8], r1 = 1.0f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) ch[c].values(u[c]);
+            if (p.post) {
+                float ss[1] = {0.0f};
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) ss[0] = fmaf(u[c][j], u[c][j], ss[0]);
+                group_sum<CROSS, 1>(ss, p.tps, sm, turn);
+                r1 = rsqrtf(fmaf(ss[0], p.inv_s, p.eps));
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (q.ts + c * p.tps) * 8;
+                const uint32_t keep =
+                    p.drop.threshold && left[c] > 0 ? keep_from(p.drop, base, at + col) : 0xFFu;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = u[c][j] * r1 * post[c][j] * p.drop.factor;
+                    v[c][j] = fmaf(gate[c][j], (keep >> j) & 1u ? d : 0.0f, v[c][j]);
+                }
+                cx[c].set_store(v[c], y + at + col, left[c]);
+            }
+        }
+        if (n) {
+            float ss[1] = {0.0f};
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ss[0] = fmaf(v[c][j], v[c][j], ss[0]);
+            group_sum<CROSS, 1>(ss, p.tps, sm, turn);
+            const float r2 = rsqrtf(fmaf(ss[0], p.inv_s, p.eps));
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (q.ts + c * p.tps) * 8;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] = v[c][j] * r2 * pre[c][j];
+                cx[c].set_store(v[c], n + at + col, left[c]);
+            }
+        }
+    }
+}
+
+// Adds a column sum over the block's slots and stores it to dst[C].  `sm` holds slots x C words
+// (not used by a block of one slot).
+template <int NC>
+__device__ __forceinline__ void flush_columns(const JoinParams& p, const Place& q,
+                                              float (&acc)[NC][8], float* sm, float* dst) {
+    if (p.slots > 1) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int col = (q.ts + c * p.tps) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (col + j < p.S && q.slot < p.slots) {
+                const int at = q.seg * p.S + col + j;
+                if (p.slots > 1)
+                    sm[q.slot * p.C + at] = acc[c][j];
+                else
+                    dst[at] = acc[c][j];
+            }
+            acc[c][j] = 0.0f;
+        }
+    }
+    if (p.slots > 1) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
+            float s = 0.0f;
+            for (int k = 0; k < p.slots; ++k) s += sm[k * p.C + c];
+            dst[c] = s;
+        }
+    }
+}
+
+template <typename T, int LV, int NC, bool CROSS>
+__global__ void __launch_bounds__(CROSS ? 512 : 256) join_bwd_kernel(const JoinParams p) {
+    __shared__ float sm[2][96];
+    int turn = 0;
+    extern __shared__ float cols[];
+    griddep_launch_dependents();
+    griddep_wait();
+    const Place q = place_of(p);
+    float post[NC][8], pre[NC][8], gate[NC][8];
+    float a_post[NC][8] = {}, a_pre[NC][8] = {}, a_gate[NC][8] = {};
+    load_columns<NC>(p.post, p, q, 1.0f, post);
+    load_columns<NC>(p.pre, p, q, 1.0f, pre);
+    const unsigned long long base = p.drop.threshold ? dropout_base(p.drop) : 0ull;
+    const T *h = static_cast<const T*>(p.h), *y = static_cast<const T*>(p.y);
+    const T *dy = static_cast<const T*>(p.dy), *dn = static_cast<const T*>(p.dn);
+    T *dx = static_cast<T*>(p.out_y), *dh = static_cast<T*>(p.out_n);
+    for (long long u = blockIdx.x; u < p.units; u += gridDim.x) {
+        const long long image = u / p.chunks, k = u - image * p.chunks;
+        const long long first = image * p.rows_per_image + k * p.chunk_rows;
+        long long last = first + p.chunk_rows;
+        if (last > (image + 1) * p.rows_per_image) last = (image + 1) * p.rows_per_image;
+        if (h) load_columns<NC>(p.gate ? p.gate + image * p.C : nullptr, p, q, 1.0f, gate);
+        for (long long r0 = first; r0 < last; r0 += p.slots) {
+            const long long row = r0 + q.slot;
+            const bool active = row < last && q.slot < p.slots;
+            const long long at = row * p.C + q.seg * p.S;
+            Chunk<T, LV> cdy[NC], cdn[NC], cy[NC], ch[NC];
+            int left[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (q.ts + c * p.tps) * 8;
+                left[c] = active ? p.S - col : 0;
+                if (dy)
+                    cdy[c].load(dy + at + col, left[c]);
+                else
+                    cdy[c].zero();
+                if (dn) {
+                    cdn[c].load(dn + at + col, left[c]);
+                    cy[c].load(y + at + col, left[c]);
+                }
+                if (h) ch[c].load(h + at + col, left[c]);
+            }
+            float g[NC][8], hv[NC][8];
+            float s3[3] = {0.0f, 0.0f, 0.0f};  // sums of h^2, y^2 and t y
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                cdy[c].values(g[c]);
+                if (dn) {
+                    float yv[8], nv[8];
+                    cy[c].values(yv);
+                    cdn[c].values(nv);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        s3[1] = fmaf(yv[j], yv[j], s3[1]);
+                        s3[2] = fmaf(nv[j] * pre[c][j], yv[j], s3[2]);
+                    }
+                }
+                if (h) {
+                    ch[c].values(hv[c]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s3[0] = fmaf(hv[c][j], hv[c][j], s3[0]);
+                }
+            }
+            group_sum<CROSS, 3>(s3, p.tps, sm, turn);
+            const float r1 = p.post ? rsqrtf(fmaf(s3[0], p.inv_s, p.eps)) : 1.0f;
+            if (dn) {
+                const float r2 = rsqrtf(fmaf(s3[1], p.inv_s, p.eps));
+                const float m = s3[2] * p.inv_s * r2 * r2;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const int col = (q.ts + c * p.tps) * 8;
+                    float yv[8], nv[8];
+                    cy[c].values(yv);
+                    cdn[c].values(nv);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        g[c][j] = fmaf(r2, fmaf(-m, yv[j], nv[j] * pre[c][j]), g[c][j]);
+                        a_pre[c][j] = fmaf(nv[j] * r2, yv[j], a_pre[c][j]);
+                    }
+                    cy[c].set_store(g[c], dx + at + col, left[c]);
+                }
+            } else if (dx) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                    cdy[c].set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
+            }
+            if (h) {
+                float w1[1] = {0.0f};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const int col = (q.ts + c * p.tps) * 8;
+                    const uint32_t keep = p.drop.threshold && left[c] > 0
+                                              ? keep_from(p.drop, base, at + col)
+                                              : 0xFFu;
+                    const float f = p.alpha * p.drop.factor;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float s = (keep >> j) & 1u ? f * g[c][j] : 0.0f;
+                        const float hn = hv[c][j] * r1;
+                        a_gate[c][j] = fmaf(s, hn * post[c][j], a_gate[c][j]);
+                        const float v = s * gate[c][j];
+                        a_post[c][j] = fmaf(v, hn, a_post[c][j]);
+                        g[c][j] = v * post[c][j];  // w
+                        w1[0] = fmaf(g[c][j], hv[c][j], w1[0]);
+                    }
+                }
+                float m = 0.0f;
+                if (p.post) {
+                    group_sum<CROSS, 1>(w1, p.tps, sm, turn);
+                    m = w1[0] * p.inv_s * r1 * r1;
+                }
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[c][j] = r1 * fmaf(-m, hv[c][j], g[c][j]);
+                    ch[c].set_store(g[c], dh + at + (q.ts + c * p.tps) * 8, left[c]);
+                }
+            }
+        }
+        if (p.part_gate) flush_columns<NC>(p, q, a_gate, cols, p.part_gate + u * p.C);
+    }
+    const long long b = blockIdx.x * p.part_stride;
+    if (p.part_post) flush_columns<NC>(p, q, a_post, cols, p.part_post + b);
+    if (p.part_pre) flush_columns<NC>(p, q, a_pre, cols, p.part_pre + b);
+}
+
+// out[v][c] = sum over k < count of part[v stride_v + k stride_k + c], for the vectors v of
+// blockIdx.y; 32 channels a block, eight threads a channel, joined in a fixed order.
+struct ColumnSum {
+    const float* part;
+    float* out;
+    long long stride_v, stride_k;
+    int count;
+};
+__global__ void __launch_bounds__(256)
+    join_columns_kernel(ColumnSum a, ColumnSum b, ColumnSum c, int C) {
+    __shared__ float sm[8][32];
+    griddep_launch_dependents();
+    griddep_wait();
+    const long long v = blockIdx.y;
+    const ColumnSum& s = v == 0 ? a : (v == 1 ? b : c);
+    if (!s.out) return;
+    const long long w = v < 2 ? 0 : v - 2;
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + lane;
+    float acc = 0.0f;
+    if (col < C) {
+        const float* src = s.part + w * s.stride_v + col;
+#pragma unroll 8
+        for (int k = part; k < s.count; k += 8) acc += src[k * s.stride_k];
+    }
+    sm[part][lane] = acc;
+    __syncthreads();
+    if (part == 0 && col < C) {
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t += sm[k][lane];
+        s.out[w * C + col] = t;
+    }
+}
+
+constexpr int JOIN_MAX_THREADS = 512;
+
+// Threads of a group, chunks a thread, threads of a block and rows side by side in it.
+struct JoinPlan {
+    int tps, nc, threads, slots;
+    long long chunk_rows, units;  // backward
+    int chunks, grid;
+};
+
+bool join_plan(int C, int groups, JoinPlan* pl) {
+    const int S = C / groups;
+    for (pl->nc = 1; pl->nc <= 2; ++pl->nc) {
+        pl->tps = 1;
+        while (pl->tps * 8 * pl->nc < S) pl->tps *= 2;
+        if (pl->tps * groups <= JOIN_MAX_THREADS) break;
+    }
+    if (pl->nc > 2) return false;
+    const int tpr = pl->tps * groups;
+    pl->threads = tpr > 256 ? tpr : 256;
+    pl->slots = pl->threads / tpr;
+    return true;
+}
+
+// Backward: rows are cut into units within an image, so many that the SMs have a few blocks
+// each; a block takes units until none is left.
+void join_units(JoinPlan* pl, long long rows, long long images, int num_sms) {
+    const long long per_image = rows / images;
+    const long long target = static_cast<long long>(num_sms) * (pl->threads > 256 ? 1 : 2);
+    long long chunks = (target + images - 1) / images;
+    const long long most = (per_image + pl->slots - 1) / pl->slots;
+    if (chunks > most) chunks = most;
+    long long r = (per_image + chunks - 1) / chunks;
+    r = (r + pl->slots - 1) / pl->slots * pl->slots;
+    pl->chunk_rows = r;
+    pl->chunks = static_cast<int>((per_image + r - 1) / r);
+    pl->units = images * pl->chunks;
+    pl->grid = static_cast<int>(pl->units < target ? pl->units : target);
+}
+
+template <typename T>
+int load_width(int S, int C, const void* const* t, int n) {
+    uintptr_t a = 0;
+    for (int i = 0; i < n; ++i) a |= reinterpret_cast<uintptr_t>(t[i]);
+    const int row = C * static_cast<int>(sizeof(T));
+    if (S % 8 == 0 && row % 16 == 0 && a % raw_align<T, 8>() == 0) return 8;
+    if (S % 4 == 0 && a % raw_align<T, 4>() == 0) return 4;
+    return 1;
+}
+
+// A thread's one or two chunks; two only where a row takes more than the block's threads, so
+// where its sums cross warps.
+template <typename T, int LV, int NC, bool CROSS>
+cudaError_t launch_join_nc(const JoinParams& p, const JoinPlan& pl, bool backward, int grid,
+                           cudaStream_t stream) {
+    const dim3 g(static_cast<unsigned>(grid)), b(static_cast<unsigned>(pl.threads));
+    if (!backward) return launch_pdl(join_fwd_kernel<T, LV, NC, CROSS>, g, b, 0, stream, p);
+    const size_t smem = pl.slots > 1 ? static_cast<size_t>(pl.slots) * p.C * 4 : 0;
+    return launch_pdl(join_bwd_kernel<T, LV, NC, CROSS>, g, b, smem, stream, p);
+}
+
+template <typename T, int LV>
+cudaError_t launch_join_lv(const JoinParams& p, const JoinPlan& pl, bool backward, int grid,
+                           cudaStream_t stream) {
+    if (pl.nc == 2) return launch_join_nc<T, LV, 2, true>(p, pl, backward, grid, stream);
+    return pl.tps > 32 ? launch_join_nc<T, LV, 1, true>(p, pl, backward, grid, stream)
+                       : launch_join_nc<T, LV, 1, false>(p, pl, backward, grid, stream);
+}
+
+template <typename T>
+cudaError_t launch_join_t(const JoinParams& p, const JoinPlan& pl, int lv, bool backward,
+                          int grid, cudaStream_t stream) {
+    return lv == 8   ? launch_join_lv<T, 8>(p, pl, backward, grid, stream)
+           : lv == 4 ? launch_join_lv<T, 4>(p, pl, backward, grid, stream)
+                     : launch_join_lv<T, 1>(p, pl, backward, grid, stream);
+}
+
+void fill(JoinParams* p, const JoinArgs& a, const JoinPlan& pl) {
+    p->x = a.x;
+    p->h = a.h;
+    p->y = a.y;
+    p->dy = a.dy;
+    p->dn = a.dn;
+    p->post = a.post;
+    p->gate = a.gate;
+    p->pre = a.pre;
+    p->out_y = a.out_y;
+    p->out_n = a.out_n;
+    p->rows = a.rows;
+    p->rows_per_image = a.rows / a.images;
+    p->C = a.C;
+    p->S = a.C / a.groups;
+    p->groups = a.groups;
+    p->tps = pl.tps;
+    p->slots = pl.slots;
+    p->alpha = a.alpha;
+    p->eps = a.eps;
+    p->inv_s = 1.0f / static_cast<float>(p->S);
+    p->drop = a.drop;
+}
+
+int join_load_width(const JoinArgs& a) {
+    const void* t[] = {a.x, a.h, a.y, a.dy, a.dn, a.out_y, a.out_n};
+    return a.f32 ? load_width<float>(a.C / a.groups, a.C, t, 7)
+                 : load_width<__nv_bfloat16>(a.C / a.groups, a.C, t, 7);
+}
+
+}  // namespace
+
+DropoutArgs dropout_args(float p, unsigned long long seed, unsigned long long offset,
+                         const unsigned long long* counter) {
+    DropoutArgs d;
+    d.threshold = static_cast<uint32_t>(p * 65536.0 + 0.5);
+    d.factor = d.threshold < 65536u
+                   ? static_cast<float>(65536.0 / (65536.0 - static_cast<double>(d.threshold)))
+                   : 0.0f;
+    d.key0 = static_cast<uint32_t>(seed);
+    d.key1 = static_cast<uint32_t>(seed >> 32);
+    d.offset = offset;
+    d.counter = counter;
+    return d;
+}
+
+cudaError_t launch_dropout(const void* x, long long n, bool f32, const DropoutArgs& d, void* out,
+                           int num_sms, cudaStream_t stream) {
+    if (n == 0) return cudaSuccess;
+    const long long groups = (n + 7) / 8;
+    long long blocks = (groups + 255) / 256;
+    const long long cap = static_cast<long long>(num_sms) * 32;
+    if (blocks > cap) blocks = cap;
+    const dim3 g(static_cast<unsigned>(blocks)), b(256);
+    const bool vec = (reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+    if (f32) {
+        auto* i = static_cast<const float*>(x);
+        auto* o = static_cast<float*>(out);
+        return vec ? launch_pdl(dropout_kernel<float, true>, g, b, 0, stream, i, n, d, o)
+                   : launch_pdl(dropout_kernel<float, false>, g, b, 0, stream, i, n, d, o);
+    }
+    auto* i = static_cast<const __nv_bfloat16*>(x);
+    auto* o = static_cast<__nv_bfloat16*>(out);
+    return vec ? launch_pdl(dropout_kernel<__nv_bfloat16, true>, g, b, 0, stream, i, n, d, o)
+               : launch_pdl(dropout_kernel<__nv_bfloat16, false>, g, b, 0, stream, i, n, d, o);
+}
+
+bool join_supported(int C, int groups) {
+    JoinPlan pl;
+    return join_plan(C, groups, &pl);
+}
+
+cudaError_t launch_join_fwd(const JoinArgs& a, int num_sms, cudaStream_t stream) {
+    if (a.rows == 0) return cudaSuccess;
+    JoinPlan pl;
+    join_plan(a.C, a.groups, &pl);
+    JoinParams p = {};
+    fill(&p, a, pl);
+    long long blocks = (a.rows + pl.slots - 1) / pl.slots;
+    const long long cap = static_cast<long long>(num_sms) * (pl.threads > 256 ? 2 : 6);
+    if (blocks > cap) blocks = cap;
+    const int lv = join_load_width(a);
+    return a.f32 ? launch_join_t<float>(p, pl, lv, false, static_cast<int>(blocks), stream)
+                 : launch_join_t<__nv_bfloat16>(p, pl, lv, false, static_cast<int>(blocks),
+                                                stream);
+}
+
+// Partial sums: one row of dpost and dpre a block, and one row of dgate a unit, unless there is
+// just one (it then is the result).
+size_t join_bwd_workspace_bytes(long long rows, int C, int groups, long long images,
+                                int num_sms) {
+    JoinPlan pl;
+    if (rows == 0 || !join_plan(C, groups, &pl)) return 0;
+    join_units(&pl, rows, images, num_sms);
+    const size_t w = pl.grid > 1 ? 2u * static_cast<size_t>(pl.grid) : 0;
+    const size_t g = pl.chunks > 1 ? static_cast<size_t>(pl.units) : 0;
+    return (w + g) * C * sizeof(float);
+}
+
+cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, float* dgate,
+                            float* dpre, int num_sms, cudaStream_t stream) {
+    if (a.rows == 0) {
+        float* out[] = {dpost, dgate, dpre};
+        for (int k = 0; k < 3; ++k) {
+            if (!out[k]) continue;
+            const size_t n = static_cast<size_t>(a.C) * (k == 1 ? a.images : 1);
+            const cudaError_t e = cudaMemsetAsync(out[k], 0, n * sizeof(float), stream);
+            if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+    }
+    JoinPlan pl;
+    join_plan(a.C, a.groups, &pl);
+    join_units(&pl, a.rows, a.images, num_sms);
+    JoinParams p = {};
+    fill(&p, a, pl);
+    p.units = pl.units;
+    p.chunk_rows = pl.chunk_rows;
+    p.chunks = pl.chunks;
+    const long long C = a.C;
+    float* gate_part = workspace + (pl.grid > 1 ? 2LL * pl.grid * C : 0);
+    p.part_gate = a.gate ? (pl.chunks > 1 ? gate_part : dgate) : nullptr;
+    // (one block: its sums are the results)
+    const bool many = pl.grid > 1;
+    p.part_post = dpost ? (many ? workspace : dpost) : nullptr;
+    p.part_pre = dpre ? (many ? workspace + C : dpre) : nullptr;
+    p.part_stride = 2 * C;
+    const int lv = join_load_width(a);
+    cudaError_t e = a.f32 ? launch_join_t<float>(p, pl, lv, true, pl.grid, stream)
+                          : launch_join_t<__nv_bfloat16>(p, pl, lv, true, pl.grid, stream);
+    if (e != cudaSuccess) return e;
+    const bool sum_g = a.gate && pl.chunks > 1;
+    if (!(many && (dpost || dpre)) && !sum_g) return cudaSuccess;
+    const ColumnSum post = {p.part_post, many ? dpost : nullptr, 0, 2 * C, pl.grid};
+    const ColumnSum pre = {p.part_pre, many ? dpre : nullptr, 0, 2 * C, pl.grid};
+    const ColumnSum gate = {gate_part, dgate, pl.chunks * C, C, pl.chunks};
+    const dim3 g(static_cast<unsigned>((a.C + 31) / 32),
+                 static_cast<unsigned>(2 + (sum_g ? a.images : 0)));
+    return launch_pdl(join_columns_kernel, g, dim3(256), 0, stream, post, pre, gate, a.C);
+}
+
+}  // namespace quan

@@ -20,6 +20,7 @@ HEADER = os.path.join(os.path.dirname(PKG_DIR), "include", "quan.h")
 QUAN_OK, QUAN_ERR_INVALID_ARG, QUAN_ERR_UNSUPPORTED, QUAN_ERR_CUDA, QUAN_ERR_DEVICE_TIMEOUT = range(5)
 QUAN_ACT_NONE, QUAN_ACT_RELU, QUAN_ACT_SILU = 0, 1, 2
 QUAN_PATH_AUTO, QUAN_PATH_TC, QUAN_PATH_SIMT = 0, 1, 2
+QUAN_DTYPE_BF16, QUAN_DTYPE_F32 = 0, 1
 
 _lock = threading.Lock()
 _lib = None
@@ -91,6 +92,14 @@ def load():
         _bwd_weight_args = [_vp] * 2 + [_i] * 9 + [_vp] * 5
         lib.quan_qconv2d_bwd_weight.argtypes = _bwd_weight_args
         lib.quan_qconv2d_sep_bwd_weight.argtypes = _bwd_weight_args
+        _ull, _ll, _f = ctypes.c_ulonglong, ctypes.c_longlong, ctypes.c_float
+        lib.quan_dropout.argtypes = [_vp, _ll, _i, _f, _ull, _ull, _vp, _vp, _vp]
+        _join_args = [_vp] * 3 + [_ll, _i, _i, _ll, _i, _f, _f, _f, _ull, _ull, _vp]
+        lib.quan_residual_join_fwd.argtypes = [_vp] * 2 + _join_args + [_vp] * 3
+        lib.quan_residual_join_bwd.argtypes = ([_vp] * 4 + _join_args + [_vp, ctypes.c_size_t] +
+                                               [_vp] * 6)
+        lib.quan_residual_join_bwd_workspace_size.argtypes = [_ll, _i, _i, _ll]
+        lib.quan_residual_join_bwd_workspace_size.restype = ctypes.c_size_t
         lib.quan_set_path.argtypes = [_i]
         lib.quan_last_path.argtypes = []
         lib.quan_last_kernel.argtypes = []
@@ -119,7 +128,8 @@ def load():
                      "quan_qconv2d_sep_bwd_data", "quan_qconv2d_bwd_weight",
                      "quan_qconv2d_bwd_data_static", "quan_iqbn_batch_stats",
                      "quan_qconv2d_maxpool_fwd", "quan_qconv2d_maxpool_rgb_fwd",
-                     "quan_iqbn_train_fwd",
+                     "quan_iqbn_train_fwd", "quan_dropout", "quan_residual_join_fwd",
+                     "quan_residual_join_bwd",
                      "quan_qconv2d_sep_bwd_weight",
                      "quan_maxpool2d_fwd", "quan_set_path", "quan_set_tc_tiles",
                      "quan_set_wait_limit_ns", "quan_device_status", "quan_set_fault_injection",
@@ -178,6 +188,9 @@ _BWD_WEIGHT = struct.Struct("16q").pack
 _STATS = struct.Struct("8q").pack
 _TRAIN = struct.Struct("7qd3q").pack
 _SIZES = struct.Struct("9q").pack
+_DROPOUT = struct.Struct("3qd2Q3q").pack
+_JOIN_FWD = struct.Struct("10q3d2Q4q").pack
+_JOIN_BWD = struct.Struct("12q3d2Q9q").pack
 
 
 def _call(op: int, words: bytes) -> None:
@@ -539,3 +552,159 @@ def maxpool2d(x, *, k=3, stride=2, pad=1, out=None, stream=None):
         out = torch.empty((N, Ho, Wo, C), dtype=x.dtype, device=x.device)
     quan_maxpool2d_fwd(x, N, H, W, C, k, stride, pad, out, stream)
     return out
+
+
+# ------------------------------------------------------------------ residual blocks
+
+def quan_dropout(x, n, dtype, p, seed, offset, counter, out, stream=None) -> None:
+    _call(13, _DROPOUT(_addr(x), n, dtype, p, seed, offset, _addr(counter), _addr(out),
+                       _stream(stream)))
+
+
+def quan_residual_join_fwd(x, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p,
+                           seed, offset, counter, y, n, stream=None) -> None:
+    _call(14, _JOIN_FWD(_addr(x), _addr(h), _addr(post), _addr(gate), _addr(pre), rows, images, C,
+                        groups, dtype, alpha, eps, p, seed, offset, _addr(counter), _addr(y),
+                        _addr(n), _stream(stream)))
+
+
+def quan_residual_join_bwd_workspace_size(rows, C, groups, images) -> int:
+    return load().quan_residual_join_bwd_workspace_size(rows, C, groups, images)
+
+
+def quan_residual_join_bwd(dy, dn, y, h, post, gate, pre, rows, C, groups, images, dtype, alpha,
+                           eps, p, seed, offset, counter, workspace, workspace_bytes, dx, dh,
+                           dpost, dgate, dpre, stream=None) -> None:
+    _call(15, _JOIN_BWD(_addr(dy), _addr(dn), _addr(y), _addr(h), _addr(post), _addr(gate),
+                        _addr(pre), rows, images, C, groups, dtype, alpha, eps, p, seed, offset,
+                        _addr(counter), _addr(workspace), workspace_bytes, _addr(dx), _addr(dh),
+                        _addr(dpost), _addr(dgate), _addr(dpre), _stream(stream)))
+
+
+def _empty(stream, shape, dtype, device):
+    """An empty tensor whose memory belongs to `stream` (None: the current one), so that the
+    allocator hands it on only after that stream's work."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream)
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _check_tensor(name, t, shape, dtype):
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or \
+            not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor %s of %s (got %s of %s)" % (
+            name, list(shape), dtype, list(t.shape), t.dtype))
+
+
+def _dtype_of(name, t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return QUAN_DTYPE_BF16
+    if t.dtype == torch.float32:
+        return QUAN_DTYPE_F32
+    raise ValueError("%s must be bfloat16 or float32 (got %s)" % (name, t.dtype))
+
+
+def _check_counter(counter):
+    import torch
+    if counter is not None:
+        _check_tensor("counter", counter.reshape(-1), (1,), torch.int64)
+
+
+def dropout(x, p, seed, offset=0, *, counter=None, out=None, stream=None):
+    """Dropout of a bf16 or fp32 CUDA tensor with probability p in steps of 2^-16: kept elements
+    are multiplied by 1 / (1 - p), the others become 0.  The mask is a function of seed, offset
+    and the element's index and is never stored: the same call on the gradient is the backward
+    pass.  A call uses ceil(n / 8) counters from `offset` on (plus the int64 CUDA scalar
+    `counter`, read when the kernel runs), so calls of one seed take offsets that far apart.
+    out may be x."""
+    dtype = _dtype_of("x", x)
+    _check_tensor("x", x, x.shape, x.dtype)
+    _check_counter(counter)
+    if out is None:
+        out = _empty(stream, x.shape, x.dtype, x.device)
+    else:
+        _check_tensor("out", out, x.shape, x.dtype)
+    quan_dropout(x, x.numel(), dtype, p, seed, offset, counter, out, stream)
+    return out
+
+
+def _join_shape(like, post, gate, pre):
+    """(rows, C, images) of a join's tensors, its vectors checked."""
+    import torch
+    C = like.shape[-1]
+    images = 1
+    if gate is not None:
+        images = 1 if gate.dim() == 1 else like.shape[0]
+        _check_tensor("gate", gate, (C,) if gate.dim() == 1 else (images, C), torch.float32)
+    for name, v in (("post", post), ("pre", pre)):
+        if v is not None:
+            _check_tensor(name, v, (C,), torch.float32)
+    return like.numel() // C if C else 0, C, max(images, 1)
+
+
+def residual_join(x, h=None, *, post=None, gate=None, pre=None, alpha=1.0, groups=1, eps=1e-5,
+                  p=0.0, seed=0, offset=0, counter=None, y=None, n=None, stream=None):
+    """The end of a residual branch and the norm in front of the next one, in one pass:
+        u = h / rms(h) * post,  y = x + alpha * gate * dropout(u),  n = y / rms(y) * pre
+    x, h: bf16 or fp32 [N, ..., C] (CUDA).  post, pre: fp32 [C]; without one, no such norm (u = h;
+    no n).  gate: fp32 [C], or [N, C] for a gate of each image.  groups=4 normalises each
+    quaternion component by itself.  p, seed, offset, counter: see `dropout`.  Without h only the
+    norm of x is taken.  Returns (y, n); y may be given as x and n as h (in place)."""
+    dtype = _dtype_of("x", x)
+    _check_tensor("x", x, x.shape, x.dtype)
+    rows, C, images = _join_shape(x, post, gate, pre)
+    _check_counter(counter)
+    if h is not None:
+        _check_tensor("h", h, x.shape, x.dtype)
+        if y is None:
+            y = _empty(stream, x.shape, x.dtype, x.device)
+    if pre is not None and n is None:
+        n = _empty(stream, x.shape, x.dtype, x.device)
+    for name, t in (("y", y), ("n", n)):
+        if t is not None:
+            _check_tensor(name, t, x.shape, x.dtype)
+    quan_residual_join_fwd(x, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p,
+                           seed, offset, counter, y, n, stream)
+    return y, n
+
+
+def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None, alpha=1.0,
+                           groups=1, eps=1e-5, p=0.0, seed=0, offset=0, counter=None,
+                           workspace=None, dx=None, dh=None, stream=None):
+    """Gradients of `residual_join`, from dy (None: 0) and dn (None without pre) and the forward
+    call's y (needed with pre) and h.  Returns (dx, dh, dpost, dgate, dpre), fp32 sums shaped as
+    their vectors, None for what is absent; without pre, dx is dy itself.  dx may be given as dy
+    or dn, dh as dn or h (in place)."""
+    import torch
+    like = dy if dy is not None else dn
+    if like is None:
+        raise ValueError("dy or dn must be given")
+    dtype = _dtype_of("dy" if dy is not None else "dn", like)
+    rows, C, images = _join_shape(like, post, gate, pre)
+    _check_counter(counter)
+    for name, t in (("dy", dy), ("dn", dn), ("y", y), ("h", h), ("dx", dx), ("dh", dh)):
+        if t is not None:
+            _check_tensor(name, t, like.shape, like.dtype)
+    if pre is None:
+        y = None
+    elif dx is None:
+        dx = _empty(stream, like.shape, like.dtype, like.device)
+    if h is not None and dh is None:
+        dh = _empty(stream, like.shape, like.dtype, like.device)
+    need = quan_residual_join_bwd_workspace_size(rows, C, groups, images)
+    if workspace is None and need:
+        workspace = _empty(stream, (need,), torch.uint8, like.device)
+    sums = [None if v is None else _empty(stream, v.shape, torch.float32, like.device)
+            for v in (post, gate, pre)]
+    if pre is None and h is None:
+        return dy, None, None, None, None
+    quan_residual_join_bwd(
+        dy, dn, y, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p, seed,
+        offset, counter, workspace,
+        0 if workspace is None else workspace.numel() * workspace.element_size(), dx, dh, *sums,
+        stream)
+    return (dy if dx is None else dx, dh, *sums)
