@@ -15,8 +15,9 @@
  *   - the separable form of Eq. 7 and its backward pass (Eq. 8-10), and the backward
  *     pass of the full form (input and weight gradients before the epilogue);
  *   - IQBN in training mode: batch statistics (Eq. 11) and normalisation (Eq. 12);
- *   - the parts of a residual block of pointwise layers beside its convolutions: the join of
- *     branch and stream with its norms, gate and dropout, and its gradients.
+ *   - residual blocks of pointwise layers: the pointwise convolution in 8-bit floating point
+ *     and its input gradient, and the join of branch and stream with its norms, gate and
+ *     dropout, and its gradients.
  *
  * Conventions shared by every entry point
  *   Layout      x is NHWC [N][H][W][C_in]; the C_in real channels are four
@@ -497,6 +498,57 @@ quan_status_t quan_residual_join_bwd(const void* dy, const void* dn, const void*
                                      const unsigned long long* counter, void* workspace,
                                      size_t workspace_bytes, void* dx, void* dh, float* dpost,
                                      float* dgate, float* dpre, quan_stream_t stream);
+
+/*
+ * The pointwise (1x1, stride 1) quaternion convolution of Eq. 5 in 8-bit floating point (e4m3)
+ * with a scale for each block of 128.  Letters and input are quantised block by block: a block's
+ * scale is the smallest 2^e with max |v| / 2^e <= 448 (e >= -126; 1 for a block of zeros), its
+ * values are v / 2^e rounded to e4m3 (nearest, ties to even).  Blocks are 128 output x 128 input
+ * channels of a letter, and 128 channels of one component of one pixel of the input (the last
+ * ones of a row or column are smaller).  Products are exact, sums fp32; the output is bf16.  A
+ * block that holds an infinity or a NaN has scale NaN: every output computed from it is NaN.
+ *
+ * quan_f8_weights quantises the letters once, for quan_qpoint_f8_fwd (transpose 0) or
+ * quan_qpoint_f8_bwd_data (transpose 1; the same 8-bit values and scales, the letters' axes
+ * swapped).
+ *   wr..wk   bf16 [Cout/4][1][1][Cin/4] (device), 2-byte aligned
+ *   q        e4m3 [4][n][pitch] (device, 16-byte aligned), n = Cout/4 and pitch = Cin/4 rounded
+ *            up to 16 (transpose: the other way round), padding zero;
+ *            quan_f8_weights_bytes(Cin, Cout, transpose) bytes
+ *   scale    fp32 [4][ceil(n / 128)][ceil(k / 128)] (device), k = Cin/4 (transpose: Cout/4)
+ */
+size_t quan_f8_weights_bytes(int Cin, int Cout, int transpose);
+quan_status_t quan_f8_weights(const void* wr, const void* wi, const void* wj, const void* wk,
+                              int Cin, int Cout, int transpose, void* q, float* scale,
+                              quan_stream_t stream);
+
+/*
+ * out = act(iqbn_scale * (x W + bias) + iqbn_shift), W the letters of quan_f8_weights
+ * (transpose 0), the rest as in quan_qconv2d_fwd.
+ *   x          bf16 [rows][Cin] (device), rows = N H W pixels; quantised in the call
+ *   workspace  device scratch of quan_qpoint_f8_workspace_size(rows, Cin, Cout) bytes, 256-byte
+ *              aligned, overwritten (may be NULL when that is 0); calls that may run at the same
+ *              time need separate ones
+ *   out        bf16 [rows][Cout] (device), rounded once from fp32; no overlap with an input
+ * rows = 0 is a no-op.  The tcgen05 kernel needs sm_103; its waits are bounded
+ * (quan_device_status).
+ */
+size_t quan_qpoint_f8_workspace_size(long long rows, int Cin, int Cout);
+quan_status_t quan_qpoint_f8_fwd(const void* x, const void* wq, const float* wscale,
+                                 const float* bias, const float* iqbn_scale,
+                                 const float* iqbn_shift, long long rows, int Cin, int Cout,
+                                 int act, void* workspace, size_t workspace_bytes, void* out,
+                                 quan_stream_t stream);
+
+/*
+ * Input gradient of that product: dx = dL/dx, bf16 [rows][Cin], from dy = dL/d(x W), bf16
+ * [rows][Cout], which is quantised in the call as x is, and the letters of quan_f8_weights with
+ * transpose 1.  Cin and Cout are the forward call's; the workspace has
+ * quan_qpoint_f8_workspace_size(rows, Cout, Cin) bytes.
+ */
+quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const float* wscale,
+                                      long long rows, int Cin, int Cout, void* workspace,
+                                      size_t workspace_bytes, void* dx, quan_stream_t stream);
 
 /* Select the path of later quan_qconv2d_fwd / _res calls in this process (default AUTO). */
 quan_status_t quan_set_path(int path);

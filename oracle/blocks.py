@@ -84,3 +84,77 @@ def join_backward(dy, dn, y, h=None, post=None, gate=None, pre=None, alpha=1.0, 
             dpost = (v * hn).sum(axis=0)
             dh = back(v * post, h, r)
     return dx, dh, dpost, dgate, dpre
+
+
+def round_e4m3(v):
+    """|v| <= 448 to the nearest e4m3 value (three mantissa bits, smallest step 2^-9), ties to
+    even."""
+    v = np.asarray(v, dtype=np.float64)
+    _, e = np.frexp(v)
+    step = np.ldexp(1.0, np.maximum(e - 4, -9))
+    return np.rint(v / step) * step
+
+
+def f8_scale(amax):
+    """The smallest 2^e with amax / 2^e <= 448, e >= -126; 1 for 0, NaN for inf or NaN."""
+    amax = np.asarray(amax, dtype=np.float64)
+    ok = np.isfinite(amax) & (amax > 0)
+    m, e = np.frexp(np.where(ok, amax, 1.0))  # 448 = 0.875 2^9
+    s = np.ldexp(1.0, np.maximum(e - 9 + (m > 0.875), -126))
+    return np.where(ok, s, np.where(amax == 0, 1.0, np.nan))
+
+
+def _amax(v, axis):
+    a = np.abs(v).max(axis=axis, initial=0.0)
+    return np.where(np.isnan(v).any(axis=axis), np.nan, a)
+
+
+def f8_rows(x):
+    """The values that rows [rows, C] stand for after quantisation: 128 channels of one component
+    a block."""
+    out = np.array(x, dtype=np.float64)
+    Q = out.shape[1] // 4
+    for c in range(4):
+        for k in range(0, Q, 128):
+            part = out[:, c * Q + k:c * Q + min(k + 128, Q)]
+            s = f8_scale(_amax(part, 1))[:, None]
+            ok = np.isfinite(s)
+            q = round_e4m3(np.where(ok, part, 0.0) / np.where(ok, s, 1.0))
+            part[:] = np.where(ok, q * np.where(ok, s, 1.0), np.nan)
+    return out
+
+
+def f8_letter(w):
+    """(values, scales) of one letter [Qout, Qin]: 128 x 128 blocks."""
+    w = np.array(w, dtype=np.float64)
+    Qo, Qi = w.shape
+    scales = np.empty((-(-Qo // 128), -(-Qi // 128)))
+    for a in range(scales.shape[0]):
+        for b in range(scales.shape[1]):
+            part = w[128 * a:128 * a + 128, 128 * b:128 * b + 128]
+            s = f8_scale(_amax(part, (0, 1)))
+            scales[a, b] = s
+            part[:] = round_e4m3(part / s) * s if np.isfinite(s) else np.nan
+    return w, scales
+
+
+# Eq. 3: output component co takes input component ci through letter co xor ci.
+_SIGN = np.array([[1, -1, -1, -1], [1, 1, -1, 1], [1, 1, 1, -1], [1, -1, 1, 1]], dtype=np.float64)
+
+
+def qpoint(rows, letters, transpose=False):
+    """Rows times the real block matrix of the letters (values), or with transpose times its
+    transpose's counterpart, the input gradient: (result, sum of the terms' magnitudes)."""
+    n_out, n_in = letters[0].shape
+    k = n_out if transpose else n_in
+    out, mag = [], []
+    for a in range(4):
+        acc, m = 0.0, 0.0
+        for b in range(4):
+            part = rows[:, b * k:(b + 1) * k]
+            w = letters[a ^ b] if transpose else letters[a ^ b].T
+            acc = acc + (_SIGN[b, a] if transpose else _SIGN[a, b]) * (part @ w)
+            m = m + np.abs(part) @ np.abs(w)
+        out.append(acc)
+        mag.append(m)
+    return np.concatenate(out, axis=1), np.concatenate(mag, axis=1)

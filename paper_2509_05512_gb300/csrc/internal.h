@@ -230,6 +230,18 @@ size_t join_bwd_workspace_bytes(long long rows, int C, int groups, long long ima
 cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, float* dgate,
                             float* dpre, int num_sms, cudaStream_t stream);
 
+// The pointwise product in 8-bit floating point (qpoint_f8.cu) of Kq input and Nq output
+// quaternion channels.  f8_pitch: bytes of a row of 8-bit channels of one component.
+int f8_pitch(int Kq);
+cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool transpose, void* q,
+                              float* scale, cudaStream_t stream);
+size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq);
+cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
+                             const EpilogueArgs& ep, long long rows, int Kq, int Nq, bool conj,
+                             int act, void* workspace, void* out, int num_sms,
+                             unsigned long long wait_limit_ns, int inject_stall,
+                             cudaStream_t stream, char* err, size_t errlen);
+
 // Per-real-channel max pooling, bf16 NHWC.
 cudaError_t launch_maxpool_bf16(const void* x, int N, int H, int W, int C, int k, int stride,
                                 int pad, void* out, int num_sms, cudaStream_t stream);

@@ -204,6 +204,31 @@ extern "C" int quan_packed_call(int op, const long long* words) {
             return quan_residual_join_bwd(t[0], t[1], t[2], t[3], QUAN_JOIN_ARGS, ws, bytes, dx,
                                           dh, d[0], d[1], d[2], g.stream());
         }
+        case 16: {
+            void* x = g.ptr();
+            void* wq = g.ptr();
+            float* v[4];
+            for (auto& p : v) p = g.f32();
+            const long long rows = g.next();
+            const int Cin = g.num(), Cout = g.num(), act = g.num();
+            void* ws = g.ptr();
+            const size_t bytes = static_cast<size_t>(g.next());
+            void* out = g.ptr();
+            return quan_qpoint_f8_fwd(x, wq, v[0], v[1], v[2], v[3], rows, Cin, Cout, act, ws,
+                                      bytes, out, g.stream());
+        }
+        case 17: {
+            void* dy = g.ptr();
+            void* wq = g.ptr();
+            float* scale = g.f32();
+            const long long rows = g.next();
+            const int Cin = g.num(), Cout = g.num();
+            void* ws = g.ptr();
+            const size_t bytes = static_cast<size_t>(g.next());
+            void* dx = g.ptr();
+            return quan_qpoint_f8_bwd_data(dy, wq, scale, rows, Cin, Cout, ws, bytes, dx,
+                                           g.stream());
+        }
         default:
             return QUAN_ERR_INVALID_ARG;
     }

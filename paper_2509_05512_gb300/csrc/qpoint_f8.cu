@@ -1,0 +1,292 @@
+// qpoint_f8.cu -- the pointwise (1x1) quaternion convolution in 8-bit floating point: x is
+// quantised in the call, the letters once (f8.cuh), both with a scale for each block of 128:
+//   activations  128 channels of one component of one row;
+//   letters      128 output x 128 input channels of one letter.
+// With q the 8-bit values, s the scales, L = co xor ci and sgn Eq. 6's signs,
+//   y[m][co][n] = sum over ci, blocks b of  sgn(co, ci) s_x[ci][b][m] s_w[L][n / 128][b]
+//                 sum over k in b of  q_x[m][ci][k] q_w[L][n][k].
+// The input gradient is the same product with dy in place of x and the letters transposed, whose
+// signs are those of conj(W): letters i, j and k negated.
+//
+// Layouts: q_x [row][4][Kp] and q_w [4][Nq][Kp] with Kp = Kq rounded up to 16, zeros in the
+// padding; s_x [4][blocks][rows], s_w [4][ceil(Nq / 128)][blocks].
+#include <cuda_bf16.h>
+
+#include "f8.cuh"
+#include "internal.h"
+#include "ptx.cuh"
+#include "tc_common.cuh"
+#include "vec_io.cuh"
+
+namespace quan {
+namespace {
+
+// Eight consecutive bf16 channels from k on (the row has Kq of them), 0 past the end.
+template <bool VEC>
+__device__ __forceinline__ void load_x8(const __nv_bfloat16* p, int k, int Kq, float (&v)[8]) {
+    if (VEC) {  // Kq is a multiple of 8
+        Raw<__nv_bfloat16, 8> r;
+        if (k < Kq)
+            r.load(p + k);
+        else
+            r.zero();
+        r.values(v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = k + j < Kq ? __bfloat162float(p[k + j]) : 0.0f;
+    }
+}
+
+// Scale of the 128 channels that a half-warp holds, eight a lane.
+__device__ __forceinline__ float half_warp_scale(const float (&v)[8], float& inv) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return f8_scale(__uint_as_float(m), inv);
+}
+
+// ------------------------------------------------------------------ letters
+
+struct F8Letters {
+    const __nv_bfloat16* w[4];  // [rows][cols]
+    int rows, cols;             // Qout, Qin
+    uint8_t* q;                 // [4][N][Kp]: N = rows, K = cols, or the other way round
+    float* scale;               // [4][N blocks][K blocks]
+    int Kp, nblk, kblk;
+};
+
+// One 128 x 128 block of one letter: its scale, then its 8-bit values, by way of shared memory so
+// that the transposed form too is read and written along its rows.
+template <bool TRANSPOSE>
+__global__ void __launch_bounds__(256) f8_letters_kernel(const F8Letters p) {
+    __shared__ __nv_bfloat16 tile[128][130];  // 130: both directions miss no bank twice
+    __shared__ uint32_t top[8];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int letter = blockIdx.z, r0 = blockIdx.y * 128, c0 = blockIdx.x * 128;
+    const __nv_bfloat16* w = p.w[letter];
+    uint32_t m = 0;
+    for (int i = threadIdx.x; i < 128 * 128; i += 256) {
+        const int r = i >> 7, c = i & 127;
+        const bool in = r0 + r < p.rows && c0 + c < p.cols;
+        const __nv_bfloat16 v =
+            in ? w[static_cast<long long>(r0 + r) * p.cols + c0 + c] : __float2bfloat16_rn(0.0f);
+        tile[r][c] = v;
+        m = max(m, abs_bits(__bfloat162float(v)));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = max(m, top[k]);
+    float inv;
+    const float s = f8_scale(__uint_as_float(m), inv);
+    const int nb = TRANSPOSE ? blockIdx.x : blockIdx.y, kb = TRANSPOSE ? blockIdx.y : blockIdx.x;
+    if (threadIdx.x == 0)
+        p.scale[(static_cast<long long>(letter) * p.nblk + nb) * p.kblk + kb] = s;
+    const int N = TRANSPOSE ? p.cols : p.rows;
+    uint8_t* q = p.q + static_cast<long long>(letter) * N * p.Kp;
+    for (int i = threadIdx.x; i < 128 * 32; i += 256) {
+        const int n = i >> 5, k = (i & 31) * 4;
+        if (nb * 128 + n >= N || kb * 128 + k >= p.Kp) continue;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] = __bfloat162float(TRANSPOSE ? tile[k + j][n] : tile[n][k + j]) * inv;
+        *reinterpret_cast<uint32_t*>(q + static_cast<long long>(nb * 128 + n) * p.Kp + kb * 128 +
+                                     k) = f8x4_from_f32(v[0], v[1], v[2], v[3]);
+    }
+}
+
+// ------------------------------------------------------------------ the product
+
+struct F8Params {
+    const __nv_bfloat16* x;  // [rows][4 Kq]
+    const uint8_t* wq;       // [4][Nq][Kp]
+    const float* ws;         // [4][nblk][kblk]
+    EpilogueArgs ep;
+    __nv_bfloat16* out;      // [rows][4 Nq]
+    long long rows;
+    int Kq, Nq, Kp, kblk, nblk;
+    int conj;  // letters i, j and k enter negated
+    int act;
+};
+
+// The epilogue's activation; a NaN stays one (a block without a scale has to show).
+__device__ __forceinline__ float f8_act(float z, int act) {
+    return act == 1 ? (z < 0.0f ? 0.0f : z) : tc::activate(z, act);
+}
+
+__device__ __forceinline__ void f8_store(const F8Params& p, long long row, int co, int n,
+                                         float acc) {
+    const int c = co * p.Nq + n;
+    if (p.ep.bias) acc += __ldg(p.ep.bias + c);
+    if (p.ep.scale) acc = fmaf(__ldg(p.ep.scale + c), acc, __ldg(p.ep.shift + c));
+    p.out[row * (4LL * p.Nq) + c] = __float2bfloat16_rn(f8_act(acc, p.act));
+}
+
+// A warp per quaternion output channel, RT rows a block: the block quantises its rows' channels
+// 512 at a time into shared memory (as the values they stand for), each lane multiplies four
+// channels of a block of 128, and the warp adds its lanes at the end.  Every product is exact in
+// fp32.
+constexpr int ROWS_K = 512;
+template <int RT, bool VEC>
+__global__ void __launch_bounds__(256) qpoint_rows_kernel(const F8Params p) {
+    __shared__ float xs[RT][4][ROWS_K];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int half = threadIdx.x >> 4, hl = threadIdx.x & 15;
+    const int n = blockIdx.y * 8 + warp;
+    const long long row0 = static_cast<long long>(blockIdx.x) * RT;
+    float acc[RT][4] = {};
+    for (int k0 = 0; k0 < p.Kq; k0 += ROWS_K) {
+        __syncthreads();
+        for (int u = half; u < RT * 16; u += 16) {
+            const int r = u >> 4, ci = (u >> 2) & 3, b = u & 3;
+            const int k = k0 + b * F8_BLOCK + hl * 8;
+            float v[8], inv;
+            if (row0 + r < p.rows) {
+                load_x8<VEC>(p.x + (row0 + r) * (4LL * p.Kq) + ci * p.Kq, k, p.Kq, v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+            }
+            const float s = half_warp_scale(v, inv);
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                float d[4];
+                f8x4_to_f32(f8x4_from_f32(v[j] * inv, v[j + 1] * inv, v[j + 2] * inv,
+                                          v[j + 3] * inv), d);
+                *reinterpret_cast<float4*>(&xs[r][ci][b * F8_BLOCK + hl * 8 + j]) =
+                    make_float4(d[0] * s, d[1] * s, d[2] * s, d[3] * s);
+            }
+        }
+        __syncthreads();
+        if (n >= p.Nq) continue;
+        for (int b = 0; b < ROWS_K / F8_BLOCK && k0 + b * F8_BLOCK < p.Kq; ++b) {
+            const int kb = k0 / F8_BLOCK + b, k = kb * F8_BLOCK + lane * 4;
+            float w[4][4];
+#pragma unroll
+            for (int L = 0; L < 4; ++L) {
+                const uint32_t q =
+                    k < p.Kp ? __ldg(reinterpret_cast<const uint32_t*>(
+                                   p.wq + (static_cast<long long>(L) * p.Nq + n) * p.Kp + k))
+                             : 0u;
+                float s = __ldg(p.ws + (static_cast<long long>(L) * p.nblk + n / F8_BLOCK) *
+                                           p.kblk + kb);
+                if (p.conj && L > 0) s = -s;
+                f8x4_to_f32(q, w[L]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[L][j] *= s;
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+#pragma unroll
+                for (int ci = 0; ci < 4; ++ci) {
+                    const float4 x4 =
+                        *reinterpret_cast<const float4*>(&xs[r][ci][b * F8_BLOCK + lane * 4]);
+                    const float xv[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+                    for (int co = 0; co < 4; ++co)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            acc[r][co] = fmaf(
+                                (tc::NEG_MASK >> (4 * co + ci)) & 1u ? -w[co ^ ci][j]
+                                                                     : w[co ^ ci][j],
+                                xv[j], acc[r][co]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int co = 0; co < 4; ++co) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                acc[r][co] += __shfl_xor_sync(0xffffffffu, acc[r][co], o);
+        }
+    if (n < p.Nq && lane < 4) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            if (row0 + r < p.rows) {
+                const float v = lane == 0 ? acc[r][0]
+                                          : (lane == 1 ? acc[r][1]
+                                                       : (lane == 2 ? acc[r][2] : acc[r][3]));
+                f8_store(p, row0 + r, lane, n, v);
+            }
+    }
+}
+
+template <int RT>
+cudaError_t launch_rows(const F8Params& p, bool vec, cudaStream_t stream) {
+    const dim3 g(static_cast<unsigned>((p.rows + RT - 1) / RT),
+                 static_cast<unsigned>((p.Nq + 7) / 8));
+    return vec ? launch_pdl(qpoint_rows_kernel<RT, true>, g, dim3(256), 0, stream, p)
+               : launch_pdl(qpoint_rows_kernel<RT, false>, g, dim3(256), 0, stream, p);
+}
+
+int blocks_of(int q) { return (q + F8_BLOCK - 1) / F8_BLOCK; }
+
+}  // namespace
+
+int f8_pitch(int Kq) { return (Kq + 15) / 16 * 16; }
+
+cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool transpose, void* q,
+                              float* scale, cudaStream_t stream) {
+    F8Letters p;
+    for (int L = 0; L < 4; ++L) p.w[L] = static_cast<const __nv_bfloat16*>(w[L]);
+    p.rows = Qout;
+    p.cols = Qin;
+    p.q = static_cast<uint8_t*>(q);
+    p.scale = scale;
+    p.Kp = f8_pitch(transpose ? Qout : Qin);
+    p.nblk = blocks_of(transpose ? Qin : Qout);
+    p.kblk = blocks_of(transpose ? Qout : Qin);
+    const dim3 g(static_cast<unsigned>(blocks_of(Qin)), static_cast<unsigned>(blocks_of(Qout)),
+                 4);
+    return transpose ? launch_pdl(f8_letters_kernel<true>, g, dim3(256), 0, stream, p)
+                     : launch_pdl(f8_letters_kernel<false>, g, dim3(256), 0, stream, p);
+}
+
+size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq) {
+    (void)rows;
+    (void)Kq;
+    (void)Nq;
+    return 0;
+}
+
+cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
+                             const EpilogueArgs& ep, long long rows, int Kq, int Nq, bool conj,
+                             int act, void* workspace, void* out, int num_sms,
+                             unsigned long long wait_limit_ns, int inject_stall,
+                             cudaStream_t stream, char* err, size_t errlen) {
+    (void)workspace;
+    (void)num_sms;
+    (void)wait_limit_ns;
+    (void)inject_stall;
+    (void)err;
+    (void)errlen;
+    F8Params p;
+    p.x = static_cast<const __nv_bfloat16*>(x);
+    p.wq = static_cast<const uint8_t*>(wq);
+    p.ws = ws;
+    p.ep = ep;
+    p.out = static_cast<__nv_bfloat16*>(out);
+    p.rows = rows;
+    p.Kq = Kq;
+    p.Nq = Nq;
+    p.Kp = f8_pitch(Kq);
+    p.kblk = blocks_of(Kq);
+    p.nblk = blocks_of(Nq);
+    p.conj = conj ? 1 : 0;
+    p.act = act;
+    const bool vec = Kq % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+    return launch_rows<4>(p, vec, stream);
+}
+
+}  // namespace quan

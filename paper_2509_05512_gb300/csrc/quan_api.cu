@@ -419,6 +419,61 @@ bool misaligned(const void* const* t, int n, size_t align) {
     return false;
 }
 
+// The product both directions of the 8-bit pointwise convolution run: K input and N output
+// channels of the call.
+quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
+                            const quan::EpilogueArgs& ep, long long rows, int K, int N, int act,
+                            bool conj, void* workspace, size_t workspace_bytes, void* out,
+                            quan_stream_t stream) {
+    if (rows < 0 || K < 1 || N < 1 || K % 4 || N % 4)
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "rows=%lld must be >= 0, the channel counts %d and %d positive multiples of 4",
+                    rows, K, N);
+    if ((ep.scale == nullptr) != (ep.shift == nullptr))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "iqbn_scale and iqbn_shift must both be given or both NULL");
+    if (act < QUAN_ACT_NONE || act > QUAN_ACT_SILU)
+        return fail(QUAN_ERR_INVALID_ARG, "unknown activation %d", act);
+    if (rows == 0) return QUAN_OK;
+    if (!x || !wq || !wscale || !out) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    if (rows >= (1LL << 31) || rows >= (1LL << 40) / K || rows >= (1LL << 40) / N ||
+        static_cast<long long>(K) * N >= (1LL << 34))
+        return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
+    const void* half[] = {x, out};
+    const void* vectors[] = {wscale, ep.bias, ep.scale, ep.shift};
+    if (misaligned(half, 2, 2) || misaligned(vectors, 4, 4) || misaligned(&wq, 1, 16))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "tensors must be aligned to their elements, the 8-bit letters to 16 bytes");
+    const int Kq = K / 4, Nq = N / 4;
+    const size_t need = quan::qpoint_f8_workspace_bytes(rows, Kq, Nq);
+    if (need > 0 && (!workspace || workspace_bytes < need ||
+                     reinterpret_cast<uintptr_t>(workspace) % 256 != 0))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "workspace must hold %zu bytes, 256-byte aligned (got %zu)", need,
+                    workspace_bytes);
+    const size_t wb = size_t(4) * Nq * quan::f8_pitch(Kq);
+    const size_t sb = size_t(16) * ((Nq + 127) / 128) * ((Kq + 127) / 128), cb = size_t(4) * N;
+    const Span outs[] = {{out, static_cast<size_t>(rows) * N * 2},
+                         {need ? workspace : nullptr, need}};
+    const Span ins[] = {{x, static_cast<size_t>(rows) * K * 2}, {wq, wb}, {wscale, sb},
+                        {ep.bias, cb}, {ep.scale, cb}, {ep.shift, cb}};
+    const unsigned equal[] = {0u, 0u};
+    if (clash(outs, 2, ins, 6, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "out or the workspace overlaps another tensor");
+    int num_sms = 0, cc = 0;
+    cudaError_t e;
+    if (!device_info(&num_sms, &cc, &e)) return cuda_fail(e, "device query");
+    if (cc != 103)
+        return fail(QUAN_ERR_UNSUPPORTED, "the 8-bit product needs sm_103 (device cc %d)", cc);
+    char err[256] = "";
+    e = quan::launch_qpoint_f8(x, wq, wscale, ep, rows, Kq, Nq, conj, act, workspace, out,
+                               num_sms, g_wait_limit.load(), g_inject.load(),
+                               reinterpret_cast<cudaStream_t>(stream), err, sizeof(err));
+    if (err[0] != '\0') return fail(QUAN_ERR_UNSUPPORTED, "%s", err);
+    if (e != cudaSuccess) return cuda_fail(e, "qpoint_f8 launch");
+    return QUAN_OK;
+}
+
 }  // namespace
 
 thread_local const char* quan::last_variant = "";
@@ -1020,6 +1075,60 @@ quan_status_t quan_residual_join_bwd(const void* dy, const void* dn, const void*
                                reinterpret_cast<cudaStream_t>(stream));
     if (ce != cudaSuccess) return cuda_fail(ce, "residual join gradient launch");
     return QUAN_OK;
+}
+
+size_t quan_f8_weights_bytes(int Cin, int Cout, int transpose) {
+    if (Cin < 1 || Cout < 1 || Cin % 4 || Cout % 4) return 0;
+    const int n = (transpose ? Cin : Cout) / 4, k = (transpose ? Cout : Cin) / 4;
+    return size_t(4) * n * quan::f8_pitch(k);
+}
+
+quan_status_t quan_f8_weights(const void* wr, const void* wi, const void* wj, const void* wk,
+                              int Cin, int Cout, int transpose, void* q, float* scale,
+                              quan_stream_t stream) {
+    const void* w[4] = {wr, wi, wj, wk};
+    if (!wr || !wi || !wj || !wk || !q || !scale)
+        return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    if (Cin < 1 || Cout < 1 || Cin % 4 || Cout % 4)
+        return fail(QUAN_ERR_INVALID_ARG, "Cin=%d and Cout=%d must be positive multiples of 4",
+                    Cin, Cout);
+    if (static_cast<long long>(Cin) * Cout >= (1LL << 34) || Cout > 4 * 128 * 65535)
+        return fail(QUAN_ERR_UNSUPPORTED, "letters too large");
+    if (misaligned(w, 4, 2) || reinterpret_cast<uintptr_t>(q) % 16 != 0 ||
+        reinterpret_cast<uintptr_t>(scale) % 4 != 0)
+        return fail(QUAN_ERR_INVALID_ARG, "letters must be 2-byte, q 16-byte, scale 4-byte aligned");
+    const size_t wb = size_t(Cin / 4) * (Cout / 4) * 2;
+    const size_t sb = size_t(16) * ((Cin / 4 + 127) / 128) * ((Cout / 4 + 127) / 128);
+    const Span outs[] = {{q, quan_f8_weights_bytes(Cin, Cout, transpose)}, {scale, sb}};
+    const Span ins[] = {{wr, wb}, {wi, wb}, {wj, wb}, {wk, wb}};
+    const unsigned equal[] = {0u, 0u};
+    if (clash(outs, 2, ins, 4, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "q or scale overlaps another tensor");
+    const cudaError_t e = quan::launch_f8_letters(w, Cout / 4, Cin / 4, transpose != 0, q, scale,
+                                                  reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "f8 letters launch");
+    return QUAN_OK;
+}
+
+size_t quan_qpoint_f8_workspace_size(long long rows, int Cin, int Cout) {
+    if (rows < 1 || Cin < 1 || Cout < 1 || Cin % 4 || Cout % 4) return 0;
+    return quan::qpoint_f8_workspace_bytes(rows, Cin / 4, Cout / 4);
+}
+
+quan_status_t quan_qpoint_f8_fwd(const void* x, const void* wq, const float* wscale,
+                                 const float* bias, const float* iqbn_scale,
+                                 const float* iqbn_shift, long long rows, int Cin, int Cout,
+                                 int act, void* workspace, size_t workspace_bytes, void* out,
+                                 quan_stream_t stream) {
+    return run_qpoint_f8(x, wq, wscale, {bias, iqbn_scale, iqbn_shift, nullptr}, rows, Cin, Cout,
+                         act, false, workspace, workspace_bytes, out, stream);
+}
+
+quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const float* wscale,
+                                      long long rows, int Cin, int Cout, void* workspace,
+                                      size_t workspace_bytes, void* dx, quan_stream_t stream) {
+    return run_qpoint_f8(dy, wq, wscale, {nullptr, nullptr, nullptr, nullptr}, rows, Cout, Cin,
+                         QUAN_ACT_NONE, true, workspace, workspace_bytes, dx, stream);
 }
 
 quan_status_t quan_set_path(int path) {

@@ -12,6 +12,7 @@ import os
 import re
 import struct
 import threading
+import typing
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG_DIR, "libquan.so")
@@ -100,6 +101,15 @@ def load():
                                                [_vp] * 6)
         lib.quan_residual_join_bwd_workspace_size.argtypes = [_ll, _i, _i, _ll]
         lib.quan_residual_join_bwd_workspace_size.restype = ctypes.c_size_t
+        lib.quan_f8_weights.argtypes = [_vp] * 4 + [_i, _i, _i, _vp, _vp, _vp]
+        lib.quan_f8_weights_bytes.argtypes = [_i, _i, _i]
+        lib.quan_f8_weights_bytes.restype = ctypes.c_size_t
+        lib.quan_qpoint_f8_fwd.argtypes = ([_vp] * 6 + [_ll, _i, _i, _i, _vp, ctypes.c_size_t] +
+                                           [_vp] * 2)
+        lib.quan_qpoint_f8_bwd_data.argtypes = ([_vp] * 3 + [_ll, _i, _i, _vp, ctypes.c_size_t] +
+                                                [_vp] * 2)
+        lib.quan_qpoint_f8_workspace_size.argtypes = [_ll, _i, _i]
+        lib.quan_qpoint_f8_workspace_size.restype = ctypes.c_size_t
         lib.quan_set_path.argtypes = [_i]
         lib.quan_last_path.argtypes = []
         lib.quan_last_kernel.argtypes = []
@@ -129,7 +139,8 @@ def load():
                      "quan_qconv2d_bwd_data_static", "quan_iqbn_batch_stats",
                      "quan_qconv2d_maxpool_fwd", "quan_qconv2d_maxpool_rgb_fwd",
                      "quan_iqbn_train_fwd", "quan_dropout", "quan_residual_join_fwd",
-                     "quan_residual_join_bwd",
+                     "quan_residual_join_bwd", "quan_f8_weights", "quan_qpoint_f8_fwd",
+                     "quan_qpoint_f8_bwd_data",
                      "quan_qconv2d_sep_bwd_weight",
                      "quan_maxpool2d_fwd", "quan_set_path", "quan_set_tc_tiles",
                      "quan_set_wait_limit_ns", "quan_device_status", "quan_set_fault_injection",
@@ -190,6 +201,8 @@ _TRAIN = struct.Struct("7qd3q").pack
 _SIZES = struct.Struct("9q").pack
 _DROPOUT = struct.Struct("3qd2Q3q").pack
 _JOIN_FWD = struct.Struct("10q3d2Q4q").pack
+_QPOINT_F8 = struct.Struct("14q").pack
+_QPOINT_F8_BWD = struct.Struct("10q").pack
 _JOIN_BWD = struct.Struct("12q3d2Q9q").pack
 
 
@@ -629,6 +642,106 @@ def dropout(x, p, seed, offset=0, *, counter=None, out=None, stream=None):
     else:
         _check_tensor("out", out, x.shape, x.dtype)
     quan_dropout(x, x.numel(), dtype, p, seed, offset, counter, out, stream)
+    return out
+
+
+def quan_f8_weights(wr, wi, wj, wk, Cin, Cout, transpose, q, scale, stream=None) -> None:
+    _check(load().quan_f8_weights(_ptr(wr), _ptr(wi), _ptr(wj), _ptr(wk), Cin, Cout,
+                                  1 if transpose else 0, _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def quan_f8_weights_bytes(Cin, Cout, transpose) -> int:
+    return load().quan_f8_weights_bytes(Cin, Cout, 1 if transpose else 0)
+
+
+def quan_qpoint_f8_workspace_size(rows, Cin, Cout) -> int:
+    return load().quan_qpoint_f8_workspace_size(rows, Cin, Cout)
+
+
+def quan_qpoint_f8_fwd(x, wq, wscale, bias, iqbn_scale, iqbn_shift, rows, Cin, Cout, act,
+                       workspace, workspace_bytes, out, stream=None) -> None:
+    _call(16, _QPOINT_F8(_addr(x), _addr(wq), _addr(wscale), _addr(bias), _addr(iqbn_scale),
+                         _addr(iqbn_shift), rows, Cin, Cout, act, _addr(workspace),
+                         workspace_bytes, _addr(out), _stream(stream)))
+
+
+def quan_qpoint_f8_bwd_data(dy, wq, wscale, rows, Cin, Cout, workspace, workspace_bytes, dx,
+                            stream=None) -> None:
+    _call(17, _QPOINT_F8_BWD(_addr(dy), _addr(wq), _addr(wscale), rows, Cin, Cout,
+                             _addr(workspace), workspace_bytes, _addr(dx), _stream(stream)))
+
+
+class F8Weights(typing.NamedTuple):
+    """Letters of a pointwise layer in 8-bit floating point, as quantize_f8_weights lays them
+    out: q e4m3 [4, n, pitch], scale fp32 [4, ceil(n / 128), ceil(k / 128)]; n, k = Cout / 4,
+    Cin / 4, or the other way round when transposed (for the input gradient)."""
+    q: object
+    scale: object
+    Cin: int
+    Cout: int
+    transposed: bool
+
+
+def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
+    """The four letters [Cout/4, 1, 1, Cin/4] (bf16, CUDA) of a pointwise layer as F8Weights for
+    qpointwise_f8, or with transpose=True for qpointwise_f8_backward_data: e4m3 with a
+    power-of-two scale for each 128 x 128 block."""
+    import torch
+    Qout, kh, kw, Qin = wr.shape
+    if kh != 1 or kw != 1:
+        raise ValueError("the letters of a pointwise layer are [Cout/4, 1, 1, Cin/4]")
+    for name, w in (("wr", wr), ("wi", wi), ("wj", wj), ("wk", wk)):
+        _check_tensor(name, w, wr.shape, torch.bfloat16)
+    n, k = (Qin, Qout) if transpose else (Qout, Qin)
+    need = quan_f8_weights_bytes(4 * Qin, 4 * Qout, transpose)
+    if need == 0:
+        raise ValueError("a layer has at least four input and output channels")
+    q = _empty(stream, (4, n, need // (4 * n)), torch.float8_e4m3fn, wr.device)
+    scale = _empty(stream, (4, -(-n // 128), -(-k // 128)), torch.float32, wr.device)
+    quan_f8_weights(wr, wi, wj, wk, 4 * Qin, 4 * Qout, transpose, q, scale, stream)
+    return F8Weights(q, scale, 4 * Qin, 4 * Qout, bool(transpose))
+
+
+def _qpoint_f8(x, w, K, N, workspace, out, stream):
+    """rows, workspace and output of one 8-bit product of K input and N output channels."""
+    import torch
+    _check_tensor("x", x, x.shape[:-1] + (K,), torch.bfloat16)
+    rows = x.numel() // K
+    if out is None:
+        out = _empty(stream, x.shape[:-1] + (N,), torch.bfloat16, x.device)
+    else:
+        _check_tensor("out", out, x.shape[:-1] + (N,), torch.bfloat16)
+    need = quan_qpoint_f8_workspace_size(rows, K, N)
+    if workspace is None and need:
+        workspace = _empty(stream, (need,), torch.uint8, x.device)
+    return rows, workspace, \
+        0 if workspace is None else workspace.numel() * workspace.element_size(), out
+
+
+def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE, workspace=None,
+                  out=None, stream=None):
+    """Pointwise quaternion convolution in 8-bit floating point: bf16 x [..., Cin] (CUDA), which
+    is quantised in the call, and w = quantize_f8_weights(...) -> bf16 [..., Cout],
+    act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d."""
+    import torch
+    if w.transposed:
+        raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
+    for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
+        if v is not None:
+            _check_tensor(name, v, (w.Cout,), torch.float32)
+    rows, workspace, nbytes, out = _qpoint_f8(x, w, w.Cin, w.Cout, workspace, out, stream)
+    quan_qpoint_f8_fwd(x, w.q, w.scale, bias, scale, shift, rows, w.Cin, w.Cout, act, workspace,
+                       nbytes, out, stream)
+    return out
+
+
+def qpointwise_f8_backward_data(dy, w, *, workspace=None, out=None, stream=None):
+    """Input gradient of that convolution before its epilogue: bf16 dy [..., Cout] (CUDA),
+    quantised in the call, and w = quantize_f8_weights(..., transpose=True) -> bf16 [..., Cin]."""
+    if not w.transposed:
+        raise ValueError("w holds the forward letters: quantize_f8_weights(..., transpose=True)")
+    rows, workspace, nbytes, out = _qpoint_f8(dy, w, w.Cout, w.Cin, workspace, out, stream)
+    quan_qpoint_f8_bwd_data(dy, w.q, w.scale, rows, w.Cin, w.Cout, workspace, nbytes, out, stream)
     return out
 
 
