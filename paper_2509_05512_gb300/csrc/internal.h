@@ -235,6 +235,12 @@ cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, f
 int f8_pitch(int Kq);
 cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool transpose, void* q,
                               float* scale, cudaStream_t stream);
+// Status word of its kernels, as read_and_clear_status.
+cudaError_t read_and_clear_status_f8(unsigned* status, cudaStream_t stream);
+// Tiled map of a byte tensor of three dimensions, innermost first (strides: of the outer two, in
+// bytes), boxes with the 128-byte swizzle, 0 past the ends (qconv_tc.cu).
+bool encode_bytes_3d(CUtensorMap* map, const void* base, const unsigned long long dims[3],
+                     const unsigned long long strides[2], const unsigned box[3]);
 size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq);
 cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
                              const EpilogueArgs& ep, long long rows, int Kq, int Nq, bool conj,

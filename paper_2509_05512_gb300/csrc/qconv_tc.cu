@@ -2510,6 +2510,17 @@ cudaError_t launch_bwd_weight_tc(const ConvShape& s, const void* x, const void* 
 
 const char* last_tc_kernel() { return t_kernel_name; }
 
+bool encode_bytes_3d(CUtensorMap* map, const void* base, const unsigned long long dims[3],
+                     const unsigned long long strides[2], const unsigned box[3]) {
+    if (!load_encoders()) return false;
+    const cuuint64_t d[3] = {dims[0], dims[1], dims[2]}, s[2] = {strides[0], strides[1]};
+    const cuuint32_t b[3] = {box[0], box[1], box[2]}, one[3] = {1, 1, 1};
+    return g_encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), d, s, b,
+                          one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t read_and_clear_status(unsigned* status, cudaStream_t stream) {
     cudaError_t e = cudaMemcpyFromSymbolAsync(status, g_status, sizeof(unsigned), 0,
                                               cudaMemcpyDeviceToHost, stream);

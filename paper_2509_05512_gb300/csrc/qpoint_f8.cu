@@ -12,6 +12,8 @@
 // padding; s_x [4][blocks][rows], s_w [4][ceil(Nq / 128)][blocks].
 #include <cuda_bf16.h>
 
+#include <cstdio>
+
 #include "f8.cuh"
 #include "internal.h"
 #include "ptx.cuh"
@@ -230,6 +232,51 @@ cudaError_t launch_rows(const F8Params& p, bool vec, cudaStream_t stream) {
                : launch_pdl(qpoint_rows_kernel<RT, false>, g, dim3(256), 0, stream, p);
 }
 
+// ------------------------------------------------------------------ rows in 8 bits
+
+// A half-warp a block of 128 channels, 16 bytes a lane: the block's scale, then its 8-bit values.
+// Bound by HBM: 2 bytes read, 1 written a channel.
+struct F8Rows {
+    const __nv_bfloat16* x;  // [rows][4 Kq]
+    uint8_t* q;              // [rows][4][Kp]
+    float* scale;            // [4][kblk][rows]
+    long long rows;
+    int Kq, Kp, kblk;
+};
+template <bool VEC>
+__global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
+    griddep_launch_dependents();
+    griddep_wait();
+    const int hl = threadIdx.x & 15;
+    const int per_row = 4 * p.kblk;
+    const long long units = p.rows * per_row;
+    // whole warps stay together: the scale is taken with full-warp shuffles
+    for (long long u0 = static_cast<long long>(blockIdx.x) * 16 + (threadIdx.x >> 5) * 2;
+         u0 < units; u0 += static_cast<long long>(gridDim.x) * 16) {
+        const long long u = u0 + ((threadIdx.x >> 4) & 1);
+        const bool in = u < units;
+        const long long row = u / per_row;
+        const int rest = static_cast<int>(u - row * per_row);
+        const int ci = rest / p.kblk, b = rest - ci * p.kblk, k = b * F8_BLOCK + hl * 8;
+        float v[8], inv;
+        if (in) {
+            load_x8<VEC>(p.x + row * (4LL * p.Kq) + ci * p.Kq, k, p.Kq, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        }
+        const float s = half_warp_scale(v, inv);
+        if (!in) continue;
+        if (hl == 0) p.scale[(static_cast<long long>(ci) * p.kblk + b) * p.rows + row] = s;
+        if (k < p.Kp)
+            *reinterpret_cast<uint2*>(p.q + (row * 4 + ci) * p.Kp + k) = make_uint2(
+                f8x4_from_f32(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                f8x4_from_f32(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+    }
+}
+
+#include "qpoint_f8_tc.cuh"
+
 int blocks_of(int q) { return (q + F8_BLOCK - 1) / F8_BLOCK; }
 
 }  // namespace
@@ -253,11 +300,55 @@ cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool tr
                      : launch_pdl(f8_letters_kernel<false>, g, dim3(256), 0, stream, p);
 }
 
+namespace {
+
+// Rows up to which the CUDA-core kernel runs.
+constexpr int F8_FEW_ROWS = 4;
+
+size_t quantised_bytes(long long rows, int Kq) {
+    return (static_cast<size_t>(rows) * 4 * f8_pitch(Kq) + 255) / 256 * 256;
+}
+
+// Quaternion output channels of a tile, by the estimated clocks of the waves of tiles.
+int f8_tile_width(long long rows, int Kq, int Nq, int num_sms) {
+    const int widths[3] = {64, 32, 16}, partial[3] = {512, 320, 220}, rest[3] = {800, 500, 400};
+    int best = 64;
+    double least = 0.0;
+    for (int i = 0; i < 3; ++i) {
+        const long long tiles = (rows + F8_BM - 1) / F8_BM * ((Nq + widths[i] - 1) / widths[i]);
+        const long long waves = (tiles + num_sms - 1) / num_sms;
+        const double t = static_cast<double>(waves) *
+                         (4.0 * blocks_of(Kq) * partial[i] + rest[i]);
+        if (i == 0 || t < least) best = widths[i], least = t;
+    }
+    return best;
+}
+
+template <int BNQ>
+cudaError_t launch_f8_tc(const CUtensorMap& mx, const CUtensorMap& mw, const F8TcParams& p,
+                         int num_sms, cudaStream_t stream) {
+    using C = F8Cfg<BNQ>;
+    const cudaError_t e = cudaFuncSetAttribute(
+        qpoint_f8_kernel<BNQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
+    if (e != cudaSuccess) return e;
+    static const cudaError_t regs = [] {  // the exchange counts on the launch's registers
+        cudaFuncAttributes a;
+        const cudaError_t q = cudaFuncGetAttributes(&a, qpoint_f8_kernel<BNQ>);
+        return q != cudaSuccess ? q
+                                : (a.numRegs < F8_REGS ? cudaErrorInvalidKernelImage : cudaSuccess);
+    }();
+    if (regs != cudaSuccess) return regs;
+    const int grid = p.num_tiles < num_sms ? p.num_tiles : num_sms;
+    return launch_pdl(qpoint_f8_kernel<BNQ>, dim3(static_cast<unsigned>(grid)), dim3(F8_THREADS),
+                      C::SMEM_BYTES, stream, mx, mw, p);
+}
+
+}  // namespace
+
 size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq) {
-    (void)rows;
-    (void)Kq;
     (void)Nq;
-    return 0;
+    if (rows <= F8_FEW_ROWS) return 0;
+    return quantised_bytes(rows, Kq) + static_cast<size_t>(rows) * 4 * blocks_of(Kq) * 4;
 }
 
 cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
@@ -265,28 +356,76 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
                              int act, void* workspace, void* out, int num_sms,
                              unsigned long long wait_limit_ns, int inject_stall,
                              cudaStream_t stream, char* err, size_t errlen) {
-    (void)workspace;
-    (void)num_sms;
-    (void)wait_limit_ns;
-    (void)inject_stall;
-    (void)err;
-    (void)errlen;
-    F8Params p;
-    p.x = static_cast<const __nv_bfloat16*>(x);
-    p.wq = static_cast<const uint8_t*>(wq);
+    const int Kp = f8_pitch(Kq), kblk = blocks_of(Kq), nblk = blocks_of(Nq);
+    const bool vec = Kq % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+    auto* xb = static_cast<const __nv_bfloat16*>(x);
+    auto* ob = static_cast<__nv_bfloat16*>(out);
+    if (rows <= F8_FEW_ROWS) {
+        const F8Params p = {xb, static_cast<const uint8_t*>(wq), ws, ep, ob, rows, Kq, Nq, Kp,
+                            kblk, nblk, conj ? 1 : 0, act};
+        return launch_rows<4>(p, vec, stream);
+    }
+    auto* xq = static_cast<uint8_t*>(workspace);
+    auto* xs = reinterpret_cast<float*>(xq + quantised_bytes(rows, Kq));
+    const F8Rows r = {xb, xq, xs, rows, Kq, Kp, kblk};
+    const long long units = rows * 4 * kblk;
+    const long long blocks = (units + 15) / 16, cap = static_cast<long long>(num_sms) * 64;
+    const dim3 g(static_cast<unsigned>(blocks < cap ? blocks : cap));
+    cudaError_t e = vec ? launch_pdl(f8_rows_kernel<true>, g, dim3(256), 0, stream, r)
+                        : launch_pdl(f8_rows_kernel<false>, g, dim3(256), 0, stream, r);
+    if (e != cudaSuccess) return e;
+
+    const int bnq = f8_tile_width(rows, Kq, Nq, num_sms);
+    CUtensorMap mx, mw;
+    const unsigned long long dx[3] = {static_cast<unsigned long long>(Kq), 4,
+                                      static_cast<unsigned long long>(rows)};
+    const unsigned long long sx[2] = {static_cast<unsigned long long>(Kp), 4ull * Kp};
+    const unsigned bx[3] = {F8_BLOCK, 1, F8_BM};
+    const unsigned long long dw[3] = {static_cast<unsigned long long>(Kq),
+                                      static_cast<unsigned long long>(Nq), 4};
+    const unsigned long long sw[2] = {static_cast<unsigned long long>(Kp),
+                                      static_cast<unsigned long long>(Nq) * Kp};
+    const unsigned bw[3] = {F8_BLOCK, static_cast<unsigned>(bnq), 4};
+    if (!encode_bytes_3d(&mx, xq, dx, sx, bx) || !encode_bytes_3d(&mw, wq, dw, sw, bw)) {
+        snprintf(err, errlen, "cuTensorMapEncodeTiled failed for the 8-bit tensors");
+        return cudaErrorInvalidValue;
+    }
+    F8TcParams p = {};
+    p.xs = xs;
     p.ws = ws;
     p.ep = ep;
-    p.out = static_cast<__nv_bfloat16*>(out);
+    p.out = ob;
     p.rows = rows;
     p.Kq = Kq;
     p.Nq = Nq;
-    p.Kp = f8_pitch(Kq);
-    p.kblk = blocks_of(Kq);
-    p.nblk = blocks_of(Nq);
+    p.kblk = kblk;
+    p.nblk = nblk;
     p.conj = conj ? 1 : 0;
     p.act = act;
-    const bool vec = Kq % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
-    return launch_rows<4>(p, vec, stream);
+    p.ntiles = (Nq + bnq - 1) / bnq;
+    p.num_tiles = static_cast<int>((rows + F8_BM - 1) / F8_BM * p.ntiles);
+    const uintptr_t a = reinterpret_cast<uintptr_t>(out);
+    p.store = Nq % 16 == 0 && a % 32 == 0 ? 32 : (Nq % 8 == 0 && a % 16 == 0 ? 16 : 2);
+    p.wait_limit_ns = wait_limit_ns;
+    p.inject_stall = inject_stall;
+    switch (bnq) {
+        case 64: return launch_f8_tc<64>(mx, mw, p, num_sms, stream);
+        case 32: return launch_f8_tc<32>(mx, mw, p, num_sms, stream);
+        default: return launch_f8_tc<16>(mx, mw, p, num_sms, stream);
+    }
+}
+
+cudaError_t read_and_clear_status_f8(unsigned* status, cudaStream_t stream) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(status, g_status, sizeof(unsigned), 0,
+                                              cudaMemcpyDeviceToHost, stream);
+    if (e != cudaSuccess) return e;
+    e = cudaStreamSynchronize(stream);
+    if (e != cudaSuccess) return e;
+    const unsigned zero = 0;
+    e = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof(unsigned), 0, cudaMemcpyHostToDevice,
+                                stream);
+    if (e != cudaSuccess) return e;
+    return cudaStreamSynchronize(stream);
 }
 
 }  // namespace quan

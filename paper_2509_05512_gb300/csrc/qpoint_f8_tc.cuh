@@ -1,0 +1,418 @@
+// qpoint_f8_tc.cuh -- the 8-bit pointwise product on the tensor cores.  Included by qpoint_f8.cu
+// inside its anonymous namespace.
+//
+// A tile is 128 rows x BNQ quaternion output channels, all four output components.  For one
+// K block b (128 channels) and one input component ci a single MMA chain multiplies the rows'
+// component ci by the four letters stacked, N = 4 BNQ columns in the order r, i, j, k:
+//   P[m][L BNQ + n] = sum over k in b of q_x[m][ci][k] q_w[L][n][k]        (M 128, K 128)
+// and column group L of it belongs to output component co = L xor ci.  So the Hamilton product's
+// signs and its exchange of components cost nothing: the operands stay as they are in memory,
+// the letters of a K block serve all four input components (32 KB beside 4 x 16 KB of rows for
+// 4 x 512 clocks of MMAs, half of what a plain 128 x 256 tile of the real block matrix copies),
+// and the epilogue threads of component co read column group co xor ci and add it times
+//   sgn(co, ci) s_x[ci][b][m] s_w[L][b]
+// to their fp32 accumulators.  The scales change every 128 channels, so no sum runs in the tensor
+// core for longer than that.  Bound: the MMAs (8192 products a clock and SM) as long as a
+// partial's 128 x 256 values are taken out of TMEM, one fused multiply-add each (256 clocks of
+// the SM's FMA lanes), in the 512 clocks that the next partial's MMAs take: hence two TMEM
+// buffers, and eight epilogue warps that load a chunk of columns while they add the one before.
+// A thread keeps 2 x BNQ accumulators, so the epilogue's two warpgroups take registers that the
+// other warps hand back.
+//
+// BNQ = 64, 32 or 16: with few row tiles the narrower ones spread the letters over more SMs (see
+// f8_tile_width).
+//
+// Roles (12 warps, one CTA per SM, persistent over tiles, channel tiles first):
+//   warp 0      TMA producer: per K block the letters' box, then the rows' box of each component;
+//   warp 1      TMEM owner and MMA issuer;
+//   warps 4..11 epilogue: components 2 g and 2 g + 1 of warpgroup g = 0 or 1 (warps 4..7, 8..11),
+//               TMEM lane quadrant warp mod 4.
+// Waits are bounded like every kernel here (tc_common.cuh).
+
+constexpr int F8_THREADS = 12 * 32;
+constexpr int F8_EPI_WARP0 = 4;
+constexpr int F8_EPI_WARPS = 8;
+constexpr int F8_BM = 128;
+// Registers a thread: at launch, and after the warpgroups' exchange.  An increase waits until
+// the block's own registers cover it, so the shares must not pass the launch's total.
+constexpr int F8_REGS = 168, F8_REGS_ISSUE = 40, F8_REGS_EPI = 232;
+static_assert(128 * F8_REGS_ISSUE + 256 * F8_REGS_EPI <= F8_THREADS * F8_REGS, "register shares");
+
+struct F8TcParams {
+    const float* xs;  // [4][kblk][rows]
+    const float* ws;  // [4][nblk][kblk]
+    EpilogueArgs ep;
+    __nv_bfloat16* out;  // [rows][4 Nq]
+    long long rows;
+    int Kq, Nq, kblk, nblk;
+    int conj, act;
+    int ntiles, num_tiles;
+    int store;  // bytes of a store: 32, 16 or 2 (by Nq and the output's alignment)
+    unsigned long long wait_limit_ns;
+    int inject_stall;
+};
+
+template <int BNQ>
+struct F8Cfg {
+    static constexpr int A_STAGE = F8_BM * F8_BLOCK;    // one component of 128 rows: 16 KB
+    static constexpr int B_STAGE = 4 * BNQ * F8_BLOCK;  // four letters
+    static constexpr int A_STAGES = 8, B_STAGES = 2;
+    static constexpr int RING = A_STAGES * A_STAGE + B_STAGES * B_STAGE;
+    static constexpr int VEC = F8_EPI_WARPS * 2 * 2 * BNQ * 4;  // each epilogue warp's vectors
+    // full and empty (A, B), accf, acce (2 buffers), drain
+    static constexpr int NUM_BARS = 2 * (A_STAGES + B_STAGES) + 4 + 1;
+    static constexpr int SMEM_BYTES = 1024 + RING + VEC + NUM_BARS * 8 + 16;
+    static constexpr uint32_t DESC_HI = tc::desc_hi(8 * 128, tc::desc_layout(128));
+    static constexpr uint32_t TMEM_COLS = 2 * 4 * BNQ;  // 512, 256 or 128
+    // kind::f8f6f4: e4m3 A and B (format 0), fp32 D, both K-major
+    static constexpr uint32_t IDESC = (1u << 4) | (static_cast<uint32_t>(4 * BNQ / 8) << 17) |
+                                      (static_cast<uint32_t>(F8_BM / 16) << 24);
+    static_assert(SMEM_BYTES <= 227 * 1024, "8-bit ring");
+};
+
+// D[tmem] (+)= A[smem] * B[smem]^T, kind::f8f6f4, K = 32.
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
+                                        uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 ad, bd;\n\t"
+        "mov.b64 ad, {%1, %3};\n\t"
+        "mov.b64 bd, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, uint32_t bar, int c0,
+                                            int c1, int c2, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy)
+        : "memory");
+}
+
+// 32 bytes of one row in one store: a full sector, where two 16-byte stores would reach L2 as
+// two halves of it.
+__device__ __forceinline__ void st_global_na_32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
+                     p),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
+                 "r"(v[7])
+                 : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[N]) {
+    if constexpr (N == 32)
+        tmem_ld_32x32b_x32(taddr, v);
+    else
+        tmem_ld_32x32b_x16(taddr, v);
+}
+template <int N>
+__device__ __forceinline__ void f8_add(const uint32_t (&v)[N], float f, float* acc) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = fmaf(f, __uint_as_float(v[j]), acc[j]);
+}
+
+template <int BNQ>
+__global__ void __launch_bounds__(F8_THREADS, 1)
+    qpoint_f8_kernel(const __grid_constant__ CUtensorMap tmap_x,
+                     const __grid_constant__ CUtensorMap tmap_w, const F8TcParams p) {
+    using C = F8Cfg<BNQ>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t ring_a = smem_u32(smem), ring_b = ring_a + C::A_STAGES * C::A_STAGE;
+    float* vectors = reinterpret_cast<float*>(smem + C::RING);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::VEC);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t full_a = bar0, empty_a = full_a + 8u * C::A_STAGES;
+    const uint32_t full_b = empty_a + 8u * C::A_STAGES, empty_b = full_b + 8u * C::B_STAGES;
+    const uint32_t accf = empty_b + 8u * C::B_STAGES, acce = accf + 16u, drain_bar = acce + 16u;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint64_t limit = p.wait_limit_ns;
+    auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) {
+        return tc::wait_or_abort(bar, parity, limit, abort_flag, code);
+    };
+
+    griddep_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::A_STAGES; ++i) {
+            mbar_init(full_a + 8u * i, 1);
+            mbar_init(empty_a + 8u * i, 1);
+        }
+        for (int i = 0; i < C::B_STAGES; ++i) {
+            mbar_init(full_b + 8u * i, 1);
+            mbar_init(empty_b + 8u * i, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(accf + 8u * b, 1);
+            mbar_init(acce + 8u * b, F8_EPI_WARPS);
+        }
+        mbar_init(drain_bar, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 0 && lane == 0) {
+        tma_prefetch_desc(&tmap_x);
+        tma_prefetch_desc(&tmap_w);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+
+    if (warp < F8_EPI_WARP0)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F8_REGS_ISSUE));
+    if (warp == 0) {
+        // ------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            griddep_wait();  // the quantised rows are complete
+            const uint64_t pol_x = l2_policy_evict_normal(), pol_w = l2_policy_evict_last();
+            uint32_t filled_a = 0, parity_a = 0, filled_b = 0, parity_b = 0;
+            uint32_t phase_a = 0, phase_b = 0;
+            int sa = 0, sb = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
+                const int mt = t / p.ntiles, nt = t - mt * p.ntiles;
+                for (int kb = 0; ok && kb < p.kblk; ++kb) {
+                    if (!wait(empty_b + 8u * sb, phase_b ^ 1u, STATUS_TIMEOUT_PRODUCER)) {
+                        ok = false;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(full_b + 8u * sb, C::B_STAGE);
+                    filled_b |= 1u << sb;
+                    parity_b = (parity_b & ~(1u << sb)) | (phase_b << sb);
+                    tma_load_3d(ring_b + sb * C::B_STAGE, &tmap_w, full_b + 8u * sb,
+                                kb * F8_BLOCK, nt * BNQ, 0, pol_w);
+                    if (++sb == C::B_STAGES) sb = 0, phase_b ^= 1u;
+                    for (int ci = 0; ci < 4; ++ci) {
+                        if (!wait(empty_a + 8u * sa, phase_a ^ 1u, STATUS_TIMEOUT_PRODUCER)) {
+                            ok = false;
+                            break;
+                        }
+                        mbar_arrive_expect_tx(full_a + 8u * sa, C::A_STAGE);
+                        filled_a |= 1u << sa;
+                        parity_a = (parity_a & ~(1u << sa)) | (phase_a << sa);
+                        tma_load_3d(ring_a + sa * C::A_STAGE, &tmap_x, full_a + 8u * sa,
+                                    kb * F8_BLOCK, ci, mt * F8_BM, pol_x);
+                        if (++sa == C::A_STAGES) sa = 0, phase_a ^= 1u;
+                    }
+                }
+            }
+            if (!ok || *abort_flag) {
+                tc::drain_fills(full_a, C::A_STAGES, filled_a, parity_a, limit);
+                tc::drain_fills(full_b, C::B_STAGES, filled_b, parity_b, limit);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            bool ok = true;
+            int issued = 0;
+            if (p.inject_stall) {
+                // Failure injection: wait on a barrier nothing arrives on.
+                wait(drain_bar, 0, STATUS_TIMEOUT_MMA);
+                ok = false;
+            }
+            int sa = 0, sb = 0, it = 0;
+            uint32_t phase_a = 0, phase_b = 0;
+            for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
+                for (int kb = 0; ok && kb < p.kblk; ++kb) {
+                    const int left = p.Kq - kb * F8_BLOCK;  // channels of this block
+                    const int steps = left >= F8_BLOCK ? 4 : (left + 31) / 32;
+                    if (!wait(full_b + 8u * sb, phase_b, STATUS_TIMEOUT_MMA)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t b_lo = tc::desc_lo(ring_b + sb * C::B_STAGE);
+                    for (int ci = 0; ci < 4; ++ci, ++it) {
+                        const int buf = it & 1;
+                        if (!wait(acce + 8u * buf, ((it >> 1) & 1) ^ 1, STATUS_TIMEOUT_MMA) ||
+                            !wait(full_a + 8u * sa, phase_a, STATUS_TIMEOUT_MMA)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t d = tmem_base + static_cast<uint32_t>(buf * 4 * BNQ);
+                        const uint32_t a_lo = tc::desc_lo(ring_a + sa * C::A_STAGE);
+                        for (int kk = 0; kk < steps; ++kk)  // 32 channels: 32 bytes into a row
+                            umma_f8(d, a_lo + 2 * kk, b_lo + 2 * kk, C::DESC_HI, C::IDESC,
+                                    kk != 0 ? 1u : 0u);
+                        ++issued;
+                        umma_commit(empty_a + 8u * sa);
+                        if (ci == 3) umma_commit(empty_b + 8u * sb);
+                        umma_commit(accf + 8u * buf);
+                        if (++sa == C::A_STAGES) sa = 0, phase_a ^= 1u;
+                    }
+                    if (++sb == C::B_STAGES) sb = 0, phase_b ^= 1u;
+                }
+            }
+            if (!ok && issued > 0) {
+                // let the issued MMAs finish before TMEM is released
+                umma_commit(drain_bar);
+                const uint64_t t1 = global_timer_ns();
+                while (!mbar_try_wait(drain_bar, 0u)) {
+                    if (global_timer_ns() - t1 > limit) {
+                        atomicOr(&g_status, STATUS_TIMEOUT_DRAIN);
+                        break;
+                    }
+                }
+            }
+        }
+    } else if (warp >= F8_EPI_WARP0) {
+        // ---------------------------------------------------------------- epilogue
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F8_REGS_EPI));
+        griddep_wait();  // the rows' scales; the output no longer read by an earlier kernel
+        constexpr int CH = BNQ == 16 ? 16 : 32;  // columns of a load
+        constexpr int PER = BNQ / CH;            // loads of a component
+        const int co0 = 2 * ((warp - F8_EPI_WARP0) / 4), qd = warp & 3;
+        float* scale = vectors + (warp - F8_EPI_WARP0) * 4 * BNQ;  // [2][BNQ]
+        float* shift = scale + 2 * BNQ;
+        const bool affine = p.ep.bias || p.ep.scale;
+        const long long xs_step = static_cast<long long>(p.kblk) * p.rows;  // to the next component
+        const long long ws_step = static_cast<long long>(p.nblk) * p.kblk;  // to the next letter
+        // bit 4 c + ci: sgn(co0 + c, ci), and conj(W)'s sign of letter co xor ci
+        uint32_t neg = (tc::NEG_MASK >> (4 * co0)) & 0xFFu;
+        if (p.conj) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((co0 + (i >> 2)) != (i & 3)) neg ^= 1u << i;
+        }
+        int it = 0;
+        bool ok = true;
+        for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
+            const int mt = t / p.ntiles, nt = t - mt * p.ntiles;
+            const long long row = static_cast<long long>(mt) * F8_BM + qd * 32 + lane;
+            const bool in = row < p.rows;
+            const int n0 = nt * BNQ;
+            if (affine) {
+                __syncwarp();  // the previous tile's reads
+                for (int j = lane; j < 2 * BNQ; j += 32) {
+                    const int n = n0 + (j & (BNQ - 1));
+                    const int c = (co0 + j / BNQ) * p.Nq + n;
+                    const bool col = n < p.Nq;
+                    const float sc = p.ep.scale && col ? __ldg(p.ep.scale + c) : 1.0f;
+                    const float b = p.ep.bias && col ? __ldg(p.ep.bias + c) : 0.0f;
+                    scale[j] = sc;
+                    shift[j] = fmaf(sc, b, p.ep.scale && col ? __ldg(p.ep.shift + c) : 0.0f);
+                }
+                __syncwarp();
+            }
+            const float* xs = p.xs + (in ? row : 0);
+            const float* ws = p.ws + static_cast<long long>(n0 / F8_BLOCK) * p.kblk;
+            float acc[2][BNQ];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < BNQ; ++j) acc[c][j] = 0.0f;
+            // the first block's scales; each later block's are loaded a block ahead
+            float fx[4], fw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fx[i] = in ? __ldg(xs + i * xs_step) : 0.0f;
+                fw[i] = __ldg(ws + (co0 ^ i) * ws_step);
+            }
+            for (int kb = 0; ok && kb < p.kblk; ++kb) {
+                // letter co0 xor i is that of component co0 with input i, and of component
+                // co0 + 1 with input i xor 1
+                float f[2][4];
+#pragma unroll
+                for (int ci = 0; ci < 4; ++ci) {
+                    f[0][ci] = (neg >> ci) & 1u ? -(fx[ci] * fw[ci]) : fx[ci] * fw[ci];
+                    f[1][ci] = (neg >> (4 + ci)) & 1u ? -(fx[ci] * fw[ci ^ 1])
+                                                      : fx[ci] * fw[ci ^ 1];
+                }
+                if (kb + 1 < p.kblk) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        fx[i] = in ? __ldg(xs + i * xs_step + (kb + 1) * p.rows) : 0.0f;
+                        fw[i] = __ldg(ws + (co0 ^ i) * ws_step + kb + 1);
+                    }
+                }
+#pragma unroll
+                for (int ci = 0; ci < 4; ++ci, ++it) {
+                    const int buf = it & 1;
+                    bool got = true;
+                    if (lane == 0)
+                        got = wait(accf + 8u * buf, (it >> 1) & 1, STATUS_TIMEOUT_EPILOGUE);
+                    if (__shfl_sync(0xffffffffu, got ? 1 : 0, 0) == 0) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t taddr = tmem_base + (static_cast<uint32_t>(qd * 32) << 16) +
+                                           static_cast<uint32_t>(buf * 4 * BNQ);
+                    // chunk i: columns CH (i mod PER) and up of component co0 + i / PER
+                    uint32_t v[2][CH];
+                    f8_load<CH>(taddr + (co0 ^ ci) * BNQ, v[0]);
+#pragma unroll
+                    for (int i = 0; i < 2 * PER; ++i) {
+                        tmem_ld_wait();
+                        if (i + 1 < 2 * PER) {
+                            f8_load<CH>(taddr + ((co0 + (i + 1) / PER) ^ ci) * BNQ +
+                                            CH * ((i + 1) % PER), v[(i + 1) & 1]);
+                        } else {
+                            // the partial is in registers: hand the buffer back to the issuer
+                            tc_fence_before();
+                            if (lane == 0) mbar_arrive_relaxed(acce + 8u * buf);
+                        }
+                        f8_add<CH>(v[i & 1], f[i / PER][ci], &acc[i / PER][CH * (i % PER)]);
+                    }
+                }
+            }
+            if (!ok) break;
+            if (!in) continue;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                __nv_bfloat16* out = p.out + row * (4LL * p.Nq) + (co0 + c) * p.Nq + n0;
+#pragma unroll
+                for (int g = 0; g < BNQ; g += 16) {
+                    uint32_t v[8];
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        float4 sc = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                        float4 sh = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (affine) {
+                            sc = *reinterpret_cast<const float4*>(scale + c * BNQ + g + j);
+                            sh = *reinterpret_cast<const float4*>(shift + c * BNQ + g + j);
+                        }
+                        const float* a = &acc[c][g + j];
+                        v[j / 2] = tc::pack_bf16x2(f8_act(fmaf(sc.x, a[0], sh.x), p.act),
+                                                   f8_act(fmaf(sc.y, a[1], sh.y), p.act));
+                        v[j / 2 + 1] = tc::pack_bf16x2(f8_act(fmaf(sc.z, a[2], sh.z), p.act),
+                                                       f8_act(fmaf(sc.w, a[3], sh.w), p.act));
+                    }
+                    const int left = p.Nq - n0 - g;
+                    if (left >= 16 && p.store == 32) {
+                        st_global_na_32(out + g, v);
+                    } else if (left >= 16 && p.store == 16) {
+                        st_global_na(out + g, make_uint4(v[0], v[1], v[2], v[3]));
+                        st_global_na(out + g + 8, make_uint4(v[4], v[5], v[6], v[7]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (j < left)
+                                reinterpret_cast<unsigned short*>(out)[g + j] =
+                                    static_cast<unsigned short>(v[j / 2] >> (16 * (j & 1)));
+                    }
+                }
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, C::TMEM_COLS);
+    }
+}

@@ -1184,9 +1184,12 @@ quan_status_t quan_set_fault_injection(int enable) {
 }
 
 quan_status_t quan_device_status(quan_stream_t stream, unsigned int* bits) {
-    unsigned v = 0;
+    unsigned v = 0, v8 = 0;
     cudaError_t e = quan::read_and_clear_status(&v, reinterpret_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess)
+        e = quan::read_and_clear_status_f8(&v8, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "device status");
+    v |= v8;
     if (bits) *bits = v;
     if (v) return fail(QUAN_ERR_DEVICE_TIMEOUT, "kernel wait timed out (status bits 0x%x)", v);
     return QUAN_OK;

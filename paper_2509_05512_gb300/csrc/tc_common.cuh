@@ -1,5 +1,5 @@
-// tc_common.cuh -- pieces shared by the tensor-core quaternion convolution kernels
-// (qconv_tc.cu is the only translation unit that includes this file): constants, the
+// tc_common.cuh -- pieces shared by the tensor-core kernels (qconv_tc.cu and qpoint_f8.cu include
+// this file, and each has a device status word of its own): constants, the
 // device status word, descriptor helpers, bounded waits, the issuer bookkeeping and the
 // register-only epilogues.
 #pragma once

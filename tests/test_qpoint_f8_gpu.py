@@ -236,3 +236,20 @@ def test_refuses_on_the_device():
         quan.qpointwise_f8(x, f, scale=torch.ones(64, device="cuda"))  # no shift
     with pytest.raises(quan.QuanError):
         quan.qpointwise_f8(x, f, out=x)
+
+
+def test_bounded_waits_report_a_timeout():
+    # the issuer waits on a barrier that nothing arrives on: every role gives up after the limit,
+    # the status says so, and the next call is right again
+    x, f, got = check(300, 512, 512, seed=8)
+    quan.quan_set_wait_limit_ns(20_000_000)
+    quan.quan_set_fault_injection(True)
+    try:
+        quan.qpointwise_f8(x, f)
+        st, bits = quan.quan_device_status()
+    finally:
+        quan.quan_set_fault_injection(False)
+        quan.quan_set_wait_limit_ns(0)
+    assert st == quan.QUAN_ERR_DEVICE_TIMEOUT and bits != 0
+    assert torch.equal(quan.qpointwise_f8(x, f), got)
+    assert quan.quan_device_status()[0] == quan.QUAN_OK
