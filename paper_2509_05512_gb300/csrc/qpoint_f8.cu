@@ -239,39 +239,50 @@ cudaError_t launch_rows(const F8Params& p, bool vec, cudaStream_t stream) {
 struct F8Rows {
     const __nv_bfloat16* x;  // [rows][4 Kq]
     uint8_t* q;              // [rows][4][Kp]
-    float* scale;            // [4][kblk][rows]
-    long long rows;
+    float* scale;            // [4][kblk][pitch]
+    long long rows, pitch;
     int Kq, Kp, kblk;
 };
+constexpr int F8_ROWS_UNROLL = 4;
 template <bool VEC>
 __global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
     griddep_launch_dependents();
     griddep_wait();
     const int hl = threadIdx.x & 15;
-    const int per_row = 4 * p.kblk;
-    const long long units = p.rows * per_row;
-    // whole warps stay together: the scale is taken with full-warp shuffles
-    for (long long u0 = static_cast<long long>(blockIdx.x) * 16 + (threadIdx.x >> 5) * 2;
-         u0 < units; u0 += static_cast<long long>(gridDim.x) * 16) {
-        const long long u = u0 + ((threadIdx.x >> 4) & 1);
-        const bool in = u < units;
-        const long long row = u / per_row;
-        const int rest = static_cast<int>(u - row * per_row);
-        const int ci = rest / p.kblk, b = rest - ci * p.kblk, k = b * F8_BLOCK + hl * 8;
-        float v[8], inv;
-        if (in) {
-            load_x8<VEC>(p.x + row * (4LL * p.Kq) + ci * p.Kq, k, p.Kq, v);
+    const unsigned per_row = 4u * p.kblk;
+    // a block's blocks of 128 follow one another in memory; all loads go out first
+    const long long u0 = static_cast<long long>(blockIdx.x) * (16 * F8_ROWS_UNROLL) +
+                         (threadIdx.x >> 4);
+    const long long first = u0 / per_row;
+    const unsigned rest0 = static_cast<unsigned>(u0 - first * per_row);
+    float v[F8_ROWS_UNROLL][8];
+#pragma unroll
+    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
+        const unsigned r = (rest0 + 16u * i) / per_row, rest = rest0 + 16u * i - r * per_row;
+        const long long row = first + r;
+        const unsigned ci = rest / p.kblk, b = rest - ci * p.kblk;
+        if (row < p.rows) {
+            load_x8<VEC>(p.x + row * (4LL * p.Kq) + static_cast<int>(ci) * p.Kq,
+                         static_cast<int>(b) * F8_BLOCK + hl * 8, p.Kq, v[i]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
         }
-        const float s = half_warp_scale(v, inv);
-        if (!in) continue;
-        if (hl == 0) p.scale[(static_cast<long long>(ci) * p.kblk + b) * p.rows + row] = s;
+    }
+#pragma unroll
+    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
+        const unsigned r = (rest0 + 16u * i) / per_row, rest = rest0 + 16u * i - r * per_row;
+        const long long row = first + r;
+        const unsigned ci = rest / p.kblk, b = rest - ci * p.kblk;
+        const int k = static_cast<int>(b) * F8_BLOCK + hl * 8;
+        float inv;
+        const float s = half_warp_scale(v[i], inv);  // whole warps: every lane takes part
+        if (row >= p.rows) continue;
+        if (hl == 0) p.scale[(static_cast<long long>(ci) * p.kblk + b) * p.pitch + row] = s;
         if (k < p.Kp)
             *reinterpret_cast<uint2*>(p.q + (row * 4 + ci) * p.Kp + k) = make_uint2(
-                f8x4_from_f32(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                f8x4_from_f32(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+                f8x4_from_f32(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv),
+                f8x4_from_f32(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv));
     }
 }
 
@@ -308,6 +319,10 @@ constexpr int F8_FEW_ROWS = 4;
 size_t quantised_bytes(long long rows, int Kq) {
     return (static_cast<size_t>(rows) * 4 * f8_pitch(Kq) + 255) / 256 * 256;
 }
+
+// Rows of the scales: whole tiles, so that a tile's are read without a bound (what stands past the
+// rows is never used).
+long long scale_pitch(long long rows) { return (rows + F8_BM - 1) / F8_BM * F8_BM; }
 
 // Quaternion output channels of a tile, by the estimated clocks of the waves of tiles.
 int f8_tile_width(long long rows, int Kq, int Nq, int num_sms) {
@@ -348,7 +363,7 @@ cudaError_t launch_f8_tc(const CUtensorMap& mx, const CUtensorMap& mw, const F8T
 size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq) {
     (void)Nq;
     if (rows <= F8_FEW_ROWS) return 0;
-    return quantised_bytes(rows, Kq) + static_cast<size_t>(rows) * 4 * blocks_of(Kq) * 4;
+    return quantised_bytes(rows, Kq) + static_cast<size_t>(scale_pitch(rows)) * 4 * blocks_of(Kq) * 4;
 }
 
 cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
@@ -367,10 +382,10 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     }
     auto* xq = static_cast<uint8_t*>(workspace);
     auto* xs = reinterpret_cast<float*>(xq + quantised_bytes(rows, Kq));
-    const F8Rows r = {xb, xq, xs, rows, Kq, Kp, kblk};
+    const long long pitch = scale_pitch(rows);
+    const F8Rows r = {xb, xq, xs, rows, pitch, Kq, Kp, kblk};
     const long long units = rows * 4 * kblk;
-    const long long blocks = (units + 15) / 16, cap = static_cast<long long>(num_sms) * 64;
-    const dim3 g(static_cast<unsigned>(blocks < cap ? blocks : cap));
+    const dim3 g(static_cast<unsigned>((units + 16 * F8_ROWS_UNROLL - 1) / (16 * F8_ROWS_UNROLL)));
     cudaError_t e = vec ? launch_pdl(f8_rows_kernel<true>, g, dim3(256), 0, stream, r)
                         : launch_pdl(f8_rows_kernel<false>, g, dim3(256), 0, stream, r);
     if (e != cudaSuccess) return e;
@@ -396,6 +411,7 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     p.ep = ep;
     p.out = ob;
     p.rows = rows;
+    p.pitch = pitch;
     p.Kq = Kq;
     p.Nq = Nq;
     p.kblk = kblk;

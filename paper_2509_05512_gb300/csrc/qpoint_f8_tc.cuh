@@ -17,14 +17,25 @@
 // the SM's FMA lanes), in the 512 clocks that the next partial's MMAs take: hence two TMEM
 // buffers, and eight epilogue warps that load a chunk of columns while they add the one before.
 // A thread keeps 2 x BNQ accumulators, so the epilogue's two warpgroups take registers that the
-// other warps hand back.
+// other warps hand back.  The factors are multiplied by a warp of their own, a K block ahead, into
+// shared memory: loaded by the epilogue's threads they put a load's latency, 500 clocks, into
+// every block (495 against 452 us for 25,600 rows 4096 -> 4096).
+//
+// What bounds it now: a buffer's round trip.  A partial's MMAs take 514 clocks, and 390 more pass
+// from their issue to their arrival at the epilogue; taking the partial out takes the slowest of
+// eight warps about 700, the way back to the issuer 200; two buffers make that about 1000 clocks a
+// partial.  Four buffers of 128 columns (BNQ = 32) hide the trip, but an MMA of 128 columns takes
+// 94 clocks, not 64 (the rows' operand is read again), and the epilogue's fixed work is per
+// partial: 563 us.
 //
 // BNQ = 64, 32 or 16: with few row tiles the narrower ones spread the letters over more SMs (see
 // f8_tile_width).
 //
 // Roles (12 warps, one CTA per SM, persistent over tiles, channel tiles first):
 //   warp 0      TMA producer: per K block the letters' box, then the rows' box of each component;
-//   warp 1      TMEM owner and MMA issuer;
+//   warps 1, 2  MMA issuers, one a TMEM buffer, taking partials in turn: the waits and commits of
+//               the one pass while the other's MMAs run, 5% over one issuer (warp 1 owns TMEM);
+//   warp 3      the factors of a K block: sgn(co, ci) s_x s_w for the tile's rows;
 //   warps 4..11 epilogue: components 2 g and 2 g + 1 of warpgroup g = 0 or 1 (warps 4..7, 8..11),
 //               TMEM lane quadrant warp mod 4.
 // Waits are bounded like every kernel here (tc_common.cuh).
@@ -35,15 +46,16 @@ constexpr int F8_EPI_WARPS = 8;
 constexpr int F8_BM = 128;
 // Registers a thread: at launch, and after the warpgroups' exchange.  An increase waits until
 // the block's own registers cover it, so the shares must not pass the launch's total.
-constexpr int F8_REGS = 168, F8_REGS_ISSUE = 40, F8_REGS_EPI = 232;
+constexpr int F8_REGS = 168, F8_REGS_ISSUE = 72, F8_REGS_EPI = 216;
 static_assert(128 * F8_REGS_ISSUE + 256 * F8_REGS_EPI <= F8_THREADS * F8_REGS, "register shares");
 
 struct F8TcParams {
-    const float* xs;  // [4][kblk][rows]
+    const float* xs;  // [4][kblk][pitch]
     const float* ws;  // [4][nblk][kblk]
     EpilogueArgs ep;
     __nv_bfloat16* out;  // [rows][4 Nq]
     long long rows;
+    long long pitch;  // rows rounded up to whole tiles
     int Kq, Nq, kblk, nblk;
     int conj, act;
     int ntiles, num_tiles;
@@ -59,9 +71,11 @@ struct F8Cfg {
     static constexpr int A_STAGES = 8, B_STAGES = 2;
     static constexpr int RING = A_STAGES * A_STAGE + B_STAGES * B_STAGE;
     static constexpr int VEC = F8_EPI_WARPS * 2 * 2 * BNQ * 4;  // each epilogue warp's vectors
-    // full and empty (A, B), accf, acce (2 buffers), drain
-    static constexpr int NUM_BARS = 2 * (A_STAGES + B_STAGES) + 4 + 1;
-    static constexpr int SMEM_BYTES = 1024 + RING + VEC + NUM_BARS * 8 + 16;
+    static constexpr int S_STAGES = 2, S_STAGE = 4 * 4 * F8_BM * 4;  // factors of a K block: 8 KB
+    static constexpr int SCALES = S_STAGES * S_STAGE;
+    // full and done (A), full and empty (B, factors), acce (2 buffers), drain (2 issuers)
+    static constexpr int NUM_BARS = 2 * (A_STAGES + B_STAGES + S_STAGES) + 2 + 2;
+    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + VEC + NUM_BARS * 8 + 16;
     static constexpr uint32_t DESC_HI = tc::desc_hi(8 * 128, tc::desc_layout(128));
     static constexpr uint32_t TMEM_COLS = 2 * 4 * BNQ;  // 512, 256 or 128
     // kind::f8f6f4: e4m3 A and B (format 0), fp32 D, both K-major
@@ -102,17 +116,89 @@ __device__ __forceinline__ void st_global_na_32(void* p, const uint32_t (&v)[8])
                  : "memory");
 }
 
+__device__ __forceinline__ float lds_f1(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+// v with its sign flipped.
+__device__ __forceinline__ float negate_if(float v, uint32_t flip) {
+    return __uint_as_float(__float_as_uint(v) ^ (flip << 31));
+}
+
 template <int N>
 __device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[N]) {
-    if constexpr (N == 32)
-        tmem_ld_32x32b_x32(taddr, v);
-    else
-        tmem_ld_32x32b_x16(taddr, v);
+#pragma unroll
+    for (int k = 0; k < N; k += 16)
+        tmem_ld_32x32b_x16(taddr + k, *reinterpret_cast<uint32_t(*)[16]>(&v[k]));
 }
 template <int N>
 __device__ __forceinline__ void f8_add(const uint32_t (&v)[N], float f, float* acc) {
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = fmaf(f, __uint_as_float(v[j]), acc[j]);
+}
+
+// SiLU of two values with one reciprocal: z / (1 + 2^(-z log2 e)) as tc::activate has it, the two
+// divisors inverted through their product (each below 2^61, the exponent being capped at 60: past
+// z = -41 the result's magnitude stays below 2^-54).  A tile's 32,768 values would take the
+// special function units 4096 clocks with two instructions each, and take 3072 with three a pair.
+__device__ __forceinline__ void f8_silu2(float& a, float& b) {
+    const float u = 1.0f + ex2_approx_ftz(fminf(a * -1.44269504f, 60.0f));
+    const float v = 1.0f + ex2_approx_ftz(fminf(b * -1.44269504f, 60.0f));
+    const float r = rcp_approx_ftz(u * v);
+    a = a * (r * v);
+    b = b * (r * u);
+}
+
+// A thread's row of a tile, two components of BNQ channels, out of its accumulators: affine,
+// activation, one rounding, stores of `store` bytes; `left` of the tile's channels exist.
+template <int BNQ, int ACT>
+__device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const float* scale,
+                                              const float* shift, bool affine,
+                                              __nv_bfloat16* row, int Nq, int left, int store) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        __nv_bfloat16* out = row + c * Nq;
+#pragma unroll
+        for (int g = 0; g < BNQ; g += 16) {
+            uint32_t v[8];
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                float z[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) z[k] = acc[c][g + j + k];
+                if (affine) {
+                    const float4 sc = *reinterpret_cast<const float4*>(scale + c * BNQ + g + j);
+                    const float4 sh = *reinterpret_cast<const float4*>(shift + c * BNQ + g + j);
+                    z[0] = fmaf(sc.x, z[0], sh.x);
+                    z[1] = fmaf(sc.y, z[1], sh.y);
+                    z[2] = fmaf(sc.z, z[2], sh.z);
+                    z[3] = fmaf(sc.w, z[3], sh.w);
+                }
+                if constexpr (ACT == 2) {
+                    f8_silu2(z[0], z[1]);
+                    f8_silu2(z[2], z[3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) z[k] = f8_act(z[k], ACT);
+                }
+                v[j / 2] = tc::pack_bf16x2(z[0], z[1]);
+                v[j / 2 + 1] = tc::pack_bf16x2(z[2], z[3]);
+            }
+            if (left >= g + 16 && store == 32) {
+                st_global_na_32(out + g, v);
+            } else if (left >= g + 16 && store == 16) {
+                st_global_na(out + g, make_uint4(v[0], v[1], v[2], v[3]));
+                st_global_na(out + g + 8, make_uint4(v[4], v[5], v[6], v[7]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (g + j < left)
+                        reinterpret_cast<unsigned short*>(out)[g + j] =
+                            static_cast<unsigned short>(v[j / 2] >> (16 * (j & 1)));
+            }
+        }
+    }
 }
 
 template <int BNQ>
@@ -124,14 +210,16 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
     uint8_t* smem = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t ring_a = smem_u32(smem), ring_b = ring_a + C::A_STAGES * C::A_STAGE;
-    float* vectors = reinterpret_cast<float*>(smem + C::RING);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::VEC);
+    float* vectors = reinterpret_cast<float*>(smem + C::RING + C::SCALES);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::SCALES + C::VEC);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t bar0 = smem_u32(bars);
-    const uint32_t full_a = bar0, empty_a = full_a + 8u * C::A_STAGES;
-    const uint32_t full_b = empty_a + 8u * C::A_STAGES, empty_b = full_b + 8u * C::B_STAGES;
-    const uint32_t accf = empty_b + 8u * C::B_STAGES, acce = accf + 16u, drain_bar = acce + 16u;
+    const uint32_t full_a = bar0, done_a = full_a + 8u * C::A_STAGES;
+    const uint32_t full_b = done_a + 8u * C::A_STAGES, empty_b = full_b + 8u * C::B_STAGES;
+    const uint32_t full_s = empty_b + 8u * C::B_STAGES, empty_s = full_s + 8u * C::S_STAGES;
+    const uint32_t acce = empty_s + 8u * C::S_STAGES, drain_bar = acce + 16u;
+    const uint32_t factors = ring_a + C::RING;  // [stage][ci][co][row]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint64_t limit = p.wait_limit_ns;
     auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) {
@@ -142,17 +230,20 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::A_STAGES; ++i) {
             mbar_init(full_a + 8u * i, 1);
-            mbar_init(empty_a + 8u * i, 1);
+            mbar_init(done_a + 8u * i, 1);
         }
         for (int i = 0; i < C::B_STAGES; ++i) {
             mbar_init(full_b + 8u * i, 1);
-            mbar_init(empty_b + 8u * i, 1);
+            mbar_init(empty_b + 8u * i, 2);
+        }
+        for (int i = 0; i < C::S_STAGES; ++i) {
+            mbar_init(full_s + 8u * i, 32);
+            mbar_init(empty_s + 8u * i, F8_EPI_WARPS);
         }
         for (int b = 0; b < 2; ++b) {
-            mbar_init(accf + 8u * b, 1);
             mbar_init(acce + 8u * b, F8_EPI_WARPS);
+            mbar_init(drain_bar + 8u * b, 1);
         }
-        mbar_init(drain_bar, 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -194,7 +285,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                                 kb * F8_BLOCK, nt * BNQ, 0, pol_w);
                     if (++sb == C::B_STAGES) sb = 0, phase_b ^= 1u;
                     for (int ci = 0; ci < 4; ++ci) {
-                        if (!wait(empty_a + 8u * sa, phase_a ^ 1u, STATUS_TIMEOUT_PRODUCER)) {
+                        if (!wait(done_a + 8u * sa, phase_a ^ 1u, STATUS_TIMEOUT_PRODUCER)) {
                             ok = false;
                             break;
                         }
@@ -212,9 +303,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                 tc::drain_fills(full_b, C::B_STAGES, filled_b, parity_b, limit);
             }
         }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------ MMA issuer
+    } else if (warp <= 2) {
+        // ------------------------------------------------------------ MMA issuers
         if (lane == 0) {
+            const int buf = warp - 1;  // this issuer's TMEM buffer, and its partials' parity
             bool ok = true;
             int issued = 0;
             if (p.inject_stall) {
@@ -222,8 +314,9 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                 wait(drain_bar, 0, STATUS_TIMEOUT_MMA);
                 ok = false;
             }
-            int sa = 0, sb = 0, it = 0;
-            uint32_t phase_a = 0, phase_b = 0;
+            const uint32_t d = tmem_base + static_cast<uint32_t>(buf * 4 * BNQ);
+            int sa = buf, sb = 0;
+            uint32_t phase_a = 0, phase_b = 0, use = 0;
             for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
                 for (int kb = 0; ok && kb < p.kblk; ++kb) {
                     const int left = p.Kq - kb * F8_BLOCK;  // channels of this block
@@ -233,38 +326,74 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                         break;
                     }
                     const uint32_t b_lo = tc::desc_lo(ring_b + sb * C::B_STAGE);
-                    for (int ci = 0; ci < 4; ++ci, ++it) {
-                        const int buf = it & 1;
-                        if (!wait(acce + 8u * buf, ((it >> 1) & 1) ^ 1, STATUS_TIMEOUT_MMA) ||
+                    for (int half = 0; half < 2; ++half) {  // components buf and buf + 2
+                        if (!wait(acce + 8u * buf, use ^ 1u, STATUS_TIMEOUT_MMA) ||
                             !wait(full_a + 8u * sa, phase_a, STATUS_TIMEOUT_MMA)) {
                             ok = false;
                             break;
                         }
+                        use ^= 1u;
                         tc_fence_after();
-                        const uint32_t d = tmem_base + static_cast<uint32_t>(buf * 4 * BNQ);
                         const uint32_t a_lo = tc::desc_lo(ring_a + sa * C::A_STAGE);
                         for (int kk = 0; kk < steps; ++kk)  // 32 channels: 32 bytes into a row
                             umma_f8(d, a_lo + 2 * kk, b_lo + 2 * kk, C::DESC_HI, C::IDESC,
                                     kk != 0 ? 1u : 0u);
                         ++issued;
-                        umma_commit(empty_a + 8u * sa);
-                        if (ci == 3) umma_commit(empty_b + 8u * sb);
-                        umma_commit(accf + 8u * buf);
-                        if (++sa == C::A_STAGES) sa = 0, phase_a ^= 1u;
+                        umma_commit(done_a + 8u * sa);
+                        if (half == 1) umma_commit(empty_b + 8u * sb);
+                        if ((sa += 2) >= C::A_STAGES) sa = buf, phase_a ^= 1u;
                     }
                     if (++sb == C::B_STAGES) sb = 0, phase_b ^= 1u;
                 }
             }
             if (!ok && issued > 0) {
                 // let the issued MMAs finish before TMEM is released
-                umma_commit(drain_bar);
+                umma_commit(drain_bar + 8u * buf);
                 const uint64_t t1 = global_timer_ns();
-                while (!mbar_try_wait(drain_bar, 0u)) {
+                while (!mbar_try_wait(drain_bar + 8u * buf, 0u)) {
                     if (global_timer_ns() - t1 > limit) {
                         atomicOr(&g_status, STATUS_TIMEOUT_DRAIN);
                         break;
                     }
                 }
+            }
+        }
+    } else if (warp == 3) {
+        // ------------------------------------------------------------ factors
+        // sgn(co, ci) s_x[ci][kb][row] s_w[co xor ci][kb], four rows a lane
+        griddep_wait();
+        bool ok = true;
+        uint32_t ss = 0, phase = 0;
+        for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
+            const int mt = t / p.ntiles, nt = t - mt * p.ntiles;
+            const float* xs = p.xs + static_cast<long long>(mt) * F8_BM + 4 * lane;
+            const float* ws = p.ws + static_cast<long long>(nt * BNQ / F8_BLOCK) * p.kblk;
+            for (int kb = 0; kb < p.kblk; ++kb, xs += p.pitch, ++ws) {
+                float4 x[4];
+                float w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    x[k] = __ldg(reinterpret_cast<const float4*>(xs + k * p.kblk * p.pitch));
+                    w[k] = __ldg(ws + static_cast<long long>(k) * p.nblk * p.kblk);
+                }
+                ok = __all_sync(0xffffffffu,
+                                wait(empty_s + 8u * ss, phase ^ 1u, STATUS_TIMEOUT_PRODUCER));
+                if (!ok) break;
+                const uint32_t dst = factors + ss * C::S_STAGE + 16u * lane;
+#pragma unroll
+                for (int ci = 0; ci < 4; ++ci)
+#pragma unroll
+                    for (int co = 0; co < 4; ++co) {
+                        const uint32_t flip = ((tc::NEG_MASK >> (4 * co + ci)) & 1u) ^
+                                              (co != ci ? static_cast<uint32_t>(p.conj) : 0u);
+                        const float f = negate_if(w[co ^ ci], flip);
+                        const float4 v = make_float4(f * x[ci].x, f * x[ci].y, f * x[ci].z,
+                                                     f * x[ci].w);
+                        sts_u4(dst + (4 * ci + co) * (F8_BM * 4),
+                               *reinterpret_cast<const uint4*>(&v));
+                    }
+                mbar_arrive(full_s + 8u * ss);
+                if (++ss == C::S_STAGES) ss = 0, phase ^= 1u;
             }
         }
     } else if (warp >= F8_EPI_WARP0) {
@@ -277,15 +406,9 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         float* scale = vectors + (warp - F8_EPI_WARP0) * 4 * BNQ;  // [2][BNQ]
         float* shift = scale + 2 * BNQ;
         const bool affine = p.ep.bias || p.ep.scale;
-        const long long xs_step = static_cast<long long>(p.kblk) * p.rows;  // to the next component
-        const long long ws_step = static_cast<long long>(p.nblk) * p.kblk;  // to the next letter
-        // bit 4 c + ci: sgn(co0 + c, ci), and conj(W)'s sign of letter co xor ci
-        uint32_t neg = (tc::NEG_MASK >> (4 * co0)) & 0xFFu;
-        if (p.conj) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if ((co0 + (i >> 2)) != (i & 3)) neg ^= 1u << i;
-        }
+        // factors of this lane's row for component co0; co0 + 1 is 512 bytes on, ci 2 KB a step
+        const uint32_t mine = factors + co0 * (F8_BM * 4) + 4u * (qd * 32 + lane);
+        uint32_t ss = 0, phase_s = 0;
         int it = 0;
         bool ok = true;
         for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
@@ -306,105 +429,59 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                 }
                 __syncwarp();
             }
-            const float* xs = p.xs + (in ? row : 0);
-            const float* ws = p.ws + static_cast<long long>(n0 / F8_BLOCK) * p.kblk;
             float acc[2][BNQ];
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int j = 0; j < BNQ; ++j) acc[c][j] = 0.0f;
-            // the first block's scales; each later block's are loaded a block ahead
-            float fx[4], fw[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fx[i] = in ? __ldg(xs + i * xs_step) : 0.0f;
-                fw[i] = __ldg(ws + (co0 ^ i) * ws_step);
-            }
-            for (int kb = 0; ok && kb < p.kblk; ++kb) {
-                // letter co0 xor i is that of component co0 with input i, and of component
-                // co0 + 1 with input i xor 1
-                float f[2][4];
-#pragma unroll
-                for (int ci = 0; ci < 4; ++ci) {
-                    f[0][ci] = (neg >> ci) & 1u ? -(fx[ci] * fw[ci]) : fx[ci] * fw[ci];
-                    f[1][ci] = (neg >> (4 + ci)) & 1u ? -(fx[ci] * fw[ci ^ 1])
-                                                      : fx[ci] * fw[ci ^ 1];
+            const int partials = 4 * p.kblk;
+#pragma unroll 1
+            for (int i = 0; i < partials; ++i, ++it) {
+                const int ci = i & 3, buf = it & 1;
+                bool got = true;
+                if (ci == 0) got = wait(full_s + 8u * ss, phase_s, STATUS_TIMEOUT_EPILOGUE);
+                got = got && wait(done_a + 8u * (it & (C::A_STAGES - 1)),
+                                  (it / C::A_STAGES) & 1, STATUS_TIMEOUT_EPILOGUE);
+                ok = __all_sync(0xffffffffu, got);
+                if (!ok) break;
+                const uint32_t fa = mine + ss * C::S_STAGE + ci * (4 * F8_BM * 4);
+                const float f[2] = {lds_f1(fa), lds_f1(fa + F8_BM * 4)};
+                if (ci == 3) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(empty_s + 8u * ss);
+                    if (++ss == C::S_STAGES) ss = 0, phase_s ^= 1u;
                 }
-                if (kb + 1 < p.kblk) {
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + (static_cast<uint32_t>(qd * 32) << 16) +
+                                       static_cast<uint32_t>(buf * 4 * BNQ);
+                const uint32_t t0 = taddr + (co0 ^ ci) * BNQ, t1 = taddr + (co0 ^ 1 ^ ci) * BNQ;
+                // chunk k: columns CH (k mod PER) and up of component co0 + k / PER
+                uint32_t v[2][CH];
+                f8_load<CH>(t0, v[0]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        fx[i] = in ? __ldg(xs + i * xs_step + (kb + 1) * p.rows) : 0.0f;
-                        fw[i] = __ldg(ws + (co0 ^ i) * ws_step + kb + 1);
+                for (int k = 0; k < 2 * PER; ++k) {
+                    tmem_ld_wait();
+                    if (k + 1 < 2 * PER) {
+                        f8_load<CH>((k + 1 < PER ? t0 : t1) + CH * ((k + 1) % PER),
+                                    v[(k + 1) & 1]);
+                    } else {
+                        // the partial is in registers: hand the buffer back to the issuer
+                        tc_fence_before();
+                        if (lane == 0) mbar_arrive_relaxed(acce + 8u * buf);
                     }
-                }
-#pragma unroll
-                for (int ci = 0; ci < 4; ++ci, ++it) {
-                    const int buf = it & 1;
-                    bool got = true;
-                    if (lane == 0)
-                        got = wait(accf + 8u * buf, (it >> 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-                    if (__shfl_sync(0xffffffffu, got ? 1 : 0, 0) == 0) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t taddr = tmem_base + (static_cast<uint32_t>(qd * 32) << 16) +
-                                           static_cast<uint32_t>(buf * 4 * BNQ);
-                    // chunk i: columns CH (i mod PER) and up of component co0 + i / PER
-                    uint32_t v[2][CH];
-                    f8_load<CH>(taddr + (co0 ^ ci) * BNQ, v[0]);
-#pragma unroll
-                    for (int i = 0; i < 2 * PER; ++i) {
-                        tmem_ld_wait();
-                        if (i + 1 < 2 * PER) {
-                            f8_load<CH>(taddr + ((co0 + (i + 1) / PER) ^ ci) * BNQ +
-                                            CH * ((i + 1) % PER), v[(i + 1) & 1]);
-                        } else {
-                            // the partial is in registers: hand the buffer back to the issuer
-                            tc_fence_before();
-                            if (lane == 0) mbar_arrive_relaxed(acce + 8u * buf);
-                        }
-                        f8_add<CH>(v[i & 1], f[i / PER][ci], &acc[i / PER][CH * (i % PER)]);
-                    }
+                    f8_add<CH>(v[k & 1], f[k / PER], &acc[k / PER][CH * (k % PER)]);
                 }
             }
             if (!ok) break;
             if (!in) continue;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                __nv_bfloat16* out = p.out + row * (4LL * p.Nq) + (co0 + c) * p.Nq + n0;
-#pragma unroll
-                for (int g = 0; g < BNQ; g += 16) {
-                    uint32_t v[8];
-#pragma unroll
-                    for (int j = 0; j < 16; j += 4) {
-                        float4 sc = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-                        float4 sh = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (affine) {
-                            sc = *reinterpret_cast<const float4*>(scale + c * BNQ + g + j);
-                            sh = *reinterpret_cast<const float4*>(shift + c * BNQ + g + j);
-                        }
-                        const float* a = &acc[c][g + j];
-                        v[j / 2] = tc::pack_bf16x2(f8_act(fmaf(sc.x, a[0], sh.x), p.act),
-                                                   f8_act(fmaf(sc.y, a[1], sh.y), p.act));
-                        v[j / 2 + 1] = tc::pack_bf16x2(f8_act(fmaf(sc.z, a[2], sh.z), p.act),
-                                                       f8_act(fmaf(sc.w, a[3], sh.w), p.act));
-                    }
-                    const int left = p.Nq - n0 - g;
-                    if (left >= 16 && p.store == 32) {
-                        st_global_na_32(out + g, v);
-                    } else if (left >= 16 && p.store == 16) {
-                        st_global_na(out + g, make_uint4(v[0], v[1], v[2], v[3]));
-                        st_global_na(out + g + 8, make_uint4(v[4], v[5], v[6], v[7]));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (j < left)
-                                reinterpret_cast<unsigned short*>(out)[g + j] =
-                                    static_cast<unsigned short>(v[j / 2] >> (16 * (j & 1)));
-                    }
-                }
-            }
+            __nv_bfloat16* out = p.out + row * (4LL * p.Nq) + co0 * p.Nq + n0;
+            const int left = p.Nq - n0;
+            if (p.act == 2)
+                f8_store_tile<BNQ, 2>(acc, scale, shift, affine, out, p.Nq, left, p.store);
+            else if (p.act == 1)
+                f8_store_tile<BNQ, 1>(acc, scale, shift, affine, out, p.Nq, left, p.store);
+            else
+                f8_store_tile<BNQ, 0>(acc, scale, shift, affine, out, p.Nq, left, p.store);
         }
     }
 
