@@ -76,7 +76,8 @@ def join_backward(dy, dn, y, h=None, post=None, gate=None, pre=None, alpha=1.0, 
         u = hn if post is None else hn * post
         if gate is not None:
             g = np.asarray(gate)
-            dgate = (s * u).reshape(g.reshape(-1, C).shape[0], -1, C).sum(axis=1).reshape(g.shape)
+            kept = u if factor is None else np.where(factor == 0.0, 0.0, u)
+            dgate = (s * kept).reshape(g.reshape(-1, C).shape[0], -1, C).sum(axis=1).reshape(g.shape)
         v = s * _gate_rows(gate, rows, C)
         if post is None:
             dh = v

@@ -33,18 +33,29 @@ __device__ __forceinline__ uint4 philox4x32_10(unsigned long long block, uint32_
     return make_uint4(c0, c1, c2, c3);
 }
 
-// Bit j is set when element j of block `block` is kept.
-__device__ __forceinline__ uint32_t dropout_keep8(const DropoutArgs& d, unsigned long long block) {
-    const uint4 r = philox4x32_10(block, d.key0, d.key1);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-    uint32_t keep = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        keep |= ((w[j] & 0xFFFFu) >= d.threshold ? 1u : 0u) << (2 * j);
-        keep |= ((w[j] >> 16) >= d.threshold ? 1u : 0u) << (2 * j + 1);
+// The draws of a block's eight elements: element j is kept when keep(j).  A draw is compared in
+// the upper half of a word, so the odd ones need no shift.
+struct Dropout8 {
+    uint32_t w[4];
+    __device__ __forceinline__ void draw(const DropoutArgs& d, unsigned long long block) {
+        const uint4 r = philox4x32_10(block, d.key0, d.key1);
+        w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;
     }
-    return keep;
-}
+    __device__ __forceinline__ bool keep(const DropoutArgs& d, int j) const {
+        return (j & 1 ? w[j >> 1] : w[j >> 1] << 16) >= d.bound;
+    }
+    // The eight elements from element s of this block on, `next` holding the block after it.
+    __device__ __forceinline__ void shift(const Dropout8& next, int s) {
+        const int n = s >> 1;
+        uint32_t a[8] = {w[0], w[1], w[2], w[3], next.w[0], next.w[1], next.w[2], next.w[3]};
+#pragma unroll
+        for (int k = 0; k < 6; ++k) a[k] = n & 2 ? a[k + 2] : a[k];
+#pragma unroll
+        for (int k = 0; k < 5; ++k) a[k] = n & 1 ? a[k + 1] : a[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = s & 1 ? (a[k] >> 16) | (a[k + 1] << 16) : a[k];
+    }
+};
 
 // The counter base of a call: the offset, and the device word when there is one.
 __device__ __forceinline__ unsigned long long dropout_base(const DropoutArgs& d) {

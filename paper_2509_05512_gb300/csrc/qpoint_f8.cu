@@ -242,47 +242,73 @@ struct F8Rows {
     float* scale;            // [4][kblk][pitch]
     long long rows, pitch;
     int Kq, Kp, kblk;
+    int group;  // rows side by side in a block of threads
 };
+//
+// A block of threads takes 16 of a row's blocks side by side (grid.y counts the sixteens), or as
+// many whole rows as fit in 16, and F8_ROWS_UNROLL such row groups, whose loads all go out first;
+// so a thread's component and block, the results of two divisions, hold for all of them.
 constexpr int F8_ROWS_UNROLL = 4;
+
 template <bool VEC>
 __global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
     griddep_launch_dependents();
     griddep_wait();
     const int hl = threadIdx.x & 15;
-    const unsigned per_row = 4u * p.kblk;
-    // a block's blocks of 128 follow one another in memory; all loads go out first
-    const long long u0 = static_cast<long long>(blockIdx.x) * (16 * F8_ROWS_UNROLL) +
-                         (threadIdx.x >> 4);
-    const long long first = u0 / per_row;
-    const unsigned rest0 = static_cast<unsigned>(u0 - first * per_row);
-    float v[F8_ROWS_UNROLL][8];
+    const unsigned per_row = 4u * p.kblk, unit = blockIdx.y * 16u + (threadIdx.x >> 4);
+    const unsigned r0 = unit / per_row, rest = unit - r0 * per_row;  // r0: 0 if per_row >= 16
+    const unsigned ci = rest / p.kblk, b = rest - ci * p.kblk;
+    const int k = static_cast<int>(b) * F8_BLOCK + hl * 8;
+    // units past the row groups' whole rows have nothing to do
+    const bool mine = r0 < static_cast<unsigned>(p.group);
+    const long long row0 = static_cast<long long>(blockIdx.x) * (p.group * F8_ROWS_UNROLL) + r0;
+    const __nv_bfloat16* x = p.x + row0 * (4LL * p.Kq) + static_cast<int>(ci) * p.Kq + k;
+    uint32_t w[F8_ROWS_UNROLL][4];  // eight bf16 channels
 #pragma unroll
     for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
-        const unsigned r = (rest0 + 16u * i) / per_row, rest = rest0 + 16u * i - r * per_row;
-        const long long row = first + r;
-        const unsigned ci = rest / p.kblk, b = rest - ci * p.kblk;
-        if (row < p.rows) {
-            load_x8<VEC>(p.x + row * (4LL * p.Kq) + static_cast<int>(ci) * p.Kq,
-                         static_cast<int>(b) * F8_BLOCK + hl * 8, p.Kq, v[i]);
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+        for (int j = 0; j < 4; ++j) w[i][j] = 0u;
+        if (mine && row0 + i * p.group < p.rows) {
+            const __nv_bfloat16* xi = x + static_cast<long long>(i * p.group) * (4LL * p.Kq);
+            if (VEC) {
+                if (k < p.Kq) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(xi);
+                    w[i][0] = v.x, w[i][1] = v.y, w[i][2] = v.z, w[i][3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (k + j < p.Kq)
+                        w[i][j / 2] |= static_cast<uint32_t>(
+                                           reinterpret_cast<const unsigned short*>(xi)[j])
+                                       << (16 * (j & 1));
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
-        const unsigned r = (rest0 + 16u * i) / per_row, rest = rest0 + 16u * i - r * per_row;
-        const long long row = first + r;
-        const unsigned ci = rest / p.kblk, b = rest - ci * p.kblk;
-        const int k = static_cast<int>(b) * F8_BLOCK + hl * 8;
+        // largest magnitude: the bits without the sign order as the numbers do, NaN above all
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __vmaxu2(m, w[i][j] & 0x7FFF7FFFu);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+        m = max(m << 16, m & 0xFFFF0000u);
+        const long long row = row0 + i * p.group;
+        if (!mine || row >= p.rows) continue;
         float inv;
-        const float s = half_warp_scale(v[i], inv);  // whole warps: every lane takes part
-        if (row >= p.rows) continue;
+        const float s = f8_scale(__uint_as_float(m), inv);
         if (hl == 0) p.scale[(static_cast<long long>(ci) * p.kblk + b) * p.pitch + row] = s;
+        uint32_t q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float lo, hi;
+            bf16x2_to_f32(w[i][j], lo, hi);
+            q[j] = f8x2_from_f32(lo * inv, hi * inv);
+        }
         if (k < p.Kp)
-            *reinterpret_cast<uint2*>(p.q + (row * 4 + ci) * p.Kp + k) = make_uint2(
-                f8x4_from_f32(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv),
-                f8x4_from_f32(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv));
+            *reinterpret_cast<uint2*>(p.q + (row * 4 + static_cast<int>(ci)) * p.Kp + k) =
+                make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
     }
 }
 
@@ -383,9 +409,11 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     auto* xq = static_cast<uint8_t*>(workspace);
     auto* xs = reinterpret_cast<float*>(xq + quantised_bytes(rows, Kq));
     const long long pitch = scale_pitch(rows);
-    const F8Rows r = {xb, xq, xs, rows, pitch, Kq, Kp, kblk};
-    const long long units = rows * 4 * kblk;
-    const dim3 g(static_cast<unsigned>((units + 16 * F8_ROWS_UNROLL - 1) / (16 * F8_ROWS_UNROLL)));
+    const int per_row = 4 * kblk, group = per_row < 16 ? 16 / per_row : 1;
+    const F8Rows r = {xb, xq, xs, rows, pitch, Kq, Kp, kblk, group};
+    const dim3 g(static_cast<unsigned>((rows + group * F8_ROWS_UNROLL - 1) /
+                                       (group * F8_ROWS_UNROLL)),
+                 static_cast<unsigned>((per_row + 15) / 16));
     cudaError_t e = vec ? launch_pdl(f8_rows_kernel<true>, g, dim3(256), 0, stream, r)
                         : launch_pdl(f8_rows_kernel<false>, g, dim3(256), 0, stream, r);
     if (e != cudaSuccess) return e;

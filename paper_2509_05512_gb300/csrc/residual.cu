@@ -32,35 +32,52 @@ namespace {
 
 // ------------------------------------------------------------------ dropout
 
-template <typename T, bool VEC>
+// UNROLL blocks of eight elements a thread, their loads first.
+template <typename T, bool VEC, int UNROLL>
 __global__ void __launch_bounds__(256) dropout_kernel(const T* x, long long n, DropoutArgs d,
                                                       T* out) {
     griddep_launch_dependents();
     griddep_wait();
     const unsigned long long base = dropout_base(d);
-    const long long groups = (n + 7) / 8, step = static_cast<long long>(gridDim.x) * blockDim.x;
-    for (long long g = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; g < groups;
-         g += step) {
-        const uint32_t keep = d.threshold ? dropout_keep8(d, base + g) : 0xFFu;
-        float v[8];
-        if (VEC && 8 * g + 8 <= n) {
-            Raw<T, 8> r;
-            r.load(x + 8 * g);
-            r.values(v);
+    const long long g0 = static_cast<long long>(blockIdx.x) * (256 * UNROLL) + threadIdx.x;
+    Raw<T, 8> r[UNROLL];
+    if (VEC) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * d.factor : 0.0f;
-            r.set(v);
-            r.store(out + 8 * g);
+        for (int i = 0; i < UNROLL; ++i)
+            if (8 * (g0 + 256 * i) + 8 <= n) r[i].load(x + 8 * (g0 + 256 * i));
+    }
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+        const long long g = g0 + 256 * i;
+        if (8 * g >= n) break;
+        Dropout8 m;
+        if (d.mode == 1) m.draw(d, base + g);
+        auto drop = [&](float v, int j) {
+            return d.mode == 0 || (d.mode == 1 && m.keep(d, j)) ? v * d.factor : 0.0f;
+        };
+        if (VEC && 8 * g + 8 <= n) {
+            float v[8];
+            r[i].values(v);
+            if (d.mode == 1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = m.keep(d, j) ? v[j] * d.factor : 0.0f;
+            } else if (d.mode == 2) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+            }
+            r[i].set(v);
+            r[i].store(out + 8 * g);
         } else {
-            const int left = static_cast<int>(n - 8 * g < 8 ? n - 8 * g : 8);
-            for (int j = 0; j < left; ++j) {
-                Raw<T, 1> r;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (8 * g + j >= n) break;
+                Raw<T, 1> e;
                 float w[1];
-                r.load(x + 8 * g + j);
-                r.values(w);
-                w[0] = (keep >> j) & 1u ? w[0] * d.factor : 0.0f;
-                r.set(w);
-                r.store(out + 8 * g + j);
+                e.load(x + 8 * g + j);
+                e.values(w);
+                w[0] = drop(w[0], j);
+                e.set(w);
+                e.store(out + 8 * g + j);
             }
         }
     }
@@ -185,14 +202,20 @@ __device__ __forceinline__ void load_columns(const float* v, const JoinParams& p
     }
 }
 
-// Bits of the eight elements from linear index i on.
-__device__ __forceinline__ uint32_t keep_from(const DropoutArgs& d, unsigned long long base,
-                                              long long i) {
-    const int s = static_cast<int>(i & 7);
-    const uint32_t lo = dropout_keep8(d, base + (static_cast<unsigned long long>(i) >> 3));
-    if (s == 0) return lo;
-    return (lo >> s) |
-           (dropout_keep8(d, base + (static_cast<unsigned long long>(i) >> 3) + 1) << (8 - s));
+// The draws of the eight elements from linear index i on.
+template <bool ALIGNED>
+__device__ __forceinline__ void draw_from(Dropout8& m, const DropoutArgs& d,
+                                          unsigned long long base, long long i) {
+    const unsigned long long block = base + (static_cast<unsigned long long>(i) >> 3);
+    m.draw(d, block);
+    if constexpr (!ALIGNED) {
+        const int s = static_cast<int>(i & 7);
+        if (s != 0) {
+            Dropout8 next;
+            next.draw(d, block + 1);
+            m.shift(next, s);
+        }
+    }
 }
 
 template <typename T, int LV, int NC, bool CROSS>
@@ -202,39 +225,59 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
     griddep_launch_dependents();
     griddep_wait();
     const Place q = place_of(p);
-    float post[NC][8], pre[NC][8], gate[NC][8];
-    load_columns<NC>(p.post, p, q, 1.0f, post);
+    // pg = alpha gate post / (1 - p): what a kept element of h / rms(h) is multiplied by
+    float pg[NC][8], pre[NC][8];
+    auto load_gate = [&](long long image) {
+        float post[NC][8];
+        load_columns<NC>(p.post, p, q, p.alpha * p.drop.factor, post);
+        load_columns<NC>(p.gate ? p.gate + image * p.C : nullptr, p, q, 1.0f, pg);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pg[c][j] *= post[c][j];
+    };
+    load_gate(0);
     load_columns<NC>(p.pre, p, q, 1.0f, pre);
-    load_columns<NC>(p.gate, p, q, p.alpha, gate);
-    const unsigned long long base = p.drop.threshold ? dropout_base(p.drop) : 0ull;
+    const unsigned long long base = p.drop.mode == 1 ? dropout_base(p.drop) : 0ull;
     const T *x = static_cast<const T*>(p.x), *h = static_cast<const T*>(p.h);
     T *y = static_cast<T*>(p.out_y), *n = static_cast<T*>(p.out_n);
-    long long image = 0;
     const long long step = static_cast<long long>(gridDim.x) * p.slots;
-    for (long long r0 = static_cast<long long>(blockIdx.x) * p.slots; r0 < p.rows; r0 += step) {
-        const long long row = r0 + q.slot;
-        const bool active = row < p.rows && q.slot < p.slots;
+    // a row's tensors are loaded one row ahead
+    Chunk<T, LV> nx[NC], nh[NC];
+    auto fetch = [&](long long row) {
         const long long at = row * p.C + q.seg * p.S;
-        Chunk<T, LV> cx[NC], ch[NC];
-        int left[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (q.ts + c * p.tps) * 8;
-            left[c] = active ? p.S - col : 0;
-            cx[c].load(x + at + col, left[c]);
-            if (h) ch[c].load(h + at + col, left[c]);
+            const int left = row < p.rows && q.slot < p.slots ? p.S - col : 0;
+            nx[c].load(x + at + col, left);
+            if (h) nh[c].load(h + at + col, left);
         }
-        float v[NC][8];
+    };
+    long long row = static_cast<long long>(blockIdx.x) * p.slots + q.slot;
+    long long image = 0, image_end = p.rows_per_image;
+    fetch(row);
+    for (long long r0 = static_cast<long long>(blockIdx.x) * p.slots; r0 < p.rows;
+         r0 += step, row += step) {
+        const bool active = row < p.rows && q.slot < p.slots;
+        const long long at = row * p.C + q.seg * p.S;
+        float v[NC][8], u[NC][8];
+        int left[NC];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) cx[c].values(v[c]);
+        for (int c = 0; c < NC; ++c) {
+            left[c] = active ? p.S - (q.ts + c * p.tps) * 8 : 0;
+            nx[c].values(v[c]);
+            if (h) nh[c].values(u[c]);
+        }
+        fetch(row + step);
+        Chunk<T, LV> o;
         if (h) {
-            if (active && p.gate && row / p.rows_per_image != image) {
+            if (p.gate && active && row >= image_end) {
                 image = row / p.rows_per_image;
-                load_columns<NC>(p.gate + image * p.C, p, q, p.alpha, gate);
+                image_end = (image + 1) * p.rows_per_image;
+                load_gate(image);
             }
-            float u[NC][8], r1 = 1.0f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) ch[c].values(u[c]);
+            float r1 = 1.0f;
             if (p.post) {
                 float ss[1] = {0.0f};
 #pragma unroll
@@ -247,14 +290,21 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (q.ts + c * p.tps) * 8;
-                const uint32_t keep =
-                    p.drop.threshold && left[c] > 0 ? keep_from(p.drop, base, at + col) : 0xFFu;
+                // (the product is selected, not a factor: an infinity that is dropped is 0)
+                if (p.drop.mode == 1) {
+                    Dropout8 m;
+                    draw_from<LV == 8>(m, p.drop, base, at + col);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = u[c][j] * r1 * post[c][j] * p.drop.factor;
-                    v[c][j] = fmaf(gate[c][j], (keep >> j) & 1u ? d : 0.0f, v[c][j]);
+                    for (int j = 0; j < 8; ++j) {
+                        const float d = u[c][j] * (r1 * pg[c][j]);
+                        v[c][j] += m.keep(p.drop, j) ? d : 0.0f;
+                    }
+                } else if (p.drop.mode == 0) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        v[c][j] = fmaf(u[c][j], r1 * pg[c][j], v[c][j]);
                 }
-                cx[c].set_store(v[c], y + at + col, left[c]);
+                o.set_store(v[c], y + at + col, left[c]);
             }
         }
         if (n) {
@@ -267,10 +317,9 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
             const float r2 = rsqrtf(fmaf(ss[0], p.inv_s, p.eps));
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const int col = (q.ts + c * p.tps) * 8;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] = v[c][j] * r2 * pre[c][j];
-                cx[c].set_store(v[c], n + at + col, left[c]);
+                for (int j = 0; j < 8; ++j) v[c][j] *= r2 * pre[c][j];
+                o.set_store(v[c], n + at + (q.ts + c * p.tps) * 8, left[c]);
             }
         }
     }
@@ -308,18 +357,21 @@ __device__ __forceinline__ void flush_columns(const JoinParams& p, const Place& 
 }
 
 template <typename T, int LV, int NC, bool CROSS>
-__global__ void __launch_bounds__(CROSS ? 512 : 256) join_bwd_kernel(const JoinParams p) {
+__global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_kernel(const JoinParams p) {
     __shared__ float sm[2][96];
     int turn = 0;
     extern __shared__ float cols[];
     griddep_launch_dependents();
     griddep_wait();
     const Place q = place_of(p);
-    float post[NC][8], pre[NC][8], gate[NC][8];
-    float a_post[NC][8] = {}, a_pre[NC][8] = {}, a_gate[NC][8] = {};
-    load_columns<NC>(p.post, p, q, 1.0f, post);
+    // With c = alpha / (1 - p), k the mask and e = sum over an image's rows of k dx h r1:
+    // dgate = c post e and dpost = sum over images of c gate e, so one sum serves both;
+    // w = k dx pg with pg = c gate post.
+    float pg[NC][8], pre[NC][8];
+    float e[NC][8] = {}, a_pre[NC][8] = {}, a_post[NC][8] = {};
+    const float factor = p.alpha * p.drop.factor;  // (0 when nothing is kept)
     load_columns<NC>(p.pre, p, q, 1.0f, pre);
-    const unsigned long long base = p.drop.threshold ? dropout_base(p.drop) : 0ull;
+    const unsigned long long base = p.drop.mode == 1 ? dropout_base(p.drop) : 0ull;
     const T *h = static_cast<const T*>(p.h), *y = static_cast<const T*>(p.y);
     const T *dy = static_cast<const T*>(p.dy), *dn = static_cast<const T*>(p.dn);
     T *dx = static_cast<T*>(p.out_y), *dh = static_cast<T*>(p.out_n);
@@ -328,105 +380,142 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_bwd_kernel(const JoinP
         const long long first = image * p.rows_per_image + k * p.chunk_rows;
         long long last = first + p.chunk_rows;
         if (last > (image + 1) * p.rows_per_image) last = (image + 1) * p.rows_per_image;
-        if (h) load_columns<NC>(p.gate ? p.gate + image * p.C : nullptr, p, q, 1.0f, gate);
-        for (long long r0 = first; r0 < last; r0 += p.slots) {
-            const long long row = r0 + q.slot;
-            const bool active = row < last && q.slot < p.slots;
+        const float* gate = p.gate ? p.gate + image * p.C : nullptr;
+        {
+            float post[NC][8];
+            load_columns<NC>(p.post, p, q, 1.0f, post);
+            load_columns<NC>(gate, p, q, factor, pg);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) pg[c][j] *= post[c][j];
+        }
+        // a row's tensors are loaded one row ahead, where the registers allow it (16 words of
+        // bf16; fp32 rows have twice the bytes under way as it is)
+        constexpr bool AHEAD = sizeof(T) == 2 && NC == 1;
+        Chunk<T, LV> cdy[NC], cdn[NC], cy[NC], ch[NC];
+        auto fetch = [&](long long row) {
             const long long at = row * p.C + q.seg * p.S;
-            Chunk<T, LV> cdy[NC], cdn[NC], cy[NC], ch[NC];
-            int left[NC];
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (q.ts + c * p.tps) * 8;
-                left[c] = active ? p.S - col : 0;
+                const int left = row < last && q.slot < p.slots ? p.S - col : 0;
                 if (dy)
-                    cdy[c].load(dy + at + col, left[c]);
+                    cdy[c].load(dy + at + col, left);
                 else
                     cdy[c].zero();
                 if (dn) {
-                    cdn[c].load(dn + at + col, left[c]);
-                    cy[c].load(y + at + col, left[c]);
+                    cdn[c].load(dn + at + col, left);
+                    cy[c].load(y + at + col, left);
                 }
-                if (h) ch[c].load(h + at + col, left[c]);
+                if (h) ch[c].load(h + at + col, left);
             }
-            float g[NC][8], hv[NC][8];
+        };
+        if (AHEAD) fetch(first + q.slot);
+        for (long long r0 = first; r0 < last; r0 += p.slots) {
+            const long long row = r0 + q.slot;
+            if (!AHEAD) fetch(row);
+            const bool active = row < last && q.slot < p.slots;
+            const long long at = row * p.C + q.seg * p.S;
+            float g[NC][8], yv[NC][8], nv[NC][8], hv[NC][8];
+            int left[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                left[c] = active ? p.S - (q.ts + c * p.tps) * 8 : 0;
+                cdy[c].values(g[c]);
+                if (dn) {
+                    cy[c].values(yv[c]);
+                    cdn[c].values(nv[c]);
+                }
+                if (h) ch[c].values(hv[c]);
+            }
+            if (AHEAD) fetch(row + p.slots);
             float s3[3] = {0.0f, 0.0f, 0.0f};  // sums of h^2, y^2 and t y
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                cdy[c].values(g[c]);
                 if (dn) {
-                    float yv[8], nv[8];
-                    cy[c].values(yv);
-                    cdn[c].values(nv);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        s3[1] = fmaf(yv[j], yv[j], s3[1]);
-                        s3[2] = fmaf(nv[j] * pre[c][j], yv[j], s3[2]);
+                        s3[1] = fmaf(yv[c][j], yv[c][j], s3[1]);
+                        s3[2] = fmaf(nv[c][j] * pre[c][j], yv[c][j], s3[2]);
                     }
                 }
                 if (h) {
-                    ch[c].values(hv[c]);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) s3[0] = fmaf(hv[c][j], hv[c][j], s3[0]);
                 }
             }
             group_sum<CROSS, 3>(s3, p.tps, sm, turn);
             const float r1 = p.post ? rsqrtf(fmaf(s3[0], p.inv_s, p.eps)) : 1.0f;
+            Chunk<T, LV> o;
             if (dn) {
                 const float r2 = rsqrtf(fmaf(s3[1], p.inv_s, p.eps));
                 const float m = s3[2] * p.inv_s * r2 * r2;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    const int col = (q.ts + c * p.tps) * 8;
-                    float yv[8], nv[8];
-                    cy[c].values(yv);
-                    cdn[c].values(nv);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        g[c][j] = fmaf(r2, fmaf(-m, yv[j], nv[j] * pre[c][j]), g[c][j]);
-                        a_pre[c][j] = fmaf(nv[j] * r2, yv[j], a_pre[c][j]);
+                        g[c][j] = fmaf(r2, fmaf(-m, yv[c][j], nv[c][j] * pre[c][j]), g[c][j]);
+                        a_pre[c][j] = fmaf(nv[c][j], yv[c][j] * r2, a_pre[c][j]);
                     }
-                    cy[c].set_store(g[c], dx + at + col, left[c]);
+                    o.set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
                 }
             } else if (dx) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
-                    cdy[c].set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
+                    o.set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
             }
             if (h) {
                 float w1[1] = {0.0f};
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    const int col = (q.ts + c * p.tps) * 8;
-                    const uint32_t keep = p.drop.threshold && left[c] > 0
-                                              ? keep_from(p.drop, base, at + col)
-                                              : 0xFFu;
-                    const float f = p.alpha * p.drop.factor;
+                    Dropout8 draws;
+                    if (p.drop.mode == 1)
+                        draw_from<LV == 8>(draws, p.drop, base, at + (q.ts + c * p.tps) * 8);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float s = (keep >> j) & 1u ? f * g[c][j] : 0.0f;
-                        const float hn = hv[c][j] * r1;
-                        a_gate[c][j] = fmaf(s, hn * post[c][j], a_gate[c][j]);
-                        const float v = s * gate[c][j];
-                        a_post[c][j] = fmaf(v, hn, a_post[c][j]);
-                        g[c][j] = v * post[c][j];  // w
+                        // (both factors: what is dropped has no part, be it infinite)
+                        float hn = hv[c][j] * r1;
+                        if (p.drop.mode == 2 || (p.drop.mode == 1 && !draws.keep(p.drop, j))) {
+                            g[c][j] = 0.0f;
+                            hn = 0.0f;
+                        }
+                        e[c][j] = fmaf(g[c][j], hn, e[c][j]);
+                        g[c][j] *= pg[c][j];  // w
                         w1[0] = fmaf(g[c][j], hv[c][j], w1[0]);
                     }
                 }
-                float m = 0.0f;
                 if (p.post) {
                     group_sum<CROSS, 1>(w1, p.tps, sm, turn);
-                    m = w1[0] * p.inv_s * r1 * r1;
+                    const float m = w1[0] * p.inv_s * r1 * r1;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            g[c][j] = r1 * fmaf(-m, hv[c][j], g[c][j]);
                 }
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g[c][j] = r1 * fmaf(-m, hv[c][j], g[c][j]);
-                    ch[c].set_store(g[c], dh + at + (q.ts + c * p.tps) * 8, left[c]);
-                }
+                for (int c = 0; c < NC; ++c)
+                    o.set_store(g[c], dh + at + (q.ts + c * p.tps) * 8, left[c]);
             }
         }
-        if (p.part_gate) flush_columns<NC>(p, q, a_gate, cols, p.part_gate + u * p.C);
+        if (p.part_post || p.part_gate) {
+            float v[NC][8];
+            load_columns<NC>(gate, p, q, factor, v);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a_post[c][j] = fmaf(v[c][j], e[c][j], a_post[c][j]);
+            load_columns<NC>(p.post, p, q, factor, v);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[c][j] *= e[c][j];
+                    e[c][j] = 0.0f;
+                }
+            if (p.part_gate) flush_columns<NC>(p, q, v, cols, p.part_gate + u * p.C);
+        }
     }
     const long long b = blockIdx.x * p.part_stride;
     if (p.part_post) flush_columns<NC>(p, q, a_post, cols, p.part_post + b);
@@ -579,10 +668,10 @@ int join_load_width(const JoinArgs& a) {
 DropoutArgs dropout_args(float p, unsigned long long seed, unsigned long long offset,
                          const unsigned long long* counter) {
     DropoutArgs d;
-    d.threshold = static_cast<uint32_t>(p * 65536.0 + 0.5);
-    d.factor = d.threshold < 65536u
-                   ? static_cast<float>(65536.0 / (65536.0 - static_cast<double>(d.threshold)))
-                   : 0.0f;
+    const uint32_t t = static_cast<uint32_t>(p * 65536.0 + 0.5);
+    d.mode = t == 0 ? 0 : (t < 65536u ? 1 : 2);
+    d.bound = t << 16;
+    d.factor = t < 65536u ? static_cast<float>(65536.0 / (65536.0 - static_cast<double>(t))) : 0.0f;
     d.key0 = static_cast<uint32_t>(seed);
     d.key1 = static_cast<uint32_t>(seed >> 32);
     d.offset = offset;
@@ -593,22 +682,22 @@ DropoutArgs dropout_args(float p, unsigned long long seed, unsigned long long of
 cudaError_t launch_dropout(const void* x, long long n, bool f32, const DropoutArgs& d, void* out,
                            int num_sms, cudaStream_t stream) {
     if (n == 0) return cudaSuccess;
-    const long long groups = (n + 7) / 8;
-    long long blocks = (groups + 255) / 256;
-    const long long cap = static_cast<long long>(num_sms) * 32;
-    if (blocks > cap) blocks = cap;
-    const dim3 g(static_cast<unsigned>(blocks)), b(256);
     const bool vec = (reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % 16 == 0;
-    if (f32) {
-        auto* i = static_cast<const float*>(x);
-        auto* o = static_cast<float*>(out);
-        return vec ? launch_pdl(dropout_kernel<float, true>, g, b, 0, stream, i, n, d, o)
-                   : launch_pdl(dropout_kernel<float, false>, g, b, 0, stream, i, n, d, o);
-    }
-    auto* i = static_cast<const __nv_bfloat16*>(x);
-    auto* o = static_cast<__nv_bfloat16*>(out);
-    return vec ? launch_pdl(dropout_kernel<__nv_bfloat16, true>, g, b, 0, stream, i, n, d, o)
-               : launch_pdl(dropout_kernel<__nv_bfloat16, false>, g, b, 0, stream, i, n, d, o);
+    const long long groups = (n + 7) / 8;
+    // four blocks of eight a thread once that still fills the SMs twice
+    const bool many = groups >= 4LL * 256 * 2 * 8 * num_sms;
+    const long long per = 256 * (many ? 4 : 1);
+    const dim3 g(static_cast<unsigned>((groups + per - 1) / per)), b(256);
+#define QUAN_DROPOUT(T, VEC, U)                                                          \
+    launch_pdl(dropout_kernel<T, VEC, U>, g, b, 0, stream, static_cast<const T*>(x), n, d, \
+               static_cast<T*>(out))
+    if (f32)
+        return vec ? (many ? QUAN_DROPOUT(float, true, 4) : QUAN_DROPOUT(float, true, 1))
+                   : (many ? QUAN_DROPOUT(float, false, 4) : QUAN_DROPOUT(float, false, 1));
+    return vec ? (many ? QUAN_DROPOUT(__nv_bfloat16, true, 4) : QUAN_DROPOUT(__nv_bfloat16, true, 1))
+               : (many ? QUAN_DROPOUT(__nv_bfloat16, false, 4)
+                       : QUAN_DROPOUT(__nv_bfloat16, false, 1));
+#undef QUAN_DROPOUT
 }
 
 bool join_supported(int C, int groups) {

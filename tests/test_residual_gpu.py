@@ -258,6 +258,12 @@ def test_join_special_rows():
     y, n = quan.residual_join(x, h, pre=one, p=0.5, seed=3)
     assert not y[[0, 1, 3]].any() and not n[[0, 1, 3]].any()
     assert int(torch.isnan(y).sum()) == 1 and bool(torch.isnan(n[2]).all())
+    # and has no part in a gradient
+    g = torch.randn(4, C, device="cuda")
+    dx, dh, _, dgate, _ = quan.residual_join_backward(g, None, None, h[:2].repeat(2, 1),
+                                                      gate=one, p=0.5, seed=3)
+    keep = torch.from_numpy(f > 0).cuda()
+    assert not dh[~keep].any() and bool(torch.isfinite(dh).all())
     # everything dropped: the branch has no part, and no gradient
     h = torch.randn(4, C, device="cuda")
     x = torch.randn(4, C, device="cuda")
