@@ -201,8 +201,9 @@ cudaError_t launch_qconv_stem_pool_rgb(const ConvShape& s, const float* rgb,
 // Dropout (philox.cuh): the mask of one call.
 struct DropoutArgs {
     uint32_t bound;  // an element is kept when its 16 bits, as the upper half of a word, are >= it
-    int mode;        // 0: all are kept, 1: by the bound, 2: none is
-    float factor;    // 1 / (1 - p); 0 in mode 2
+    int draws;       // 0: no bits are drawn, every element has zeros (all are kept with bound 0,
+                     // none with bound 2^16)
+    float factor;    // 1 / (1 - p); 0 for p = 1
     uint32_t key0, key1;
     unsigned long long offset;
     const unsigned long long* counter;  // device word added to offset, or null

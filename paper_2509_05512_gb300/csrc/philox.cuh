@@ -37,6 +37,7 @@ __device__ __forceinline__ uint4 philox4x32_10(unsigned long long block, uint32_
 // the upper half of a word, so the odd ones need no shift.
 struct Dropout8 {
     uint32_t w[4];
+    __device__ __forceinline__ void none() { w[0] = w[1] = w[2] = w[3] = 0u; }
     __device__ __forceinline__ void draw(const DropoutArgs& d, unsigned long long block) {
         const uint4 r = philox4x32_10(block, d.key0, d.key1);
         w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;

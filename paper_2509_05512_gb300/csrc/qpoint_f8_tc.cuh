@@ -68,14 +68,16 @@ template <int BNQ>
 struct F8Cfg {
     static constexpr int A_STAGE = F8_BM * F8_BLOCK;    // one component of 128 rows: 16 KB
     static constexpr int B_STAGE = 4 * BNQ * F8_BLOCK;  // four letters
-    static constexpr int A_STAGES = 8, B_STAGES = 2;
+    static constexpr int A_STAGES = 4, B_STAGES = 2;  // a K block of rows, two of letters
     static constexpr int RING = A_STAGES * A_STAGE + B_STAGES * B_STAGE;
     static constexpr int VEC = F8_EPI_WARPS * 2 * 2 * BNQ * 4;  // each epilogue warp's vectors
+    static constexpr int OUT_PITCH = 2 * BNQ + 16;  // staged output row: no bank twice in a quarter
+    static constexpr int OUT = F8_EPI_WARPS * 32 * OUT_PITCH;
     static constexpr int S_STAGES = 2, S_STAGE = 4 * 4 * F8_BM * 4;  // factors of a K block: 8 KB
     static constexpr int SCALES = S_STAGES * S_STAGE;
     // full and done (A), full and empty (B, factors), acce (2 buffers), drain (2 issuers)
     static constexpr int NUM_BARS = 2 * (A_STAGES + B_STAGES + S_STAGES) + 2 + 2;
-    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + VEC + NUM_BARS * 8 + 16;
+    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + VEC + OUT + NUM_BARS * 8 + 16;
     static constexpr uint32_t DESC_HI = tc::desc_hi(8 * 128, tc::desc_layout(128));
     static constexpr uint32_t TMEM_COLS = 2 * 4 * BNQ;  // 512, 256 or 128
     // kind::f8f6f4: e4m3 A and B (format 0), fp32 D, both K-major
@@ -104,16 +106,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, uint3
         ".L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy)
         : "memory");
-}
-
-// 32 bytes of one row in one store: a full sector, where two 16-byte stores would reach L2 as
-// two halves of it.
-__device__ __forceinline__ void st_global_na_32(void* p, const uint32_t (&v)[8]) {
-    asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
-                     p),
-                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
-                 "r"(v[7])
-                 : "memory");
 }
 
 __device__ __forceinline__ float lds_f1(uint32_t addr) {
@@ -150,15 +142,31 @@ __device__ __forceinline__ void f8_silu2(float& a, float& b) {
     b = b * (r * u);
 }
 
-// A thread's row of a tile, two components of BNQ channels, out of its accumulators: affine,
-// activation, one rounding, stores of `store` bytes; `left` of the tile's channels exist.
+// 32 bytes of one row in one store: a whole sector.
+__device__ __forceinline__ void st_global_na_32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
+                     p),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
+                 "r"(v[7])
+                 : "memory");
+}
+
+// A warp's 32 rows of a tile, two components of BNQ channels, out of its threads' accumulators (a
+// row a thread): affine, activation, one rounding.  Whole sectors are stored by the thread that
+// has them (110 us for 102,400 rows 512 -> 1024, 118 by way of shared memory); rows that do not
+// start at one are staged in shared memory and stored along the rows (7473 rows 520 -> 328, 2-byte
+// stores: 49 us when each thread stores its own row, 20 staged).
 template <int BNQ, int ACT>
 __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const float* scale,
-                                              const float* shift, bool affine,
-                                              __nv_bfloat16* row, int Nq, int left, int store) {
+                                              const float* shift, bool affine, uint32_t stage,
+                                              __nv_bfloat16* out, const F8TcParams& p,
+                                              int rows, int left) {
+    using C = F8Cfg<BNQ>;
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        __nv_bfloat16* out = row + c * Nq;
+        __nv_bfloat16* o = out + c * p.Nq;
+        __syncwarp();  // the other component's reads
 #pragma unroll
         for (int g = 0; g < BNQ; g += 16) {
             uint32_t v[8];
@@ -185,17 +193,35 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                 v[j / 2] = tc::pack_bf16x2(z[0], z[1]);
                 v[j / 2 + 1] = tc::pack_bf16x2(z[2], z[3]);
             }
-            if (left >= g + 16 && store == 32) {
-                st_global_na_32(out + g, v);
-            } else if (left >= g + 16 && store == 16) {
-                st_global_na(out + g, make_uint4(v[0], v[1], v[2], v[3]));
-                st_global_na(out + g + 8, make_uint4(v[4], v[5], v[6], v[7]));
+            if (p.store == 32) {
+                if (lane < rows && g < left) st_global_na_32(o + lane * (4LL * p.Nq) + g, v);
             } else {
+                const uint32_t at = stage + lane * C::OUT_PITCH + 2 * g;
+                sts_u4(at, make_uint4(v[0], v[1], v[2], v[3]));
+                sts_u4(at + 16, make_uint4(v[4], v[5], v[6], v[7]));
+            }
+        }
+        __syncwarp();
+        if (p.store == 16) {
+            constexpr int PER_ROW = BNQ / 8;  // 16-byte units
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (g + j < left)
-                        reinterpret_cast<unsigned short*>(out)[g + j] =
-                            static_cast<unsigned short>(v[j / 2] >> (16 * (j & 1)));
+            for (int i = 0; i < PER_ROW; ++i) {
+                const int r = i * (32 / PER_ROW) + lane / PER_ROW, u = lane % PER_ROW;
+                if (r < rows && 8 * u < left)
+                    st_global_na(o + r * (4LL * p.Nq) + 8 * u,
+                                 lds_u4(stage + r * C::OUT_PITCH + 16 * u));
+            }
+        } else if (p.store == 2) {
+            for (int i = lane; i < 32 * BNQ; i += 32) {
+                const int r = i / BNQ, n = i % BNQ;
+                if (r < rows && n < left) {
+                    uint16_t h;
+                    asm volatile("ld.shared.u16 %0, [%1];"
+                                 : "=h"(h)
+                                 : "r"(stage + r * C::OUT_PITCH + 2 * n)
+                                 : "memory");
+                    reinterpret_cast<uint16_t*>(o)[r * (4LL * p.Nq) + n] = h;
+                }
             }
         }
     }
@@ -211,7 +237,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t ring_a = smem_u32(smem), ring_b = ring_a + C::A_STAGES * C::A_STAGE;
     float* vectors = reinterpret_cast<float*>(smem + C::RING + C::SCALES);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::SCALES + C::VEC);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::SCALES + C::VEC + C::OUT);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t bar0 = smem_u32(bars);
@@ -405,6 +431,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         const int co0 = 2 * ((warp - F8_EPI_WARP0) / 4), qd = warp & 3;
         float* scale = vectors + (warp - F8_EPI_WARP0) * 4 * BNQ;  // [2][BNQ]
         float* shift = scale + 2 * BNQ;
+        const uint32_t stage = smem_u32(smem + C::RING + C::SCALES + C::VEC) +
+                               (warp - F8_EPI_WARP0) * 32 * C::OUT_PITCH;
         const bool affine = p.ep.bias || p.ep.scale;
         // factors of this lane's row for component co0; co0 + 1 is 512 bytes on, ci 2 KB a step
         const uint32_t mine = factors + co0 * (F8_BM * 4) + 4u * (qd * 32 + lane);
@@ -413,8 +441,6 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         bool ok = true;
         for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
             const int mt = t / p.ntiles, nt = t - mt * p.ntiles;
-            const long long row = static_cast<long long>(mt) * F8_BM + qd * 32 + lane;
-            const bool in = row < p.rows;
             const int n0 = nt * BNQ;
             if (affine) {
                 __syncwarp();  // the previous tile's reads
@@ -473,15 +499,18 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                 }
             }
             if (!ok) break;
-            if (!in) continue;
-            __nv_bfloat16* out = p.out + row * (4LL * p.Nq) + co0 * p.Nq + n0;
+            const long long row0 = static_cast<long long>(mt) * F8_BM + qd * 32;
+            const int rows = row0 < p.rows
+                                 ? static_cast<int>(p.rows - row0 < 32 ? p.rows - row0 : 32)
+                                 : 0;
+            __nv_bfloat16* out = p.out + row0 * (4LL * p.Nq) + co0 * p.Nq + n0;
             const int left = p.Nq - n0;
             if (p.act == 2)
-                f8_store_tile<BNQ, 2>(acc, scale, shift, affine, out, p.Nq, left, p.store);
+                f8_store_tile<BNQ, 2>(acc, scale, shift, affine, stage, out, p, rows, left);
             else if (p.act == 1)
-                f8_store_tile<BNQ, 1>(acc, scale, shift, affine, out, p.Nq, left, p.store);
+                f8_store_tile<BNQ, 1>(acc, scale, shift, affine, stage, out, p, rows, left);
             else
-                f8_store_tile<BNQ, 0>(acc, scale, shift, affine, out, p.Nq, left, p.store);
+                f8_store_tile<BNQ, 0>(acc, scale, shift, affine, stage, out, p, rows, left);
         }
     }
 

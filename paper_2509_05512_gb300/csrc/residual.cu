@@ -51,20 +51,13 @@ __global__ void __launch_bounds__(256) dropout_kernel(const T* x, long long n, D
         const long long g = g0 + 256 * i;
         if (8 * g >= n) break;
         Dropout8 m;
-        if (d.mode == 1) m.draw(d, base + g);
-        auto drop = [&](float v, int j) {
-            return d.mode == 0 || (d.mode == 1 && m.keep(d, j)) ? v * d.factor : 0.0f;
-        };
+        m.none();
+        if (d.draws) m.draw(d, base + g);
         if (VEC && 8 * g + 8 <= n) {
             float v[8];
             r[i].values(v);
-            if (d.mode == 1) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = m.keep(d, j) ? v[j] * d.factor : 0.0f;
-            } else if (d.mode == 2) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-            }
+            for (int j = 0; j < 8; ++j) v[j] = m.keep(d, j) ? v[j] * d.factor : 0.0f;
             r[i].set(v);
             r[i].store(out + 8 * g);
         } else {
@@ -75,7 +68,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(const T* x, long long n, D
                 float w[1];
                 e.load(x + 8 * g + j);
                 e.values(w);
-                w[0] = drop(w[0], j);
+                w[0] = m.keep(d, j) ? w[0] * d.factor : 0.0f;
                 e.set(w);
                 e.store(out + 8 * g + j);
             }
@@ -161,7 +154,9 @@ template <bool CROSS, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], int tps, float (&both)[2][96],
                                           int& turn) {
     if constexpr (!CROSS) {
-        for (int o = tps >> 1; o > 0; o >>= 1) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            if (o >= tps) continue;
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
         }
@@ -238,7 +233,7 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
     };
     load_gate(0);
     load_columns<NC>(p.pre, p, q, 1.0f, pre);
-    const unsigned long long base = p.drop.mode == 1 ? dropout_base(p.drop) : 0ull;
+    const unsigned long long base = p.drop.draws ? dropout_base(p.drop) : 0ull;
     const T *x = static_cast<const T*>(p.x), *h = static_cast<const T*>(p.h);
     T *y = static_cast<T*>(p.out_y), *n = static_cast<T*>(p.out_n);
     const long long step = static_cast<long long>(gridDim.x) * p.slots;
@@ -291,18 +286,13 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
             for (int c = 0; c < NC; ++c) {
                 const int col = (q.ts + c * p.tps) * 8;
                 // (the product is selected, not a factor: an infinity that is dropped is 0)
-                if (p.drop.mode == 1) {
-                    Dropout8 m;
-                    draw_from<LV == 8>(m, p.drop, base, at + col);
+                Dropout8 m;
+                m.none();
+                if (p.drop.draws) draw_from<LV == 8>(m, p.drop, base, at + col);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float d = u[c][j] * (r1 * pg[c][j]);
-                        v[c][j] += m.keep(p.drop, j) ? d : 0.0f;
-                    }
-                } else if (p.drop.mode == 0) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        v[c][j] = fmaf(u[c][j], r1 * pg[c][j], v[c][j]);
+                for (int j = 0; j < 8; ++j) {
+                    const float d = u[c][j] * (r1 * pg[c][j]);
+                    v[c][j] += m.keep(p.drop, j) ? d : 0.0f;
                 }
                 o.set_store(v[c], y + at + col, left[c]);
             }
@@ -371,7 +361,7 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
     float e[NC][8] = {}, a_pre[NC][8] = {}, a_post[NC][8] = {};
     const float factor = p.alpha * p.drop.factor;  // (0 when nothing is kept)
     load_columns<NC>(p.pre, p, q, 1.0f, pre);
-    const unsigned long long base = p.drop.mode == 1 ? dropout_base(p.drop) : 0ull;
+    const unsigned long long base = p.drop.draws ? dropout_base(p.drop) : 0ull;
     const T *h = static_cast<const T*>(p.h), *y = static_cast<const T*>(p.y);
     const T *dy = static_cast<const T*>(p.dy), *dn = static_cast<const T*>(p.dn);
     T *dx = static_cast<T*>(p.out_y), *dh = static_cast<T*>(p.out_n);
@@ -450,13 +440,14 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
             Chunk<T, LV> o;
             if (dn) {
                 const float r2 = rsqrtf(fmaf(s3[1], p.inv_s, p.eps));
-                const float m = s3[2] * p.inv_s * r2 * r2;
+                const float m = -s3[2] * p.inv_s * r2 * r2 * r2;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        g[c][j] = fmaf(r2, fmaf(-m, yv[c][j], nv[c][j] * pre[c][j]), g[c][j]);
-                        a_pre[c][j] = fmaf(nv[c][j], yv[c][j] * r2, a_pre[c][j]);
+                        const float rn = r2 * nv[c][j];
+                        g[c][j] = fmaf(rn, pre[c][j], fmaf(m, yv[c][j], g[c][j]));
+                        a_pre[c][j] = fmaf(rn, yv[c][j], a_pre[c][j]);
                     }
                     o.set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
                 }
@@ -469,30 +460,28 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
                 float w1[1] = {0.0f};
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    Dropout8 draws;
-                    if (p.drop.mode == 1)
-                        draw_from<LV == 8>(draws, p.drop, base, at + (q.ts + c * p.tps) * 8);
+                    Dropout8 m;
+                    m.none();
+                    if (p.drop.draws)
+                        draw_from<LV == 8>(m, p.drop, base, at + (q.ts + c * p.tps) * 8);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        // (both factors: what is dropped has no part, be it infinite)
-                        float hn = hv[c][j] * r1;
-                        if (p.drop.mode == 2 || (p.drop.mode == 1 && !draws.keep(p.drop, j))) {
-                            g[c][j] = 0.0f;
-                            hn = 0.0f;
-                        }
-                        e[c][j] = fmaf(g[c][j], hn, e[c][j]);
-                        g[c][j] *= pg[c][j];  // w
-                        w1[0] = fmaf(g[c][j], hv[c][j], w1[0]);
+                        // (both factors are selected: what is dropped has no part, be it infinite)
+                        const bool keep = m.keep(p.drop, j);
+                        const float gk = keep ? g[c][j] : 0.0f, hk = keep ? hv[c][j] : 0.0f;
+                        e[c][j] = fmaf(gk * r1, hk, e[c][j]);
+                        g[c][j] = gk * pg[c][j];  // w
+                        w1[0] = fmaf(g[c][j], hk, w1[0]);
                     }
                 }
                 if (p.post) {
                     group_sum<CROSS, 1>(w1, p.tps, sm, turn);
-                    const float m = w1[0] * p.inv_s * r1 * r1;
+                    const float m = -w1[0] * p.inv_s * r1 * r1 * r1;
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
-                            g[c][j] = r1 * fmaf(-m, hv[c][j], g[c][j]);
+                            g[c][j] = fmaf(m, hv[c][j], r1 * g[c][j]);
                 }
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
@@ -523,16 +512,16 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
 }
 
 // out[v][c] = sum over k < count of part[v stride_v + k stride_k + c], for the vectors v of
-// blockIdx.y; 32 channels a block, eight threads a channel, joined in a fixed order.
+// blockIdx.y; 32 channels a block, 32 threads a channel, joined in a fixed order.
 struct ColumnSum {
     const float* part;
     float* out;
     long long stride_v, stride_k;
     int count;
 };
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
     join_columns_kernel(ColumnSum a, ColumnSum b, ColumnSum c, int C) {
-    __shared__ float sm[8][32];
+    __shared__ float sm[32][33];
     griddep_launch_dependents();
     griddep_wait();
     const long long v = blockIdx.y;
@@ -545,16 +534,16 @@ __global__ void __launch_bounds__(256)
     if (col < C) {
         const float* src = s.part + w * s.stride_v + col;
 #pragma unroll 8
-        for (int k = part; k < s.count; k += 8) acc += src[k * s.stride_k];
+        for (int k = part; k < s.count; k += 32) acc += src[k * s.stride_k];
     }
     sm[part][lane] = acc;
     __syncthreads();
-    if (part == 0 && col < C) {
-        float t = 0.0f;
+    // warp `part` adds the 32 parts of channel `part` of the block
+    float t = sm[lane][part];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += sm[k][lane];
-        s.out[w * C + col] = t;
-    }
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    const int mine = blockIdx.x * 32 + part;
+    if (lane == 0 && mine < C) s.out[w * C + mine] = t;
 }
 
 constexpr int JOIN_MAX_THREADS = 512;
@@ -669,8 +658,8 @@ DropoutArgs dropout_args(float p, unsigned long long seed, unsigned long long of
                          const unsigned long long* counter) {
     DropoutArgs d;
     const uint32_t t = static_cast<uint32_t>(p * 65536.0 + 0.5);
-    d.mode = t == 0 ? 0 : (t < 65536u ? 1 : 2);
-    d.bound = t << 16;
+    d.draws = t > 0 && t < 65536u;
+    d.bound = t < 65536u ? t << 16 : 1u << 16;
     d.factor = t < 65536u ? static_cast<float>(65536.0 / (65536.0 - static_cast<double>(t))) : 0.0f;
     d.key0 = static_cast<uint32_t>(seed);
     d.key1 = static_cast<uint32_t>(seed >> 32);
@@ -771,7 +760,7 @@ cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, f
     const ColumnSum gate = {gate_part, dgate, pl.chunks * C, C, pl.chunks};
     const dim3 g(static_cast<unsigned>((a.C + 31) / 32),
                  static_cast<unsigned>(2 + (sum_g ? a.images : 0)));
-    return launch_pdl(join_columns_kernel, g, dim3(256), 0, stream, post, pre, gate, a.C);
+    return launch_pdl(join_columns_kernel, g, dim3(1024), 0, stream, post, pre, gate, a.C);
 }
 
 }  // namespace quan
