@@ -597,7 +597,7 @@ def quan_residual_join_bwd(dy, dn, y, h, post, gate, pre, rows, C, groups, image
 def _empty(stream, shape, dtype, device):
     """An empty tensor whose memory belongs to `stream` (None: the current one), so that the
     allocator hands it on only after that stream's work."""
-    import torch
+    torch = _torch or _get_torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     s = stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream)
@@ -606,25 +606,34 @@ def _empty(stream, shape, dtype, device):
 
 
 def _check_tensor(name, t, shape, dtype):
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or \
-            not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous CUDA tensor %s of %s (got %s of %s)" % (
             name, list(shape), dtype, list(t.shape), t.dtype))
 
 
+_torch = None
+
+
+def _get_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _dtype_of(name, t):
-    import torch
-    if t.dtype == torch.bfloat16:
+    torch = _torch or _get_torch()
+    if t.dtype is torch.bfloat16:
         return QUAN_DTYPE_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return QUAN_DTYPE_F32
     raise ValueError("%s must be bfloat16 or float32 (got %s)" % (name, t.dtype))
 
 
 def _check_counter(counter):
-    import torch
     if counter is not None:
-        _check_tensor("counter", counter.reshape(-1), (1,), torch.int64)
+        _check_tensor("counter", counter.reshape(-1), (1,), _get_torch().int64)
 
 
 def dropout(x, p, seed, offset=0, *, counter=None, out=None, stream=None):
@@ -704,13 +713,14 @@ def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
 
 def _qpoint_f8(x, w, K, N, workspace, out, stream):
     """rows, workspace and output of one 8-bit product of K input and N output channels."""
-    import torch
-    _check_tensor("x", x, x.shape[:-1] + (K,), torch.bfloat16)
+    torch = _torch or _get_torch()
+    lead = x.shape[:-1]
+    _check_tensor("x", x, lead + (K,), torch.bfloat16)
     rows = x.numel() // K
     if out is None:
-        out = _empty(stream, x.shape[:-1] + (N,), torch.bfloat16, x.device)
+        out = _empty(stream, lead + (N,), torch.bfloat16, x.device)
     else:
-        _check_tensor("out", out, x.shape[:-1] + (N,), torch.bfloat16)
+        _check_tensor("out", out, lead + (N,), torch.bfloat16)
     need = quan_qpoint_f8_workspace_size(rows, K, N)
     if workspace is None and need:
         workspace = _empty(stream, (need,), torch.uint8, x.device)
@@ -723,12 +733,11 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
     """Pointwise quaternion convolution in 8-bit floating point: bf16 x [..., Cin] (CUDA), which
     is quantised in the call, and w = quantize_f8_weights(...) -> bf16 [..., Cout],
     act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d."""
-    import torch
     if w.transposed:
         raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
     for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
         if v is not None:
-            _check_tensor(name, v, (w.Cout,), torch.float32)
+            _check_tensor(name, v, (w.Cout,), _get_torch().float32)
     rows, workspace, nbytes, out = _qpoint_f8(x, w, w.Cin, w.Cout, workspace, out, stream)
     quan_qpoint_f8_fwd(x, w.q, w.scale, bias, scale, shift, rows, w.Cin, w.Cout, act, workspace,
                        nbytes, out, stream)
@@ -747,15 +756,20 @@ def qpointwise_f8_backward_data(dy, w, *, workspace=None, out=None, stream=None)
 
 def _join_shape(like, post, gate, pre):
     """(rows, C, images) of a join's tensors, its vectors checked."""
-    import torch
-    C = like.shape[-1]
+    f32 = (_torch or _get_torch()).float32
+    shape = like.shape
+    C = shape[-1]
     images = 1
     if gate is not None:
-        images = 1 if gate.dim() == 1 else like.shape[0]
-        _check_tensor("gate", gate, (C,) if gate.dim() == 1 else (images, C), torch.float32)
-    for name, v in (("post", post), ("pre", pre)):
-        if v is not None:
-            _check_tensor(name, v, (C,), torch.float32)
+        if gate.dim() == 1:
+            _check_tensor("gate", gate, (C,), f32)
+        else:
+            images = shape[0]
+            _check_tensor("gate", gate, (images, C), f32)
+    if post is not None:
+        _check_tensor("post", post, (C,), f32)
+    if pre is not None:
+        _check_tensor("pre", pre, (C,), f32)
     return like.numel() // C if C else 0, C, max(images, 1)
 
 
@@ -773,13 +787,14 @@ def residual_join(x, h=None, *, post=None, gate=None, pre=None, alpha=1.0, group
     _check_counter(counter)
     if h is not None:
         _check_tensor("h", h, x.shape, x.dtype)
-        if y is None:
-            y = _empty(stream, x.shape, x.dtype, x.device)
-    if pre is not None and n is None:
+    if y is not None:
+        _check_tensor("y", y, x.shape, x.dtype)
+    elif h is not None:
+        y = _empty(stream, x.shape, x.dtype, x.device)
+    if n is not None:
+        _check_tensor("n", n, x.shape, x.dtype)
+    elif pre is not None:
         n = _empty(stream, x.shape, x.dtype, x.device)
-    for name, t in (("y", y), ("n", n)):
-        if t is not None:
-            _check_tensor(name, t, x.shape, x.dtype)
     quan_residual_join_fwd(x, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p,
                            seed, offset, counter, y, n, stream)
     return y, n
