@@ -49,6 +49,36 @@ __device__ __forceinline__ float half_warp_scale(const float (&v)[8], float& inv
     return f8_scale(__uint_as_float(m), inv);
 }
 
+// Eight consecutive bf16 channels as words, LV channels a load (their address aligned to that);
+// `left` of them exist, a multiple of LV where LV > 1, the others are 0.
+template <int LV>
+__device__ __forceinline__ void load_words8(const __nv_bfloat16* p, int left, uint32_t (&w)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = 0u;
+    if constexpr (LV == 8) {
+        if (left > 0) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        }
+    } else if constexpr (LV == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (2 * j < left) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left)
+                w[j / 2] |=
+                    static_cast<uint32_t>(reinterpret_cast<const unsigned short*>(p)[j])
+                    << (16 * (j & 1));
+    }
+}
+
+// Channels a load may take of rows of n channels, all tensors or'ed into `address`.
+int load_channels(int n, uintptr_t address) {
+    return n % 8 == 0 && address % 16 == 0 ? 8 : (n % 2 == 0 && address % 4 == 0 ? 2 : 1);
+}
+
 // ------------------------------------------------------------------ letters
 
 struct F8Letters {
@@ -59,47 +89,73 @@ struct F8Letters {
     int Kp, nblk, kblk;
 };
 
-// One 128 x 128 block of one letter: its scale, then its 8-bit values, by way of shared memory so
-// that the transposed form too is read and written along its rows.
-template <bool TRANSPOSE>
+// One 128 x 128 block of one letter: its scale, then its 8-bit values, which the transposed form
+// turns in shared memory so that it too is written along its rows.  A thread has eight channels of
+// eight rows, all loaded before the first is looked at: a block is one trip to memory (LV channels
+// a load).
+template <bool TRANSPOSE, int LV>
 __global__ void __launch_bounds__(256) f8_letters_kernel(const F8Letters p) {
-    __shared__ __nv_bfloat16 tile[128][130];  // 130: both directions miss no bank twice
+    __shared__ uint8_t tile[128 * 129];  // 129: neither direction meets a bank twice
     __shared__ uint32_t top[8];
     griddep_launch_dependents();
     griddep_wait();
     const int letter = blockIdx.z, r0 = blockIdx.y * 128, c0 = blockIdx.x * 128;
-    const __nv_bfloat16* w = p.w[letter];
-    uint32_t m = 0;
-    for (int i = threadIdx.x; i < 128 * 128; i += 256) {
-        const int r = i >> 7, c = i & 127;
-        const bool in = r0 + r < p.rows && c0 + c < p.cols;
-        const __nv_bfloat16 v =
-            in ? w[static_cast<long long>(r0 + r) * p.cols + c0 + c] : __float2bfloat16_rn(0.0f);
-        tile[r][c] = v;
-        m = max(m, abs_bits(__bfloat162float(v)));
+    const int tr = threadIdx.x >> 4, tc = (threadIdx.x & 15) * 8;  // rows tr + 16 i
+    const __nv_bfloat16* w = p.w[letter] + c0 + tc;
+    uint32_t v[8][4], m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + tr + 16 * i;
+        load_words8<LV>(w + static_cast<long long>(r) * p.cols, r < p.rows ? p.cols - c0 - tc : 0,
+                        v[i]);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __vmaxu2(m, v[i][j] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
     if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m = max(m, top[k]);
+    for (int k = 0; k < 8; ++k) m = __vmaxu2(m, top[k]);
     float inv;
-    const float s = f8_scale(__uint_as_float(m), inv);
+    const float s = f8_scale(__uint_as_float(max(m << 16, m & 0xFFFF0000u)), inv);
     const int nb = TRANSPOSE ? blockIdx.x : blockIdx.y, kb = TRANSPOSE ? blockIdx.y : blockIdx.x;
     if (threadIdx.x == 0)
         p.scale[(static_cast<long long>(letter) * p.nblk + nb) * p.kblk + kb] = s;
     const int N = TRANSPOSE ? p.cols : p.rows;
-    uint8_t* q = p.q + static_cast<long long>(letter) * N * p.Kp;
-    for (int i = threadIdx.x; i < 128 * 32; i += 256) {
-        const int n = i >> 5, k = (i & 31) * 4;
-        if (nb * 128 + n >= N || kb * 128 + k >= p.Kp) continue;
-        float v[4];
+    uint8_t* q = p.q + static_cast<long long>(letter) * N * p.Kp + kb * 128;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = __bfloat162float(TRANSPOSE ? tile[k + j][n] : tile[n][k + j]) * inv;
-        *reinterpret_cast<uint32_t*>(q + static_cast<long long>(nb * 128 + n) * p.Kp + kb * 128 +
-                                     k) = f8x4_from_f32(v[0], v[1], v[2], v[3]);
+    for (int i = 0; i < 8; ++i) {
+        uint32_t h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float lo, hi;
+            bf16x2_to_f32(v[i][j], lo, hi);
+            h[j] = f8x2_from_f32(lo * inv, hi * inv);
+        }
+        const int r = tr + 16 * i;
+        if constexpr (TRANSPOSE) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                tile[r * 129 + tc + j] = static_cast<uint8_t>(h[j >> 1] >> (8 * (j & 1)));
+        } else if (r0 + r < N && kb * 128 + tc < p.Kp) {
+            *reinterpret_cast<uint2*>(q + static_cast<long long>(r0 + r) * p.Kp + tc) =
+                make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+        }
+    }
+    if constexpr (TRANSPOSE) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < 128 * 32; i += 256) {
+            const int n = i >> 5, k = (i & 31) * 4;
+            if (c0 + n >= N || kb * 128 + k >= p.Kp) continue;
+            uint32_t h = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                h |= static_cast<uint32_t>(tile[(k + j) * 129 + n]) << (8 * j);
+            *reinterpret_cast<uint32_t*>(q + static_cast<long long>(c0 + n) * p.Kp + k) = h;
+        }
     }
 }
 
@@ -234,8 +290,9 @@ cudaError_t launch_rows(const F8Params& p, bool vec, cudaStream_t stream) {
 
 // ------------------------------------------------------------------ rows in 8 bits
 
-// A half-warp a block of 128 channels, 16 bytes a lane: the block's scale, then its 8-bit values.
-// Bound by HBM: 2 bytes read, 1 written a channel.
+// GL lanes a block of 128 channels, eight channels a lane: the block's scale, then its 8-bit
+// values.  GL = 16, or 8 or 4 where a component has no more than 64 or 32 channels.  Bound by HBM:
+// 2 bytes read, 1 written a channel.
 struct F8Rows {
     const __nv_bfloat16* x;  // [rows][4 Kq]
     uint8_t* q;              // [rows][4][Kp]
@@ -245,18 +302,18 @@ struct F8Rows {
     int group;  // rows side by side in a block of threads
 };
 //
-// A block of threads takes 16 of a row's blocks side by side (grid.y counts the sixteens), or as
-// many whole rows as fit in 16, and F8_ROWS_UNROLL such row groups, whose loads all go out first;
-// so a thread's component and block, the results of two divisions, hold for all of them.
+// A block of threads takes 256 / GL of a row's blocks side by side (grid.y counts these), or as
+// many whole rows as fit, and F8_ROWS_UNROLL such row groups, whose loads all go out first; so a
+// thread's component and block, the results of two divisions, hold for all of them.
 constexpr int F8_ROWS_UNROLL = 4;
 
-template <bool VEC>
+template <int GL, int LV>
 __global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
     griddep_launch_dependents();
     griddep_wait();
-    const int hl = threadIdx.x & 15;
-    const unsigned per_row = 4u * p.kblk, unit = blockIdx.y * 16u + (threadIdx.x >> 4);
-    const unsigned r0 = unit / per_row, rest = unit - r0 * per_row;  // r0: 0 if per_row >= 16
+    const int hl = threadIdx.x & (GL - 1);
+    const unsigned per_row = 4u * p.kblk, unit = blockIdx.y * (256u / GL) + threadIdx.x / GL;
+    const unsigned r0 = unit / per_row, rest = unit - r0 * per_row;
     const unsigned ci = rest / p.kblk, b = rest - ci * p.kblk;
     const int k = static_cast<int>(b) * F8_BLOCK + hl * 8;
     // units past the row groups' whole rows have nothing to do
@@ -265,26 +322,9 @@ __global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
     const __nv_bfloat16* x = p.x + row0 * (4LL * p.Kq) + static_cast<int>(ci) * p.Kq + k;
     uint32_t w[F8_ROWS_UNROLL][4];  // eight bf16 channels
 #pragma unroll
-    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[i][j] = 0u;
-        if (mine && row0 + i * p.group < p.rows) {
-            const __nv_bfloat16* xi = x + static_cast<long long>(i * p.group) * (4LL * p.Kq);
-            if (VEC) {
-                if (k < p.Kq) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(xi);
-                    w[i][0] = v.x, w[i][1] = v.y, w[i][2] = v.z, w[i][3] = v.w;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (k + j < p.Kq)
-                        w[i][j / 2] |= static_cast<uint32_t>(
-                                           reinterpret_cast<const unsigned short*>(xi)[j])
-                                       << (16 * (j & 1));
-            }
-        }
-    }
+    for (int i = 0; i < F8_ROWS_UNROLL; ++i)
+        load_words8<LV>(x + static_cast<long long>(i * p.group) * (4LL * p.Kq),
+                        mine && row0 + i * p.group < p.rows ? p.Kq - k : 0, w[i]);
 #pragma unroll
     for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
         // largest magnitude: the bits without the sign order as the numbers do, NaN above all
@@ -292,7 +332,7 @@ __global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) m = __vmaxu2(m, w[i][j] & 0x7FFF7FFFu);
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+        for (int o = GL / 2; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
         m = max(m << 16, m & 0xFFFF0000u);
         const long long row = row0 + i * p.group;
         if (!mine || row >= p.rows) continue;
@@ -309,6 +349,20 @@ __global__ void __launch_bounds__(256) f8_rows_kernel(const F8Rows p) {
         if (k < p.Kp)
             *reinterpret_cast<uint2*>(p.q + (row * 4 + static_cast<int>(ci)) * p.Kp + k) =
                 make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
+    }
+}
+
+template <int GL>
+cudaError_t launch_f8_rows(F8Rows r, cudaStream_t stream) {
+    const int per_row = 4 * r.kblk, units = 256 / GL;
+    r.group = per_row < units ? units / per_row : 1;
+    const dim3 g(static_cast<unsigned>((r.rows + r.group * F8_ROWS_UNROLL - 1) /
+                                       (r.group * F8_ROWS_UNROLL)),
+                 static_cast<unsigned>((per_row + units - 1) / units));
+    switch (load_channels(r.Kq, reinterpret_cast<uintptr_t>(r.x))) {
+        case 8: return launch_pdl(f8_rows_kernel<GL, 8>, g, dim3(256), 0, stream, r);
+        case 2: return launch_pdl(f8_rows_kernel<GL, 2>, g, dim3(256), 0, stream, r);
+        default: return launch_pdl(f8_rows_kernel<GL, 1>, g, dim3(256), 0, stream, r);
     }
 }
 
@@ -333,8 +387,17 @@ cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool tr
     p.kblk = blocks_of(transpose ? Qout : Qin);
     const dim3 g(static_cast<unsigned>(blocks_of(Qin)), static_cast<unsigned>(blocks_of(Qout)),
                  4);
-    return transpose ? launch_pdl(f8_letters_kernel<true>, g, dim3(256), 0, stream, p)
-                     : launch_pdl(f8_letters_kernel<false>, g, dim3(256), 0, stream, p);
+    uintptr_t at = 0;
+    for (int L = 0; L < 4; ++L) at |= reinterpret_cast<uintptr_t>(w[L]);
+#define QUAN_LETTERS(LV)                                                                   \
+    (transpose ? launch_pdl(f8_letters_kernel<true, LV>, g, dim3(256), 0, stream, p)       \
+               : launch_pdl(f8_letters_kernel<false, LV>, g, dim3(256), 0, stream, p))
+    switch (load_channels(Qin, at)) {
+        case 8: return QUAN_LETTERS(8);
+        case 2: return QUAN_LETTERS(2);
+        default: return QUAN_LETTERS(1);
+    }
+#undef QUAN_LETTERS
 }
 
 namespace {
@@ -409,13 +472,10 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     auto* xq = static_cast<uint8_t*>(workspace);
     auto* xs = reinterpret_cast<float*>(xq + quantised_bytes(rows, Kq));
     const long long pitch = scale_pitch(rows);
-    const int per_row = 4 * kblk, group = per_row < 16 ? 16 / per_row : 1;
-    const F8Rows r = {xb, xq, xs, rows, pitch, Kq, Kp, kblk, group};
-    const dim3 g(static_cast<unsigned>((rows + group * F8_ROWS_UNROLL - 1) /
-                                       (group * F8_ROWS_UNROLL)),
-                 static_cast<unsigned>((per_row + 15) / 16));
-    cudaError_t e = vec ? launch_pdl(f8_rows_kernel<true>, g, dim3(256), 0, stream, r)
-                        : launch_pdl(f8_rows_kernel<false>, g, dim3(256), 0, stream, r);
+    const F8Rows r = {xb, xq, xs, rows, pitch, Kq, Kp, kblk, 0};
+    const cudaError_t e = Kq <= 32   ? launch_f8_rows<4>(r, stream)
+                          : Kq <= 64 ? launch_f8_rows<8>(r, stream)
+                                     : launch_f8_rows<16>(r, stream);
     if (e != cudaSuccess) return e;
 
     const int bnq = f8_tile_width(rows, Kq, Nq, num_sms);
@@ -449,7 +509,10 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     p.ntiles = (Nq + bnq - 1) / bnq;
     p.num_tiles = static_cast<int>((rows + F8_BM - 1) / F8_BM * p.ntiles);
     const uintptr_t a = reinterpret_cast<uintptr_t>(out);
-    p.store = Nq % 16 == 0 && a % 32 == 0 ? 32 : (Nq % 8 == 0 && a % 16 == 0 ? 16 : 2);
+    p.store = Nq % 16 == 0 && a % 32 == 0  ? F8_STORE_SECTOR
+              : Nq % 8 == 0 && a % 16 == 0 ? F8_STORE_16
+              : Nq % 2 == 0 && a % 4 == 0  ? F8_STORE_4
+                                           : F8_STORE_2;
     p.wait_limit_ns = wait_limit_ns;
     p.inject_stall = inject_stall;
     switch (bnq) {

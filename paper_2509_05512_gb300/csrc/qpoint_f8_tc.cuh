@@ -59,7 +59,7 @@ struct F8TcParams {
     int Kq, Nq, kblk, nblk;
     int conj, act;
     int ntiles, num_tiles;
-    int store;  // bytes of a store: 32, 16 or 2 (by Nq and the output's alignment)
+    int store;  // how the output leaves (f8_store_tile), by Nq and its alignment
     unsigned long long wait_limit_ns;
     int inject_stall;
 };
@@ -77,7 +77,7 @@ struct F8Cfg {
     static constexpr int SCALES = S_STAGES * S_STAGE;
     // full and done (A), full and empty (B, factors), acce (2 buffers), drain (2 issuers)
     static constexpr int NUM_BARS = 2 * (A_STAGES + B_STAGES + S_STAGES) + 2 + 2;
-    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + VEC + OUT + NUM_BARS * 8 + 16;
+    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + OUT + VEC + NUM_BARS * 8 + 16;
     static constexpr uint32_t DESC_HI = tc::desc_hi(8 * 128, tc::desc_layout(128));
     static constexpr uint32_t TMEM_COLS = 2 * 4 * BNQ;  // 512, 256 or 128
     // kind::f8f6f4: e4m3 A and B (format 0), fp32 D, both K-major
@@ -151,21 +151,58 @@ __device__ __forceinline__ void st_global_na_32(void* p, const uint32_t (&v)[8])
                  : "memory");
 }
 
-// A warp's 32 rows of a tile, two components of BNQ channels, out of its threads' accumulators (a
-// row a thread): affine, activation, one rounding.  Whole sectors are stored by the thread that
-// has them (110 us for 102,400 rows 512 -> 1024, 118 by way of shared memory); rows that do not
-// start at one are staged in shared memory and stored along the rows (7473 rows 520 -> 328, 2-byte
-// stores: 49 us when each thread stores its own row, 20 staged).
+// How a tile's output leaves, in order of preference:
+enum : int {
+    F8_STORE_SECTOR = 0,  // Nq a multiple of 16, 32-byte aligned: each thread its row's sectors
+    F8_STORE_16 = 1,      // Nq a multiple of 8, 16-byte aligned: staged, 16 bytes along the rows
+    F8_STORE_4 = 2,       // Nq even, 4-byte aligned: staged, 4 bytes along the rows
+    F8_STORE_2 = 3        // else: staged, 2 bytes
+};
+
+// Staged rows along the rows, U channels a store; T has U channels.
+template <int BNQ, typename T, int U>
+__device__ __forceinline__ void f8_copy_rows(uint32_t stage, __nv_bfloat16* o, int Nq, int rows,
+                                             int left) {
+    constexpr int PER_ROW = BNQ / U;
+    const int lane = threadIdx.x & 31;
+#pragma unroll 4
+    for (int i = lane; i < 32 * PER_ROW; i += 32) {
+        const int r = i / PER_ROW, n = U * (i % PER_ROW);
+        if (r < rows && n < left) {
+            T h;
+            if constexpr (sizeof(T) == 2)
+                asm volatile("ld.shared.u16 %0, [%1];"
+                             : "=h"(h)
+                             : "r"(stage + r * F8Cfg<BNQ>::OUT_PITCH + 2 * n)
+                             : "memory");
+            else
+                asm volatile("ld.shared.u32 %0, [%1];"
+                             : "=r"(h)
+                             : "r"(stage + r * F8Cfg<BNQ>::OUT_PITCH + 2 * n)
+                             : "memory");
+            *reinterpret_cast<T*>(o + r * (4LL * Nq) + n) = h;
+        }
+    }
+}
+
+// A warp's 32 rows of a tile, components co0 and co0 + 1 of BNQ channels, out of its threads'
+// accumulators (a row a thread): affine, activation, one rounding, and out.  Whole sectors are
+// stored by the thread that has them (102,400 rows 512 -> 1024: 113 us; 118 staged in shared
+// memory, 117 staged and copied by TMA); rows that do not start at one are staged and stored along
+// the rows (7473 rows 520 -> 328: 49 us when each thread stores its own row, staged 17).
 template <int BNQ, int ACT>
 __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const float* scale,
                                               const float* shift, bool affine, uint32_t stage,
-                                              __nv_bfloat16* out, const F8TcParams& p,
-                                              int rows, int left) {
+                                              const F8TcParams& p, long long row0, int co0,
+                                              int n0) {
     using C = F8Cfg<BNQ>;
     const int lane = threadIdx.x & 31;
+    const int rows =
+        row0 < p.rows ? static_cast<int>(p.rows - row0 < 32 ? p.rows - row0 : 32) : 0;
+    const int left = p.Nq - n0;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        __nv_bfloat16* o = out + c * p.Nq;
+        __nv_bfloat16* o = p.out + row0 * (4LL * p.Nq) + (co0 + c) * p.Nq + n0;
         __syncwarp();  // the other component's reads
 #pragma unroll
         for (int g = 0; g < BNQ; g += 16) {
@@ -193,7 +230,7 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                 v[j / 2] = tc::pack_bf16x2(z[0], z[1]);
                 v[j / 2 + 1] = tc::pack_bf16x2(z[2], z[3]);
             }
-            if (p.store == 32) {
+            if (p.store == F8_STORE_SECTOR) {
                 if (lane < rows && g < left) st_global_na_32(o + lane * (4LL * p.Nq) + g, v);
             } else {
                 const uint32_t at = stage + lane * C::OUT_PITCH + 2 * g;
@@ -202,7 +239,7 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
             }
         }
         __syncwarp();
-        if (p.store == 16) {
+        if (p.store == F8_STORE_16) {
             constexpr int PER_ROW = BNQ / 8;  // 16-byte units
 #pragma unroll
             for (int i = 0; i < PER_ROW; ++i) {
@@ -211,18 +248,10 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                     st_global_na(o + r * (4LL * p.Nq) + 8 * u,
                                  lds_u4(stage + r * C::OUT_PITCH + 16 * u));
             }
-        } else if (p.store == 2) {
-            for (int i = lane; i < 32 * BNQ; i += 32) {
-                const int r = i / BNQ, n = i % BNQ;
-                if (r < rows && n < left) {
-                    uint16_t h;
-                    asm volatile("ld.shared.u16 %0, [%1];"
-                                 : "=h"(h)
-                                 : "r"(stage + r * C::OUT_PITCH + 2 * n)
-                                 : "memory");
-                    reinterpret_cast<uint16_t*>(o)[r * (4LL * p.Nq) + n] = h;
-                }
-            }
+        } else if (p.store == F8_STORE_4) {
+            f8_copy_rows<BNQ, uint32_t, 2>(stage, o, p.Nq, rows, left);
+        } else if (p.store == F8_STORE_2) {
+            f8_copy_rows<BNQ, uint16_t, 1>(stage, o, p.Nq, rows, left);
         }
     }
 }
@@ -236,7 +265,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
     uint8_t* smem = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t ring_a = smem_u32(smem), ring_b = ring_a + C::A_STAGES * C::A_STAGE;
-    float* vectors = reinterpret_cast<float*>(smem + C::RING + C::SCALES);
+    float* vectors = reinterpret_cast<float*>(smem + C::RING + C::SCALES + C::OUT);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::SCALES + C::VEC + C::OUT);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -431,7 +460,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         const int co0 = 2 * ((warp - F8_EPI_WARP0) / 4), qd = warp & 3;
         float* scale = vectors + (warp - F8_EPI_WARP0) * 4 * BNQ;  // [2][BNQ]
         float* shift = scale + 2 * BNQ;
-        const uint32_t stage = smem_u32(smem + C::RING + C::SCALES + C::VEC) +
+        const uint32_t stage = smem_u32(smem + C::RING + C::SCALES) +
                                (warp - F8_EPI_WARP0) * 32 * C::OUT_PITCH;
         const bool affine = p.ep.bias || p.ep.scale;
         // factors of this lane's row for component co0; co0 + 1 is 512 bytes on, ci 2 KB a step
@@ -500,17 +529,12 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
             }
             if (!ok) break;
             const long long row0 = static_cast<long long>(mt) * F8_BM + qd * 32;
-            const int rows = row0 < p.rows
-                                 ? static_cast<int>(p.rows - row0 < 32 ? p.rows - row0 : 32)
-                                 : 0;
-            __nv_bfloat16* out = p.out + row0 * (4LL * p.Nq) + co0 * p.Nq + n0;
-            const int left = p.Nq - n0;
             if (p.act == 2)
-                f8_store_tile<BNQ, 2>(acc, scale, shift, affine, stage, out, p, rows, left);
+                f8_store_tile<BNQ, 2>(acc, scale, shift, affine, stage, p, row0, co0, n0);
             else if (p.act == 1)
-                f8_store_tile<BNQ, 1>(acc, scale, shift, affine, stage, out, p, rows, left);
+                f8_store_tile<BNQ, 1>(acc, scale, shift, affine, stage, p, row0, co0, n0);
             else
-                f8_store_tile<BNQ, 0>(acc, scale, shift, affine, stage, out, p, rows, left);
+                f8_store_tile<BNQ, 0>(acc, scale, shift, affine, stage, p, row0, co0, n0);
         }
     }
 

@@ -111,7 +111,8 @@ def test_letters(Cin, Cout, transpose):
 SHAPES = [(1, 4, 4), (1, 512, 1024), (2, 64, 512), (3, 520, 36), (5, 1024, 1024), (8, 2048, 128),
           (17, 100, 340), (49, 2048, 512), (127, 512, 256), (128, 512, 256), (129, 512, 260),
           (1000, 328, 520), (777, 1028, 516), (300, 4, 2048), (640, 64, 64), (2500, 128, 1280),
-          (20001, 256, 64)]
+          (20001, 256, 64), (20003, 1100, 64), (25000, 300, 20), (21000, 1028, 128),
+          (20100, 516, 1032), (6000, 12, 28), (3000, 140, 44), (9000, 520, 264)]
 
 
 @pytest.mark.parametrize("rows, Cin, Cout", SHAPES)
