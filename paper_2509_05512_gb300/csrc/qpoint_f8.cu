@@ -225,19 +225,31 @@ __global__ void __launch_bounds__(256) qpoint_rows_kernel(const F8Params p) {
         }
         __syncthreads();
         if (n >= p.Nq) continue;
-        for (int b = 0; b < ROWS_K / F8_BLOCK && k0 + b * F8_BLOCK < p.Kq; ++b) {
+        // the four blocks' letters and scales first, then the products
+        uint32_t q[ROWS_K / F8_BLOCK][4];
+        float sw[ROWS_K / F8_BLOCK][4];
+#pragma unroll
+        for (int b = 0; b < ROWS_K / F8_BLOCK; ++b) {
             const int kb = k0 / F8_BLOCK + b, k = kb * F8_BLOCK + lane * 4;
+#pragma unroll
+            for (int L = 0; L < 4; ++L) {
+                q[b][L] = k < p.Kp ? __ldg(reinterpret_cast<const uint32_t*>(
+                                         p.wq + (static_cast<long long>(L) * p.Nq + n) * p.Kp + k))
+                                   : 0u;
+                sw[b][L] = kb < p.kblk
+                               ? __ldg(p.ws + (static_cast<long long>(L) * p.nblk + n / F8_BLOCK) *
+                                                  p.kblk + kb)
+                               : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < ROWS_K / F8_BLOCK; ++b) {
+            if (k0 + b * F8_BLOCK >= p.Kq) break;
             float w[4][4];
 #pragma unroll
             for (int L = 0; L < 4; ++L) {
-                const uint32_t q =
-                    k < p.Kp ? __ldg(reinterpret_cast<const uint32_t*>(
-                                   p.wq + (static_cast<long long>(L) * p.Nq + n) * p.Kp + k))
-                             : 0u;
-                float s = __ldg(p.ws + (static_cast<long long>(L) * p.nblk + n / F8_BLOCK) *
-                                           p.kblk + kb);
-                if (p.conj && L > 0) s = -s;
-                f8x4_to_f32(q, w[L]);
+                const float s = p.conj && L > 0 ? -sw[b][L] : sw[b][L];
+                f8x4_to_f32(q[b][L], w[L]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[L][j] *= s;
             }
@@ -402,8 +414,13 @@ cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool tr
 
 namespace {
 
-// Rows up to which the CUDA-core kernel runs.
-constexpr int F8_FEW_ROWS = 4;
+// The CUDA-core kernel: one row always, a few rows while their products are few.  Measured (us,
+// CUDA cores and tensor cores with their quantisation): 1 row 512 -> 1024 2.1 and 5.2, 1 row
+// 4096 -> 4096 5.6 and 17; 4 rows 4096 -> 4096 14.4 and 16.5, 8 rows 18.2 and 16.9; 8 rows
+// 2048 -> 2048 8.3 and 10.4, 16 rows 11.0 and 10.3; 16 rows 512 -> 1024 5.5 and 5.7.
+bool f8_few_rows(long long rows, int Kq, int Nq) {
+    return rows == 1 || (rows <= 16 && rows * Kq * Nq <= (1 << 22));
+}
 
 size_t quantised_bytes(long long rows, int Kq) {
     return (static_cast<size_t>(rows) * 4 * f8_pitch(Kq) + 255) / 256 * 256;
@@ -413,12 +430,17 @@ size_t quantised_bytes(long long rows, int Kq) {
 // rows is never used).
 long long scale_pitch(long long rows) { return (rows + F8_BM - 1) / F8_BM * F8_BM; }
 
-// Quaternion output channels of a tile, by the estimated clocks of the waves of tiles.
+// Quaternion output channels of a tile, by the estimated time of the waves of tiles (1280 rows
+// 4096 -> 1024: 23.4, 18.8 and 25.3 us with 64, 32 and 16; 128 rows: 20.4, 15.9, 13.5; 20,000 rows
+// 2048 -> 512: 54.3, 58.1, 70.7).
 int f8_tile_width(long long rows, int Kq, int Nq, int num_sms) {
-    const int widths[3] = {64, 32, 16}, partial[3] = {512, 320, 220}, rest[3] = {800, 500, 400};
+    // measured ns of a partial, and of a tile's beginning and end
+    const int widths[3] = {64, 32, 16}, partial[3] = {456, 341, 272}, rest[3] = {2300, 1800, 950};
     int best = 64;
     double least = 0.0;
-    for (int i = 0; i < 3; ++i) {
+    // (below 32 rows the many CTAs of the narrowest tiles wait for the same few lines of x:
+    // 24 rows 4096 -> 4096 26 us, 16.5 with 32 channels a tile)
+    for (int i = 0; i < (rows < 32 ? 2 : 3); ++i) {
         const long long tiles = (rows + F8_BM - 1) / F8_BM * ((Nq + widths[i] - 1) / widths[i]);
         const long long waves = (tiles + num_sms - 1) / num_sms;
         const double t = static_cast<double>(waves) *
@@ -450,8 +472,7 @@ cudaError_t launch_f8_tc(const CUtensorMap& mx, const CUtensorMap& mw, const F8T
 }  // namespace
 
 size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq) {
-    (void)Nq;
-    if (rows <= F8_FEW_ROWS) return 0;
+    if (f8_few_rows(rows, Kq, Nq)) return 0;
     return quantised_bytes(rows, Kq) + static_cast<size_t>(scale_pitch(rows)) * 4 * blocks_of(Kq) * 4;
 }
 
@@ -464,10 +485,10 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     const bool vec = Kq % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
     auto* xb = static_cast<const __nv_bfloat16*>(x);
     auto* ob = static_cast<__nv_bfloat16*>(out);
-    if (rows <= F8_FEW_ROWS) {
+    if (f8_few_rows(rows, Kq, Nq)) {
         const F8Params p = {xb, static_cast<const uint8_t*>(wq), ws, ep, ob, rows, Kq, Nq, Kp,
                             kblk, nblk, conj ? 1 : 0, act};
-        return launch_rows<4>(p, vec, stream);
+        return rows == 1 ? launch_rows<1>(p, vec, stream) : launch_rows<4>(p, vec, stream);
     }
     auto* xq = static_cast<uint8_t*>(workspace);
     auto* xs = reinterpret_cast<float*>(xq + quantised_bytes(rows, Kq));
