@@ -164,9 +164,7 @@ def _addr(t):
     """_ptr as an integer (None: 0)."""
     if t is None:
         return 0
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
+    return t if t.__class__ is int else t.data_ptr()
 
 
 _raw_stream = None
