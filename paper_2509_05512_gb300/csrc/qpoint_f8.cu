@@ -13,6 +13,7 @@
 #include <cuda_bf16.h>
 
 #include <cstdio>
+#include <type_traits>
 
 #include "f8.cuh"
 #include "internal.h"
@@ -450,23 +451,31 @@ int f8_tile_width(long long rows, int Kq, int Nq, int num_sms) {
     return best;
 }
 
-template <int BNQ>
-cudaError_t launch_f8_tc(const CUtensorMap& mx, const CUtensorMap& mw, const F8TcParams& p,
+template <int BNQ, bool SILU, bool AFFINE>
+cudaError_t launch_f8_form(const CUtensorMap& mx, const CUtensorMap& mw, const F8TcParams& p,
                          int num_sms, cudaStream_t stream) {
     using C = F8Cfg<BNQ>;
     const cudaError_t e = cudaFuncSetAttribute(
-        qpoint_f8_kernel<BNQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
+        qpoint_f8_kernel<BNQ, SILU, AFFINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
     if (e != cudaSuccess) return e;
     static const cudaError_t regs = [] {  // the exchange counts on the launch's registers
         cudaFuncAttributes a;
-        const cudaError_t q = cudaFuncGetAttributes(&a, qpoint_f8_kernel<BNQ>);
+        const cudaError_t q = cudaFuncGetAttributes(&a, qpoint_f8_kernel<BNQ, SILU, AFFINE>);
         return q != cudaSuccess ? q
                                 : (a.numRegs < F8_REGS ? cudaErrorInvalidKernelImage : cudaSuccess);
     }();
     if (regs != cudaSuccess) return regs;
     const int grid = p.num_tiles < num_sms ? p.num_tiles : num_sms;
-    return launch_pdl(qpoint_f8_kernel<BNQ>, dim3(static_cast<unsigned>(grid)), dim3(F8_THREADS),
+    return launch_pdl(qpoint_f8_kernel<BNQ, SILU, AFFINE>, dim3(static_cast<unsigned>(grid)), dim3(F8_THREADS),
                       C::SMEM_BYTES, stream, mx, mw, p);
+}
+
+template <int BNQ>
+cudaError_t launch_f8_tc(const CUtensorMap& mx, const CUtensorMap& mw, const F8TcParams& p,
+                         int num_sms, cudaStream_t stream) {
+    if (p.act == 2) return launch_f8_form<BNQ, true, true>(mx, mw, p, num_sms, stream);
+    return p.ep.bias || p.ep.scale ? launch_f8_form<BNQ, false, true>(mx, mw, p, num_sms, stream)
+                                   : launch_f8_form<BNQ, false, false>(mx, mw, p, num_sms, stream);
 }
 
 }  // namespace

@@ -46,7 +46,7 @@ constexpr int F8_EPI_WARPS = 8;
 constexpr int F8_BM = 128;
 // Registers a thread: at launch, and after the warpgroups' exchange.  An increase waits until
 // the block's own registers cover it, so the shares must not pass the launch's total.
-constexpr int F8_REGS = 168, F8_REGS_ISSUE = 72, F8_REGS_EPI = 216;
+constexpr int F8_REGS = 168, F8_REGS_ISSUE = 56, F8_REGS_EPI = 224;
 static_assert(128 * F8_REGS_ISSUE + 256 * F8_REGS_EPI <= F8_THREADS * F8_REGS, "register shares");
 
 struct F8TcParams {
@@ -190,9 +190,9 @@ __device__ __forceinline__ void f8_copy_rows(uint32_t stage, __nv_bfloat16* o, i
 // stored by the thread that has them (102,400 rows 512 -> 1024: 113 us; 118 staged in shared
 // memory, 117 staged and copied by TMA); rows that do not start at one are staged and stored along
 // the rows (7473 rows 520 -> 328: 49 us when each thread stores its own row, staged 17).
-template <int BNQ, int ACT>
+template <int BNQ, bool SILU, bool AFFINE, bool SECTOR>
 __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const float* scale,
-                                              const float* shift, bool affine, uint32_t stage,
+                                              const float* shift, uint32_t stage,
                                               const F8TcParams& p, long long row0, int co0,
                                               int n0) {
     using C = F8Cfg<BNQ>;
@@ -200,10 +200,11 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
     const int rows =
         row0 < p.rows ? static_cast<int>(p.rows - row0 < 32 ? p.rows - row0 : 32) : 0;
     const int left = p.Nq - n0;
+    const float least = p.act == 1 ? 0.0f : __uint_as_float(0xFF800000u);  // ReLU; NaN stays
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         __nv_bfloat16* o = p.out + row0 * (4LL * p.Nq) + (co0 + c) * p.Nq + n0;
-        __syncwarp();  // the other component's reads
+        if constexpr (!SECTOR) __syncwarp();  // the other component's reads
 #pragma unroll
         for (int g = 0; g < BNQ; g += 16) {
             uint32_t v[8];
@@ -212,7 +213,7 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                 float z[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) z[k] = acc[c][g + j + k];
-                if (affine) {
+                if constexpr (AFFINE) {
                     const float4 sc = *reinterpret_cast<const float4*>(scale + c * BNQ + g + j);
                     const float4 sh = *reinterpret_cast<const float4*>(shift + c * BNQ + g + j);
                     z[0] = fmaf(sc.x, z[0], sh.x);
@@ -220,17 +221,17 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                     z[2] = fmaf(sc.z, z[2], sh.z);
                     z[3] = fmaf(sc.w, z[3], sh.w);
                 }
-                if constexpr (ACT == 2) {
+                if constexpr (SILU) {
                     f8_silu2(z[0], z[1]);
                     f8_silu2(z[2], z[3]);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) z[k] = f8_act(z[k], ACT);
+                    for (int k = 0; k < 4; ++k) z[k] = z[k] < least ? least : z[k];
                 }
                 v[j / 2] = tc::pack_bf16x2(z[0], z[1]);
                 v[j / 2 + 1] = tc::pack_bf16x2(z[2], z[3]);
             }
-            if (p.store == F8_STORE_SECTOR) {
+            if constexpr (SECTOR) {
                 if (lane < rows && g < left) st_global_na_32(o + lane * (4LL * p.Nq) + g, v);
             } else {
                 const uint32_t at = stage + lane * C::OUT_PITCH + 2 * g;
@@ -238,6 +239,7 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                 sts_u4(at + 16, make_uint4(v[4], v[5], v[6], v[7]));
             }
         }
+        if constexpr (SECTOR) continue;
         __syncwarp();
         if (p.store == F8_STORE_16) {
             constexpr int PER_ROW = BNQ / 8;  // 16-byte units
@@ -256,7 +258,10 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
     }
 }
 
-template <int BNQ>
+// SILU or not (ReLU or none then), and whether the epilogue has per-channel vectors: forms of their
+// own, for the epilogue's code is as long as the rest.  One form with every branch takes 157 us
+// instead of 144 for 102,400 rows 512 -> 1024 with SiLU.
+template <int BNQ, bool SILU, bool AFFINE>
 __global__ void __launch_bounds__(F8_THREADS, 1)
     qpoint_f8_kernel(const __grid_constant__ CUtensorMap tmap_x,
                      const __grid_constant__ CUtensorMap tmap_w, const F8TcParams p) {
@@ -462,7 +467,6 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         float* shift = scale + 2 * BNQ;
         const uint32_t stage = smem_u32(smem + C::RING + C::SCALES) +
                                (warp - F8_EPI_WARP0) * 32 * C::OUT_PITCH;
-        const bool affine = p.ep.bias || p.ep.scale;
         // factors of this lane's row for component co0; co0 + 1 is 512 bytes on, ci 2 KB a step
         const uint32_t mine = factors + co0 * (F8_BM * 4) + 4u * (qd * 32 + lane);
         uint32_t ss = 0, phase_s = 0;
@@ -471,7 +475,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         for (int t = blockIdx.x; ok && t < p.num_tiles; t += gridDim.x) {
             const int mt = t / p.ntiles, nt = t - mt * p.ntiles;
             const int n0 = nt * BNQ;
-            if (affine) {
+            if constexpr (AFFINE) {
                 __syncwarp();  // the previous tile's reads
                 for (int j = lane; j < 2 * BNQ; j += 32) {
                     const int n = n0 + (j & (BNQ - 1));
@@ -529,12 +533,11 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
             }
             if (!ok) break;
             const long long row0 = static_cast<long long>(mt) * F8_BM + qd * 32;
-            if (p.act == 2)
-                f8_store_tile<BNQ, 2>(acc, scale, shift, affine, stage, p, row0, co0, n0);
-            else if (p.act == 1)
-                f8_store_tile<BNQ, 1>(acc, scale, shift, affine, stage, p, row0, co0, n0);
+            if (p.store == F8_STORE_SECTOR)
+                f8_store_tile<BNQ, SILU, AFFINE, true>(acc, scale, shift, stage, p, row0, co0, n0);
             else
-                f8_store_tile<BNQ, 0>(acc, scale, shift, affine, stage, p, row0, co0, n0);
+                f8_store_tile<BNQ, SILU, AFFINE, false>(acc, scale, shift, stage, p, row0, co0,
+                                                        n0);
         }
     }
 
