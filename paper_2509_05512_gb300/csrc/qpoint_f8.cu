@@ -12,8 +12,8 @@
 // padding; s_x [4][blocks][rows], s_w [4][ceil(Nq / 128)][blocks].
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <cstdio>
-#include <type_traits>
 
 #include "f8.cuh"
 #include "internal.h"
@@ -455,18 +455,23 @@ template <int BNQ, bool SILU, bool AFFINE>
 cudaError_t launch_f8_form(const CUtensorMap& mx, const CUtensorMap& mw, const F8TcParams& p,
                          int num_sms, cudaStream_t stream) {
     using C = F8Cfg<BNQ>;
-    const cudaError_t e = cudaFuncSetAttribute(
-        qpoint_f8_kernel<BNQ, SILU, AFFINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
+    auto* kern = qpoint_f8_kernel<BNQ, SILU, AFFINE>;
+    // once a device: the shared memory, and a look at the registers that the exchange counts on
+    static std::atomic<unsigned long long> ready{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    static const cudaError_t regs = [] {  // the exchange counts on the launch's registers
+    if (dev >= 64 || !((ready.load(std::memory_order_acquire) >> dev) & 1ull)) {
         cudaFuncAttributes a;
-        const cudaError_t q = cudaFuncGetAttributes(&a, qpoint_f8_kernel<BNQ, SILU, AFFINE>);
-        return q != cudaSuccess ? q
-                                : (a.numRegs < F8_REGS ? cudaErrorInvalidKernelImage : cudaSuccess);
-    }();
-    if (regs != cudaSuccess) return regs;
+        if ((e = cudaFuncGetAttributes(&a, kern)) != cudaSuccess) return e;
+        if (a.numRegs < F8_REGS) return cudaErrorInvalidKernelImage;
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 C::SMEM_BYTES);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+    }
     const int grid = p.num_tiles < num_sms ? p.num_tiles : num_sms;
-    return launch_pdl(qpoint_f8_kernel<BNQ, SILU, AFFINE>, dim3(static_cast<unsigned>(grid)), dim3(F8_THREADS),
+    return launch_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(F8_THREADS),
                       C::SMEM_BYTES, stream, mx, mw, p);
 }
 

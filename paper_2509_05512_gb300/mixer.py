@@ -121,11 +121,13 @@ def train(steps: int = 30, N: int = 8, H: int = 16, channels: int = 256, depth: 
 def main(argv=None) -> None:
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=30)
+    ap.add_argument("--images", type=int, default=8)
+    ap.add_argument("--size", type=int, default=16, help="pixels a side of the maps")
     ap.add_argument("--channels", type=int, default=256)
     ap.add_argument("--depth", type=int, default=3)
     ap.add_argument("--dropout", type=float, default=0.1)
     a = ap.parse_args(argv)
-    train(a.steps, channels=a.channels, depth=a.depth, p=a.dropout)
+    train(a.steps, a.images, a.size, channels=a.channels, depth=a.depth, p=a.dropout)
 
 
 if __name__ == "__main__":

@@ -641,14 +641,20 @@ def dropout(x, p, seed, offset=0, *, counter=None, out=None, stream=None):
     pass.  A call uses ceil(n / 8) counters from `offset` on (plus the int64 CUDA scalar
     `counter`, read when the kernel runs), so calls of one seed take offsets that far apart.
     out may be x."""
-    dtype = _dtype_of("x", x)
-    _check_tensor("x", x, x.shape, x.dtype)
-    _check_counter(counter)
-    if out is None:
-        out = _empty(stream, x.shape, x.dtype, x.device)
+    torch = _torch or _get_torch()
+    t, shape = x.dtype, x.shape
+    dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else _dtype_of("x", x)
+    if not x.is_cuda or not x.is_contiguous():
+        _check_tensor("x", x, shape, t)
+    if counter is not None:
+        _check_counter(counter)
+    if out is not None:
+        _check_tensor("out", out, shape, t)
     else:
-        _check_tensor("out", out, x.shape, x.dtype)
-    quan_dropout(x, x.numel(), dtype, p, seed, offset, counter, out, stream)
+        out = _empty(stream, shape, t, x.device)
+    _call(13, _DROPOUT(x.data_ptr(), x.numel(), dtype, p, seed, offset,
+                       0 if counter is None else counter.data_ptr(), out.data_ptr(),
+                       _stream(stream)))
     return out
 
 
@@ -709,21 +715,24 @@ def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
     return F8Weights(q, scale, 4 * Qin, 4 * Qout, bool(transpose))
 
 
-def _qpoint_f8(x, w, K, N, workspace, out, stream):
-    """rows, workspace and output of one 8-bit product of K input and N output channels."""
+def _qpoint_f8(x, K, N, workspace, out, stream):
+    """rows, workspace, its bytes and the output of one 8-bit product of K input and N output
+    channels."""
     torch = _torch or _get_torch()
-    lead = x.shape[:-1]
-    _check_tensor("x", x, lead + (K,), torch.bfloat16)
+    shape, bf16 = x.shape, torch.bfloat16
+    if x.dtype is not bf16 or shape[-1] != K or not x.is_cuda or not x.is_contiguous():
+        _check_tensor("x", x, shape[:-1] + (K,), bf16)
     rows = x.numel() // K
     if out is None:
-        out = _empty(stream, lead + (N,), torch.bfloat16, x.device)
+        out = _empty(stream, shape[:-1] + (N,), bf16, x.device)
     else:
-        _check_tensor("out", out, lead + (N,), torch.bfloat16)
-    need = quan_qpoint_f8_workspace_size(rows, K, N)
-    if workspace is None and need:
-        workspace = _empty(stream, (need,), torch.uint8, x.device)
-    return rows, workspace, \
-        0 if workspace is None else workspace.numel() * workspace.element_size(), out
+        _check_tensor("out", out, shape[:-1] + (N,), bf16)
+    if workspace is not None:
+        return rows, workspace, workspace.numel() * workspace.element_size(), out
+    nbytes = (_lib or load()).quan_qpoint_f8_workspace_size(rows, K, N)
+    if nbytes:
+        workspace = _empty(stream, nbytes, torch.uint8, x.device)
+    return rows, workspace, nbytes, out
 
 
 def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE, workspace=None,
@@ -733,12 +742,16 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
     act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d."""
     if w.transposed:
         raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
-    for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
-        if v is not None:
-            _check_tensor(name, v, (w.Cout,), _get_torch().float32)
-    rows, workspace, nbytes, out = _qpoint_f8(x, w, w.Cin, w.Cout, workspace, out, stream)
-    quan_qpoint_f8_fwd(x, w.q, w.scale, bias, scale, shift, rows, w.Cin, w.Cout, act, workspace,
-                       nbytes, out, stream)
+    q, wscale, Cin, Cout, _ = w
+    if bias is not None or scale is not None or shift is not None:
+        f32 = (_torch or _get_torch()).float32
+        for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
+            if v is not None:
+                _check_tensor(name, v, (Cout,), f32)
+    rows, workspace, nbytes, out = _qpoint_f8(x, Cin, Cout, workspace, out, stream)
+    _call(16, _QPOINT_F8(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), _addr(bias), _addr(scale),
+                         _addr(shift), rows, Cin, Cout, act, _addr(workspace), nbytes,
+                         out.data_ptr(), _stream(stream)))
     return out
 
 
@@ -747,27 +760,32 @@ def qpointwise_f8_backward_data(dy, w, *, workspace=None, out=None, stream=None)
     quantised in the call, and w = quantize_f8_weights(..., transpose=True) -> bf16 [..., Cin]."""
     if not w.transposed:
         raise ValueError("w holds the forward letters: quantize_f8_weights(..., transpose=True)")
-    rows, workspace, nbytes, out = _qpoint_f8(dy, w, w.Cout, w.Cin, workspace, out, stream)
-    quan_qpoint_f8_bwd_data(dy, w.q, w.scale, rows, w.Cin, w.Cout, workspace, nbytes, out, stream)
+    q, wscale, Cin, Cout, _ = w
+    rows, workspace, nbytes, out = _qpoint_f8(dy, Cout, Cin, workspace, out, stream)
+    _call(17, _QPOINT_F8_BWD(dy.data_ptr(), q.data_ptr(), wscale.data_ptr(), rows, Cin, Cout,
+                             _addr(workspace), nbytes, out.data_ptr(), _stream(stream)))
     return out
 
 
-def _join_shape(like, post, gate, pre):
+def _join_shape(like, shape, post, gate, pre):
     """(rows, C, images) of a join's tensors, its vectors checked."""
     f32 = (_torch or _get_torch()).float32
-    shape = like.shape
     C = shape[-1]
-    images = 1
+    vec, images = (C,), 1
     if gate is not None:
-        if gate.dim() == 1:
-            _check_tensor("gate", gate, (C,), f32)
-        else:
+        want = vec
+        if gate.dim() != 1:
             images = shape[0]
-            _check_tensor("gate", gate, (images, C), f32)
-    if post is not None:
-        _check_tensor("post", post, (C,), f32)
-    if pre is not None:
-        _check_tensor("pre", pre, (C,), f32)
+            want = (images, C)
+        if gate.dtype is not f32 or gate.shape != want or not gate.is_cuda or \
+                not gate.is_contiguous():
+            _check_tensor("gate", gate, want, f32)
+    if post is not None and (post.dtype is not f32 or post.shape != vec or not post.is_cuda or
+                             not post.is_contiguous()):
+        _check_tensor("post", post, vec, f32)
+    if pre is not None and (pre.dtype is not f32 or pre.shape != vec or not pre.is_cuda or
+                            not pre.is_contiguous()):
+        _check_tensor("pre", pre, vec, f32)
     return like.numel() // C if C else 0, C, max(images, 1)
 
 
@@ -779,22 +797,30 @@ def residual_join(x, h=None, *, post=None, gate=None, pre=None, alpha=1.0, group
     no n).  gate: fp32 [C], or [N, C] for a gate of each image.  groups=4 normalises each
     quaternion component by itself.  p, seed, offset, counter: see `dropout`.  Without h only the
     norm of x is taken.  Returns (y, n); y may be given as x and n as h (in place)."""
-    dtype = _dtype_of("x", x)
-    _check_tensor("x", x, x.shape, x.dtype)
-    rows, C, images = _join_shape(x, post, gate, pre)
-    _check_counter(counter)
+    torch = _torch or _get_torch()
+    t, shape = x.dtype, x.shape
+    dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else _dtype_of("x", x)
+    if not x.is_cuda or not x.is_contiguous():
+        _check_tensor("x", x, shape, t)
+    rows, C, images = _join_shape(x, shape, post, gate, pre)
+    if counter is not None:
+        _check_counter(counter)
     if h is not None:
-        _check_tensor("h", h, x.shape, x.dtype)
-    if y is not None:
-        _check_tensor("y", y, x.shape, x.dtype)
-    elif h is not None:
-        y = _empty(stream, x.shape, x.dtype, x.device)
+        if h.dtype is not t or h.shape != shape or not h.is_cuda or not h.is_contiguous():
+            _check_tensor("h", h, shape, t)
+        if y is None:
+            y = _empty(stream, shape, t, x.device)
+        else:
+            _check_tensor("y", y, shape, t)
+    elif y is not None:
+        raise ValueError("y is given without h")
     if n is not None:
-        _check_tensor("n", n, x.shape, x.dtype)
+        _check_tensor("n", n, shape, t)
     elif pre is not None:
-        n = _empty(stream, x.shape, x.dtype, x.device)
-    quan_residual_join_fwd(x, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p,
-                           seed, offset, counter, y, n, stream)
+        n = _empty(stream, shape, t, x.device)
+    _call(14, _JOIN_FWD(x.data_ptr(), _addr(h), _addr(post), _addr(gate), _addr(pre), rows, images,
+                        C, groups, dtype, alpha, eps, p, seed, offset, _addr(counter), _addr(y),
+                        _addr(n), _stream(stream)))
     return y, n
 
 
@@ -805,32 +831,40 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
     call's y (needed with pre) and h.  Returns (dx, dh, dpost, dgate, dpre), fp32 sums shaped as
     their vectors, None for what is absent; without pre, dx is dy itself.  dx may be given as dy
     or dn, dh as dn or h (in place)."""
-    import torch
+    torch = _torch or _get_torch()
     like = dy if dy is not None else dn
     if like is None:
         raise ValueError("dy or dn must be given")
-    dtype = _dtype_of("dy" if dy is not None else "dn", like)
-    rows, C, images = _join_shape(like, post, gate, pre)
-    _check_counter(counter)
-    for name, t in (("dy", dy), ("dn", dn), ("y", y), ("h", h), ("dx", dx), ("dh", dh)):
-        if t is not None:
-            _check_tensor(name, t, like.shape, like.dtype)
+    t, shape, device = like.dtype, like.shape, like.device
+    dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else \
+        _dtype_of("dy" if dy is not None else "dn", like)
+    rows, C, images = _join_shape(like, shape, post, gate, pre)
+    if counter is not None:
+        _check_counter(counter)
+    for name, v in (("dy", dy), ("dn", dn), ("y", y), ("h", h), ("dx", dx), ("dh", dh)):
+        if v is not None and (v.dtype is not t or v.shape != shape or not v.is_cuda or
+                              not v.is_contiguous()):
+            _check_tensor(name, v, shape, t)
     if pre is None:
         y = None
+        if h is None and post is None and gate is None:
+            return dy, None, None, None, None
     elif dx is None:
-        dx = _empty(stream, like.shape, like.dtype, like.device)
+        dx = _empty(stream, shape, t, device)
     if h is not None and dh is None:
-        dh = _empty(stream, like.shape, like.dtype, like.device)
-    need = quan_residual_join_bwd_workspace_size(rows, C, groups, images)
-    if workspace is None and need:
-        workspace = _empty(stream, (need,), torch.uint8, like.device)
-    sums = [None if v is None else _empty(stream, v.shape, torch.float32, like.device)
-            for v in (post, gate, pre)]
-    if pre is None and h is None:
-        return dy, None, None, None, None
-    quan_residual_join_bwd(
-        dy, dn, y, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p, seed,
-        offset, counter, workspace,
-        0 if workspace is None else workspace.numel() * workspace.element_size(), dx, dh, *sums,
-        stream)
-    return (dy if dx is None else dx, dh, *sums)
+        dh = _empty(stream, shape, t, device)
+    f32 = torch.float32
+    dpost = None if post is None else _empty(stream, C, f32, device)
+    dgate = None if gate is None else _empty(stream, gate.shape, f32, device)
+    dpre = None if pre is None else _empty(stream, C, f32, device)
+    if workspace is None:
+        nbytes = (_lib or load()).quan_residual_join_bwd_workspace_size(rows, C, groups, images)
+        if nbytes:
+            workspace = _empty(stream, nbytes, torch.uint8, device)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _call(15, _JOIN_BWD(_addr(dy), _addr(dn), _addr(y), _addr(h), _addr(post), _addr(gate),
+                        _addr(pre), rows, images, C, groups, dtype, alpha, eps, p, seed, offset,
+                        _addr(counter), _addr(workspace), nbytes, _addr(dx), _addr(dh),
+                        _addr(dpost), _addr(dgate), _addr(dpre), _stream(stream)))
+    return (dy if dx is None else dx, dh, dpost, dgate, dpre)
