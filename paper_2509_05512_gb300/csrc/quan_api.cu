@@ -419,6 +419,9 @@ bool misaligned(const void* const* t, int n, size_t align) {
     return false;
 }
 
+// Channel counts of the 8-bit product (its launches' grids hold more).
+constexpr int F8_MAX_CHANNELS = 1 << 20;
+
 // The product both directions of the 8-bit pointwise convolution run: K input and N output
 // channels of the call.
 quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
@@ -437,7 +440,7 @@ quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
     if (rows == 0) return QUAN_OK;
     if (!x || !wq || !wscale || !out) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
     if (rows >= (1LL << 31) || rows >= (1LL << 40) / K || rows >= (1LL << 40) / N ||
-        static_cast<long long>(K) * N >= (1LL << 34))
+        K > F8_MAX_CHANNELS || N > F8_MAX_CHANNELS)
         return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
     const void* half[] = {x, out};
     const void* vectors[] = {wscale, ep.bias, ep.scale, ep.shift};
@@ -1092,7 +1095,7 @@ quan_status_t quan_f8_weights(const void* wr, const void* wi, const void* wj, co
     if (Cin < 1 || Cout < 1 || Cin % 4 || Cout % 4)
         return fail(QUAN_ERR_INVALID_ARG, "Cin=%d and Cout=%d must be positive multiples of 4",
                     Cin, Cout);
-    if (static_cast<long long>(Cin) * Cout >= (1LL << 34) || Cout > 4 * 128 * 65535)
+    if (Cin > F8_MAX_CHANNELS || Cout > F8_MAX_CHANNELS)
         return fail(QUAN_ERR_UNSUPPORTED, "letters too large");
     if (misaligned(w, 4, 2) || reinterpret_cast<uintptr_t>(q) % 16 != 0 ||
         reinterpret_cast<uintptr_t>(scale) % 4 != 0)

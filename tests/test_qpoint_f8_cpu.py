@@ -110,7 +110,8 @@ def test_gradient_refuses(lib, bad):
 def test_product_limits(lib):
     assert _fwd(lib, rows=0) == quan.QUAN_OK
     assert _fwd(lib, rows=1 << 31) == UNSUPPORTED
-    assert _fwd(lib, Cin=1 << 18, Cout=1 << 18) == UNSUPPORTED
+    assert _fwd(lib, Cin=1 << 21) == UNSUPPORTED and _fwd(lib, Cout=1 << 21) == UNSUPPORTED
+    assert _bwd(lib, rows=1 << 30, Cin=4, Cout=1 << 12) == UNSUPPORTED
     assert lib.quan_qpoint_f8_workspace_size(8, 6, 4) == 0
     need = lib.quan_qpoint_f8_workspace_size(4096, 512, 512)
     if need:

@@ -112,7 +112,8 @@ SHAPES = [(1, 4, 4), (1, 512, 1024), (2, 64, 512), (3, 520, 36), (5, 1024, 1024)
           (17, 100, 340), (49, 2048, 512), (127, 512, 256), (128, 512, 256), (129, 512, 260),
           (1000, 328, 520), (777, 1028, 516), (300, 4, 2048), (640, 64, 64), (2500, 128, 1280),
           (20001, 256, 64), (20003, 1100, 64), (25000, 300, 20), (21000, 1028, 128),
-          (20100, 516, 1032), (6000, 12, 28), (3000, 140, 44), (9000, 520, 264)]
+          (20100, 516, 1032), (6000, 12, 28), (3000, 140, 44), (9000, 520, 264),
+          (1280, 2060, 1024), (40000, 1032, 128), (16, 512, 512), (24, 2048, 512)]
 
 
 @pytest.mark.parametrize("rows, Cin, Cout", SHAPES)
