@@ -24,9 +24,10 @@
 // What bounds it now: a buffer's round trip.  A partial's MMAs take 514 clocks, and 390 more pass
 // from their issue to their arrival at the epilogue; taking the partial out takes the slowest of
 // eight warps about 700, the way back to the issuer 200; two buffers make that about 1000 clocks a
-// partial.  Four buffers of 128 columns (BNQ = 32) hide the trip, but an MMA of 128 columns takes
-// 94 clocks, not 64 (the rows' operand is read again), and the epilogue's fixed work is per
-// partial: 563 us.
+// partial: 25,600 rows 4096 -> 4096 365 us, 2.35 PFLOP/s.  Buffers of 128 columns, twice as many,
+// hide the trip, but an MMA of 128 columns takes 94 clocks, not 64 (the rows' operand is read
+// again): as two halves of a tile 511 us for the call that takes 420; as tiles of 32 channels on two
+// CTAs an SM 437, bound by the copies from L2, 39 bytes a clock and SM.
 //
 // BNQ = 64, 32 or 16: with few row tiles the narrower ones spread the letters over more SMs (see
 // f8_tile_width).

@@ -14,13 +14,20 @@
 // is rounded once, on its way out, and n is taken of y before that rounding.  The gradients need
 // no statistics kept from the forward call: they read h and y whole anyway.
 //
-// Both directions are bound by HBM: one pass, each tensor read or written once.  A row stays in
-// registers between its two reductions: tps threads (a power of two) hold a group, eight
-// consecutive channels a thread (chunks of two at most), so that narrow rows share a warp and
-// reduce with shuffles, wide ones a block of up to 512 threads (8192 channels at most).  Column sums stay in each
-// thread's registers for all of its block's rows; blocks leave one row of partial sums each,
-// added in a fixed order by a second launch, so that repeated calls give the same bits.
+// Both directions are one pass, each tensor read or written once.  A row stays in registers
+// between its two reductions: tps threads (a power of two) hold a group, eight consecutive channels
+// a thread (at most two such chunks), so that narrow rows share a warp and reduce with shuffles,
+// wide ones a block of up to 512 threads (8192 channels at most).  Column sums stay in each thread's
+// registers for all of its block's rows; blocks leave one row of partial sums each, added in a fixed
+// order by a second launch, so that repeated calls give the same bits.
+//
+// Measured on 32 x 56 x 56 x 256 bf16 with dropout: forward 38 us, 5.4 TB/s, bound by HBM with the
+// generator's integer work beside it (two rows under way a thread: 55 without the row ahead);
+// gradients 64 us, 4.8 TB/s, bound by issue, about 470 instructions for eight elements of four
+// tensors (the row ahead: 85 without; three blocks an SM spill: 89).
 #include <cuda_bf16.h>
+
+#include <atomic>
 
 #include "internal.h"
 #include "philox.cuh"
@@ -32,7 +39,8 @@ namespace {
 
 // ------------------------------------------------------------------ dropout
 
-// UNROLL blocks of eight elements a thread, their loads first.
+// UNROLL blocks of eight elements a thread, their loads first.  32 x 112 x 112 x 64 bf16: 17.6 us,
+// 5.8 TB/s, HBM beside the generator's integer issue (22 us with one block a thread).
 template <typename T, bool VEC, int UNROLL>
 __global__ void __launch_bounds__(256) dropout_kernel(const T* x, long long n, DropoutArgs d,
                                                       T* out) {
@@ -384,8 +392,7 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
         // bf16; fp32 rows have twice the bytes under way as it is)
         constexpr bool AHEAD = sizeof(T) == 2 && NC == 1;
         Chunk<T, LV> cdy[NC], cdn[NC], cy[NC], ch[NC];
-        auto fetch = [&](long long row) {
-            const long long at = row * p.C + q.seg * p.S;
+        auto fetch = [&](long long row, long long at) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (q.ts + c * p.tps) * 8;
@@ -401,12 +408,15 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
                 if (h) ch[c].load(h + at + col, left);
             }
         };
-        if (AHEAD) fetch(first + q.slot);
-        for (long long r0 = first; r0 < last; r0 += p.slots) {
-            const long long row = r0 + q.slot;
-            if (!AHEAD) fetch(row);
+        const long long at_step = static_cast<long long>(p.slots) * p.C;
+        long long row = first + q.slot, at = row * p.C + q.seg * p.S;
+        if (AHEAD) fetch(row, at);
+        for (long long r0 = first; r0 < last; r0 += p.slots, row += p.slots) {
+            if constexpr (!AHEAD) {  // (one register pair less across the row)
+                at = row * p.C + q.seg * p.S;
+                fetch(row, at);
+            }
             const bool active = row < last && q.slot < p.slots;
-            const long long at = row * p.C + q.seg * p.S;
             float g[NC][8], yv[NC][8], nv[NC][8], hv[NC][8];
             int left[NC];
 #pragma unroll
@@ -419,7 +429,11 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
                 }
                 if (h) ch[c].values(hv[c]);
             }
-            if (AHEAD) fetch(row + p.slots);
+            const long long here = at;
+            if constexpr (AHEAD) {
+                at += at_step;
+                fetch(row + p.slots, at);
+            }
             float s3[3] = {0.0f, 0.0f, 0.0f};  // sums of h^2, y^2 and t y
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -449,12 +463,12 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
                         g[c][j] = fmaf(rn, pre[c][j], fmaf(m, yv[c][j], g[c][j]));
                         a_pre[c][j] = fmaf(rn, yv[c][j], a_pre[c][j]);
                     }
-                    o.set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
+                    o.set_store(g[c], dx + here + (q.ts + c * p.tps) * 8, left[c]);
                 }
             } else if (dx) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
-                    o.set_store(g[c], dx + at + (q.ts + c * p.tps) * 8, left[c]);
+                    o.set_store(g[c], dx + here + (q.ts + c * p.tps) * 8, left[c]);
             }
             if (h) {
                 float w1[1] = {0.0f};
@@ -463,7 +477,7 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
                     Dropout8 m;
                     m.none();
                     if (p.drop.draws)
-                        draw_from<LV == 8>(m, p.drop, base, at + (q.ts + c * p.tps) * 8);
+                        draw_from<LV == 8>(m, p.drop, base, here + (q.ts + c * p.tps) * 8);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         // (both factors are selected: what is dropped has no part, be it infinite)
@@ -485,7 +499,7 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256, CROSS ? 1 : 2) join_bwd_ker
                 }
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
-                    o.set_store(g[c], dh + at + (q.ts + c * p.tps) * 8, left[c]);
+                    o.set_store(g[c], dh + here + (q.ts + c * p.tps) * 8, left[c]);
             }
         }
         if (p.part_post || p.part_gate) {
@@ -596,30 +610,49 @@ int load_width(int S, int C, const void* const* t, int n) {
 }
 
 // A thread's one or two chunks; two only where a row takes more than the block's threads, so
-// where its sums cross warps.
+// where its sums cross warps.  Forward, a block takes rows until none is left, and there are as many
+// blocks as run at once (`blocks` at most): with twice as many the last ones run by themselves
+// (32 x 56 x 56 x 256: 40 us, 38 with one wave).
 template <typename T, int LV, int NC, bool CROSS>
-cudaError_t launch_join_nc(const JoinParams& p, const JoinPlan& pl, bool backward, int grid,
-                           cudaStream_t stream) {
-    const dim3 g(static_cast<unsigned>(grid)), b(static_cast<unsigned>(pl.threads));
-    if (!backward) return launch_pdl(join_fwd_kernel<T, LV, NC, CROSS>, g, b, 0, stream, p);
-    const size_t smem = pl.slots > 1 ? static_cast<size_t>(pl.slots) * p.C * 4 : 0;
-    return launch_pdl(join_bwd_kernel<T, LV, NC, CROSS>, g, b, smem, stream, p);
+cudaError_t launch_join_nc(const JoinParams& p, const JoinPlan& pl, bool backward,
+                           long long blocks, int num_sms, cudaStream_t stream) {
+    const dim3 b(static_cast<unsigned>(pl.threads));
+    if (backward) {
+        const size_t smem = pl.slots > 1 ? static_cast<size_t>(pl.slots) * p.C * 4 : 0;
+        return launch_pdl(join_bwd_kernel<T, LV, NC, CROSS>,
+                          dim3(static_cast<unsigned>(blocks)), b, smem, stream, p);
+    }
+    static std::atomic<int> at_once[2];  // blocks an SM, of 256 and of 512 threads
+    std::atomic<int>& known = at_once[pl.threads > 256];
+    int per_sm = known.load(std::memory_order_relaxed);
+    if (per_sm == 0) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(
+            &per_sm, join_fwd_kernel<T, LV, NC, CROSS>, pl.threads, 0);
+        if (e != cudaSuccess) return e;
+        if (per_sm < 1) per_sm = 1;
+        known.store(per_sm, std::memory_order_relaxed);
+    }
+    const long long cap = static_cast<long long>(num_sms) * per_sm;
+    return launch_pdl(join_fwd_kernel<T, LV, NC, CROSS>,
+                      dim3(static_cast<unsigned>(blocks < cap ? blocks : cap)), b, 0, stream, p);
 }
 
 template <typename T, int LV>
-cudaError_t launch_join_lv(const JoinParams& p, const JoinPlan& pl, bool backward, int grid,
-                           cudaStream_t stream) {
-    if (pl.nc == 2) return launch_join_nc<T, LV, 2, true>(p, pl, backward, grid, stream);
-    return pl.tps > 32 ? launch_join_nc<T, LV, 1, true>(p, pl, backward, grid, stream)
-                       : launch_join_nc<T, LV, 1, false>(p, pl, backward, grid, stream);
+cudaError_t launch_join_lv(const JoinParams& p, const JoinPlan& pl, bool backward,
+                           long long blocks, int num_sms, cudaStream_t stream) {
+    if (pl.nc == 2)
+        return launch_join_nc<T, LV, 2, true>(p, pl, backward, blocks, num_sms, stream);
+    return pl.tps > 32
+               ? launch_join_nc<T, LV, 1, true>(p, pl, backward, blocks, num_sms, stream)
+               : launch_join_nc<T, LV, 1, false>(p, pl, backward, blocks, num_sms, stream);
 }
 
 template <typename T>
 cudaError_t launch_join_t(const JoinParams& p, const JoinPlan& pl, int lv, bool backward,
-                          int grid, cudaStream_t stream) {
-    return lv == 8   ? launch_join_lv<T, 8>(p, pl, backward, grid, stream)
-           : lv == 4 ? launch_join_lv<T, 4>(p, pl, backward, grid, stream)
-                     : launch_join_lv<T, 1>(p, pl, backward, grid, stream);
+                          long long blocks, int num_sms, cudaStream_t stream) {
+    return lv == 8   ? launch_join_lv<T, 8>(p, pl, backward, blocks, num_sms, stream)
+           : lv == 4 ? launch_join_lv<T, 4>(p, pl, backward, blocks, num_sms, stream)
+                     : launch_join_lv<T, 1>(p, pl, backward, blocks, num_sms, stream);
 }
 
 void fill(JoinParams* p, const JoinArgs& a, const JoinPlan& pl) {
@@ -700,13 +733,10 @@ cudaError_t launch_join_fwd(const JoinArgs& a, int num_sms, cudaStream_t stream)
     join_plan(a.C, a.groups, &pl);
     JoinParams p = {};
     fill(&p, a, pl);
-    long long blocks = (a.rows + pl.slots - 1) / pl.slots;
-    const long long cap = static_cast<long long>(num_sms) * (pl.threads > 256 ? 2 : 6);
-    if (blocks > cap) blocks = cap;
+    const long long blocks = (a.rows + pl.slots - 1) / pl.slots;
     const int lv = join_load_width(a);
-    return a.f32 ? launch_join_t<float>(p, pl, lv, false, static_cast<int>(blocks), stream)
-                 : launch_join_t<__nv_bfloat16>(p, pl, lv, false, static_cast<int>(blocks),
-                                                stream);
+    return a.f32 ? launch_join_t<float>(p, pl, lv, false, blocks, num_sms, stream)
+                 : launch_join_t<__nv_bfloat16>(p, pl, lv, false, blocks, num_sms, stream);
 }
 
 // Partial sums: one row of dpost and dpre a block, and one row of dgate a unit, unless there is
@@ -750,8 +780,9 @@ cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, f
     p.part_pre = dpre ? (many ? workspace + C : dpre) : nullptr;
     p.part_stride = 2 * C;
     const int lv = join_load_width(a);
-    cudaError_t e = a.f32 ? launch_join_t<float>(p, pl, lv, true, pl.grid, stream)
-                          : launch_join_t<__nv_bfloat16>(p, pl, lv, true, pl.grid, stream);
+    cudaError_t e =
+        a.f32 ? launch_join_t<float>(p, pl, lv, true, pl.grid, num_sms, stream)
+              : launch_join_t<__nv_bfloat16>(p, pl, lv, true, pl.grid, num_sms, stream);
     if (e != cudaSuccess) return e;
     const bool sum_g = a.gate && pl.chunks > 1;
     if (!(many && (dpost || dpre)) && !sum_g) return cudaSuccess;
