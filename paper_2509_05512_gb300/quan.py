@@ -739,7 +739,9 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
                   out=None, stream=None):
     """Pointwise quaternion convolution in 8-bit floating point: bf16 x [..., Cin] (CUDA), which
     is quantised in the call, and w = quantize_f8_weights(...) -> bf16 [..., Cout],
-    act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d."""
+    act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d.  Half the bytes of
+    bf16 letters; faster than qconv2d in wide layers only (25,600 rows: 4096 -> 4096 420 us
+    against 485, 2048 -> 1024 86 against 78; 102,400 rows of 512 -> 1024 109 against 84)."""
     if w.transposed:
         raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
     q, wscale, Cin, Cout, _ = w
