@@ -533,7 +533,7 @@ quan_status_t quan_f8_weights(const void* wr, const void* wi, const void* wj, co
  *   out        bf16 [rows][Cout] (device), rounded once from fp32; no overlap with an input
  * rows = 0 is a no-op.  Fewer than 2^31 rows, 2^40 elements a tensor and up to 2^20 channels, else
  * QUAN_ERR_UNSUPPORTED.  The tcgen05 kernel needs sm_103; its waits are bounded
- * (quan_device_status).  An activation of ReLU keeps a NaN.
+ * (quan_device_status).  An activation of ReLU keeps a NaN; SiLU of -infinity is NaN.
  */
 size_t quan_qpoint_f8_workspace_size(long long rows, int Cin, int Cout);
 quan_status_t quan_qpoint_f8_fwd(const void* x, const void* wq, const float* wscale,

@@ -174,9 +174,18 @@ struct F8Params {
     int act;
 };
 
+// SiLU z / (1 + e^-z), e^-z = 2^(-z log2 e), with the hardware's approximate 2^x and reciprocal,
+// and no cap on the exponent: from z = -87.3 down the divisor passes 2^126, its reciprocal is
+// flushed to 0 and the result is -0, where SiLU lies above -2^-119.  (A capped exponent leaves a
+// sigmoid that never falls further: -1e20 would give a number far from 0.)  -inf gives NaN, as
+// -inf / (1 + inf) does.
+__device__ __forceinline__ float f8_silu(float z) {
+    return z * rcp_approx_ftz(1.0f + ex2_approx_ftz(z * -1.44269504f));
+}
+
 // The epilogue's activation; a NaN stays one (a block without a scale has to show).
 __device__ __forceinline__ float f8_act(float z, int act) {
-    return act == 1 ? (z < 0.0f ? 0.0f : z) : tc::activate(z, act);
+    return act == 1 ? (z < 0.0f ? 0.0f : z) : (act == 2 ? f8_silu(z) : z);
 }
 
 __device__ __forceinline__ void f8_store(const F8Params& p, long long row, int co, int n,

@@ -131,18 +131,6 @@ __device__ __forceinline__ void f8_add(const uint32_t (&v)[N], float f, float* a
     for (int j = 0; j < N; ++j) acc[j] = fmaf(f, __uint_as_float(v[j]), acc[j]);
 }
 
-// SiLU of two values with one reciprocal: z / (1 + 2^(-z log2 e)) as tc::activate has it, the two
-// divisors inverted through their product (each below 2^61, the exponent being capped at 60: past
-// z = -41 the result's magnitude stays below 2^-54).  A tile's 32,768 values would take the
-// special function units 4096 clocks with two instructions each, and take 3072 with three a pair.
-__device__ __forceinline__ void f8_silu2(float& a, float& b) {
-    const float u = 1.0f + ex2_approx_ftz(fminf(a * -1.44269504f, 60.0f));
-    const float v = 1.0f + ex2_approx_ftz(fminf(b * -1.44269504f, 60.0f));
-    const float r = rcp_approx_ftz(u * v);
-    a = a * (r * v);
-    b = b * (r * u);
-}
-
 // 32 bytes of one row in one store: a whole sector.
 __device__ __forceinline__ void st_global_na_32(void* p, const uint32_t (&v)[8]) {
     asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
@@ -222,13 +210,9 @@ __device__ __forceinline__ void f8_store_tile(const float (&acc)[2][BNQ], const 
                     z[2] = fmaf(sc.z, z[2], sh.z);
                     z[3] = fmaf(sc.w, z[3], sh.w);
                 }
-                if constexpr (SILU) {
-                    f8_silu2(z[0], z[1]);
-                    f8_silu2(z[2], z[3]);
-                } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) z[k] = z[k] < least ? least : z[k];
-                }
+                for (int k = 0; k < 4; ++k)
+                    z[k] = SILU ? f8_silu(z[k]) : (z[k] < least ? least : z[k]);
                 v[j / 2] = tc::pack_bf16x2(z[0], z[1]);
                 v[j / 2 + 1] = tc::pack_bf16x2(z[2], z[3]);
             }
