@@ -831,8 +831,8 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
                            workspace=None, dx=None, dh=None, stream=None):
     """Gradients of `residual_join`, from dy (None: 0) and dn (None without pre) and the forward
     call's y (needed with pre) and h.  Returns (dx, dh, dpost, dgate, dpre), fp32 sums shaped as
-    their vectors, None for what is absent; without pre, dx is dy itself.  dx may be given as dy
-    or dn, dh as dn or h (in place)."""
+    their vectors, None for what is absent; without pre, dx is dy itself, or its copy in a dx that
+    is given.  dx may be given as dy or dn, dh as dn or h (in place)."""
     torch = _torch or _get_torch()
     like = dy if dy is not None else dn
     if like is None:
@@ -849,7 +849,8 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
             _check_tensor(name, v, shape, t)
     if pre is None:
         y = None
-        if h is None and post is None and gate is None:
+        if h is None and post is None and gate is None and dn is None and dx is None and \
+                dh is None:
             return dy, None, None, None, None
     elif dx is None:
         dx = _empty(stream, shape, t, device)

@@ -1,0 +1,79 @@
+"""The residual block's Python helpers without a GPU: what they hand to the library, seen through
+stand-ins for CUDA tensors and for the packed call."""
+import struct
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2509_05512_gb300 import build, quan
+
+
+class Device:
+    """A CUDA tensor's face: what the helpers look at, and an address that is never read."""
+
+    def __init__(self, shape, dtype, *, at=0x10000000, cuda=0, contiguous=True):
+        self.shape, self.dtype = torch.Size(shape), dtype
+        self.device = torch.device("cuda", cuda) if cuda >= 0 else torch.device("cpu")
+        self.is_cuda = cuda >= 0
+        self._at, self._contiguous = at, contiguous
+
+    def data_ptr(self):
+        return self._at
+
+    def get_device(self):
+        return self.device.index if self.is_cuda else -1
+
+    def is_contiguous(self):
+        return self._contiguous
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def reshape(self, *shape):
+        return self
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The packed calls made, as (entry point number, words); allocations are stand-ins."""
+    build.build_library()
+    quan.load()
+    made, at = [], iter(range(0x70000000000, 1 << 60, 1 << 34))
+    monkeypatch.setattr(quan, "_call", lambda op, words: made.append(
+        (op, struct.unpack("%dq" % (len(words) // 8), words))))
+    monkeypatch.setattr(quan, "_stream", lambda *a: 0)
+    monkeypatch.setattr(quan, "_empty", lambda stream, shape, dtype, device: Device(
+        (shape,) if isinstance(shape, int) else shape, dtype, at=next(at)))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    return made
+
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def test_a_given_dx_is_written_without_norm_and_branch(calls):
+    # the join without pre-norm and branch has dx = dy: a buffer for dx must be filled all the same
+    dy = Device((2, 3, 64), F32, at=0x20000000)
+    dx = Device((2, 3, 64), F32, at=0x30000000)
+    assert quan.residual_join_backward(dy, None, None)[0] is dy and not calls
+    got = quan.residual_join_backward(dy, None, None, dx=dx)
+    assert got[0] is dx and got[1:] == (None,) * 4
+    (op, words), = calls
+    assert op == 15 and words[0] == 0x20000000 and words[-6] == 0x30000000
+
+
+@pytest.mark.parametrize("extra", ["dn", "dh"])
+def test_a_gradient_that_belongs_to_nothing_reaches_the_checks(calls, extra):
+    # dn without pre, dh without h: the library refuses them, the helper may not drop them
+    dy, t = (Device((2, 3, 64), F32, at=a) for a in (0x20000000, 0x30000000))
+    args = {"dn": None, "y": None, extra: t}
+    quan.residual_join_backward(dy, **args)
+    (op, words), = calls
+    assert op == 15 and 0x30000000 in words
