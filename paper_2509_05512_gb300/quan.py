@@ -598,7 +598,12 @@ def _empty(stream, shape, dtype, device):
     torch = _torch or _get_torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    s = stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream)
+    if not isinstance(stream, int):
+        s = stream
+    elif stream == 0:  # (an ExternalStream of 0 is a new stream, not the default one)
+        s = torch.cuda.default_stream(device)
+    else:
+        s = torch.cuda.ExternalStream(stream)
     with torch.cuda.stream(s):
         return torch.empty(shape, dtype=dtype, device=device)
 

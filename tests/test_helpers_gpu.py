@@ -31,3 +31,25 @@ def test_a_given_dx_is_written_without_norm(dtype, branch):
     for bad in (dict(dn=dy), dict(dn=None, dh=dx) if not branch else dict(dn=dy)):
         with pytest.raises(quan.QuanError):
             quan.residual_join_backward(dy, y=None, h=h, **bad)
+
+
+def owner(t):
+    """The stream that the allocator keeps t's memory for."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not an allocation of torch's")
+
+
+def test_what_a_helper_allocates_belongs_to_its_stream():
+    # memory that belongs to another stream would be handed on while the call still uses it;
+    # the handle 0 is the default stream, whatever stream is current
+    x = torch.randn(1 << 22, device="cuda")  # its result is an allocation of its own
+    side = torch.cuda.Stream()
+    default = torch.cuda.default_stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for stream, handle in ((None, side.cuda_stream), (side, side.cuda_stream),
+                               (side.cuda_stream, side.cuda_stream), (default, 0), (0, 0)):
+            assert owner(quan.dropout(x, 0.5, 1, stream=stream)) == handle
+    torch.cuda.synchronize()
