@@ -614,6 +614,13 @@ def _check_tensor(name, t, shape, dtype):
             name, list(shape), dtype, list(t.shape), t.dtype))
 
 
+def _workspace_bytes(workspace):
+    """The bytes of a workspace that a caller gives."""
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return workspace.numel() * workspace.element_size()
+
+
 _torch = None
 
 
@@ -733,7 +740,7 @@ def _qpoint_f8(x, K, N, workspace, out, stream):
     else:
         _check_tensor("out", out, shape[:-1] + (N,), bf16)
     if workspace is not None:
-        return rows, workspace, workspace.numel() * workspace.element_size(), out
+        return rows, workspace, _workspace_bytes(workspace), out
     nbytes = (_lib or load()).quan_qpoint_f8_workspace_size(rows, K, N)
     if nbytes:
         workspace = _empty(stream, nbytes, torch.uint8, x.device)
@@ -870,7 +877,7 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
         if nbytes:
             workspace = _empty(stream, nbytes, torch.uint8, device)
     else:
-        nbytes = workspace.numel() * workspace.element_size()
+        nbytes = _workspace_bytes(workspace)
     _call(15, _JOIN_BWD(_addr(dy), _addr(dn), _addr(y), _addr(h), _addr(post), _addr(gate),
                         _addr(pre), rows, images, C, groups, dtype, alpha, eps, p, seed, offset,
                         _addr(counter), _addr(workspace), nbytes, _addr(dx), _addr(dh),

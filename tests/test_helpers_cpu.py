@@ -77,3 +77,44 @@ def test_a_gradient_that_belongs_to_nothing_reaches_the_checks(calls, extra):
     quan.residual_join_backward(dy, **args)
     (op, words), = calls
     assert op == 15 and 0x30000000 in words
+
+
+def letters(Cin, Cout, transposed=False, **kw):
+    n, k = (Cin // 4, Cout // 4) if transposed else (Cout // 4, Cin // 4)
+    q = dict(dict(shape=(4, n, (k + 15) // 16 * 16), dtype=torch.float8_e4m3fn, at=0x40000000),
+             **kw.get("q", {}))
+    s = dict(dict(shape=(4, -(-n // 128), -(-k // 128)), dtype=F32, at=0x50000000),
+             **kw.get("scale", {}))
+    return quan.F8Weights(Device(**q), Device(**s), Cin, Cout, transposed)
+
+
+def product(x=None, w=None, **kw):
+    return quan.qpointwise_f8(x or Device((1000, 64), BF16), w or letters(64, 128), **kw)
+
+
+def gradient(x=None, w=None, **kw):
+    return quan.qpointwise_f8_backward_data(x or Device((1000, 128), BF16),
+                                            w or letters(64, 128, True), **kw)
+
+
+def join_gradient(**kw):
+    t = [Device((1000, 64), F32, at=0x20000000 + (k << 24)) for k in range(4)]
+    v = Device((64,), F32, at=0x1000000)
+    return quan.residual_join_backward(*t, pre=v, **kw)
+
+
+BAD_WORKSPACES = [dict(cuda=-1), dict(contiguous=False)]
+
+
+@pytest.mark.parametrize("call", [product, gradient, join_gradient])
+def test_workspaces_are_looked_at(calls, call):
+    # the library gets an address and a byte count: one on the host faults, and a strided view is
+    # written past its elements
+    good = Device((1 << 20,), torch.uint8, at=0x60000000)
+    call(workspace=good)
+    (_, words), = calls
+    assert 0x60000000 in words and 1 << 20 in words
+    for bad in BAD_WORKSPACES:
+        with pytest.raises(ValueError, match="workspace must be a contiguous CUDA tensor"):
+            call(workspace=Device((1 << 20,), torch.uint8, **bad))
+    assert len(calls) == 1
