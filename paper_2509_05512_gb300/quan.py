@@ -727,13 +727,21 @@ def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
     return F8Weights(q, scale, 4 * Qin, 4 * Qout, bool(transpose))
 
 
-def _qpoint_f8(x, K, N, workspace, out, stream):
+def _qpoint_f8(x, q, scale, K, N, workspace, out, stream):
     """rows, workspace, its bytes and the output of one 8-bit product of K input and N output
-    channels."""
+    channels with the letters q, scale, which are looked at too."""
     torch = _torch or _get_torch()
     shape, bf16 = x.shape, torch.bfloat16
     if x.dtype is not bf16 or shape[-1] != K or not x.is_cuda or not x.is_contiguous():
         _check_tensor("x", x, shape[:-1] + (K,), bf16)
+    # (pitch K / 4 rounded up to 16, a scale for each 128 x 128)
+    blocks = ((N + 511) // 512, (K + 511) // 512)
+    if q.numel() != N * 16 * ((K + 63) // 64) or q.dtype is not torch.float8_e4m3fn or \
+            not q.is_cuda or not q.is_contiguous():
+        _check_tensor("w.q", q, (4, N // 4, 16 * ((K + 63) // 64)), torch.float8_e4m3fn)
+    if scale.numel() != 4 * blocks[0] * blocks[1] or scale.dtype is not torch.float32 or \
+            not scale.is_cuda or not scale.is_contiguous():
+        _check_tensor("w.scale", scale, (4,) + blocks, torch.float32)
     rows = x.numel() // K
     if out is None:
         out = _empty(stream, shape[:-1] + (N,), bf16, x.device)
@@ -762,7 +770,8 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
         for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
             if v is not None:
                 _check_tensor(name, v, (Cout,), f32)
-    rows, workspace, nbytes, out = _qpoint_f8(x, Cin, Cout, workspace, out, stream)
+    rows, workspace, nbytes, out = _qpoint_f8(x, q, wscale, Cin, Cout, workspace, out,
+                                              stream)
     _call(16, _QPOINT_F8(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), _addr(bias), _addr(scale),
                          _addr(shift), rows, Cin, Cout, act, _addr(workspace), nbytes,
                          out.data_ptr(), _stream(stream)))
@@ -775,7 +784,8 @@ def qpointwise_f8_backward_data(dy, w, *, workspace=None, out=None, stream=None)
     if not w.transposed:
         raise ValueError("w holds the forward letters: quantize_f8_weights(..., transpose=True)")
     q, wscale, Cin, Cout, _ = w
-    rows, workspace, nbytes, out = _qpoint_f8(dy, Cout, Cin, workspace, out, stream)
+    rows, workspace, nbytes, out = _qpoint_f8(dy, q, wscale, Cout, Cin, workspace, out,
+                                              stream)
     _call(17, _QPOINT_F8_BWD(dy.data_ptr(), q.data_ptr(), wscale.data_ptr(), rows, Cin, Cout,
                              _addr(workspace), nbytes, out.data_ptr(), _stream(stream)))
     return out

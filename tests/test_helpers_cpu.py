@@ -118,3 +118,38 @@ def test_workspaces_are_looked_at(calls, call):
         with pytest.raises(ValueError, match="workspace must be a contiguous CUDA tensor"):
             call(workspace=Device((1 << 20,), torch.uint8, **bad))
     assert len(calls) == 1
+
+
+BAD_LETTERS = [
+    ("q", dict(cuda=-1)), ("q", dict(contiguous=False)), ("q", dict(dtype=torch.uint8)),
+    ("q", dict(shape=(4, 32, 15))), ("q", dict(shape=(4, 16, 16))), ("q", dict(shape=(0,))),
+    ("scale", dict(cuda=-1)), ("scale", dict(contiguous=False)), ("scale", dict(dtype=BF16)),
+    ("scale", dict(shape=(3, 1, 1))),
+    ("scale", dict(shape=(0,))),
+]
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("part, bad", BAD_LETTERS)
+def test_letters_are_looked_at(calls, part, bad, transposed):
+    # F8Weights is a tuple that anyone can put together; the kernels read as much of it as the
+    # channel counts say
+    call = gradient if transposed else product
+    call(w=letters(64, 128, transposed))
+    with pytest.raises(ValueError, match="w.%s must be a contiguous CUDA tensor" % part):
+        call(w=letters(64, 128, transposed, **{part: bad}))
+    assert len(calls) == 1
+
+
+def test_channel_counts_that_the_letters_do_not_have(calls):
+    # all that fits 64 -> 128 but not the counts beside it
+    w = letters(64, 128)
+    with pytest.raises(ValueError, match="w.q"):
+        product(w=w._replace(Cout=256))
+    with pytest.raises(ValueError, match="w.q"):
+        product(x=Device((1000, 2048), BF16), w=w._replace(Cin=2048))
+    # 130 output channels a component need a second row of scales
+    w = letters(64, 520)
+    with pytest.raises(ValueError, match="w.scale"):
+        product(w=w._replace(scale=letters(64, 128).scale))
+    assert not calls
