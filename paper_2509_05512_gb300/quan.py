@@ -170,16 +170,20 @@ def _addr(t):
 _raw_stream = None
 
 
-def _stream(stream):
+def _stream(stream, dev=None):
+    """The handle of a stream; None: the current one of device `dev` (None: the current one)."""
     global _raw_stream
     if stream is None:
         # the handle of torch.cuda.current_stream() without building the Stream object
         # (0.4 us against 3)
-        import torch
-        if _raw_stream is None:
-            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-                lambda device: torch.cuda.current_stream(device).cuda_stream)
-        return _raw_stream(torch.cuda.current_device())
+        if dev is None or _raw_stream is None:
+            import torch
+            if _raw_stream is None:
+                _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+                    lambda device: torch.cuda.current_stream(device).cuda_stream)
+            if dev is None:
+                dev = torch.cuda.current_device()
+        return _raw_stream(dev)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -608,16 +612,31 @@ def _empty(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _check_tensor(name, t, shape, dtype):
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor %s of %s (got %s of %s)" % (
-            name, list(shape), dtype, list(t.shape), t.dtype))
+def _device(name, t):
+    """The device that a call's tensors have to be on: its first tensor's, which has to be the
+    current one, for that is where the kernels are launched."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("%s must be a contiguous CUDA tensor (got one on %s)" % (name, t.device))
+    current = (_torch or _get_torch()).cuda.current_device()
+    if dev != current:
+        raise ValueError("%s is on cuda:%d, but the current device is cuda:%d" % (name, dev,
+                                                                                 current))
+    return dev
 
 
-def _workspace_bytes(workspace):
+def _check_tensor(name, t, shape, dtype, dev):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or \
+            not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor %s of %s on cuda:%d (got %s of %s "
+                         "on %s)" % (name, list(shape), dtype, dev, list(t.shape), t.dtype,
+                                     t.device))
+
+
+def _workspace_bytes(workspace, dev):
     """The bytes of a workspace that a caller gives."""
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous CUDA tensor")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor on cuda:%d" % dev)
     return workspace.numel() * workspace.element_size()
 
 
@@ -641,9 +660,8 @@ def _dtype_of(name, t):
     raise ValueError("%s must be bfloat16 or float32 (got %s)" % (name, t.dtype))
 
 
-def _check_counter(counter):
-    if counter is not None:
-        _check_tensor("counter", counter.reshape(-1), (1,), _get_torch().int64)
+def _check_counter(counter, dev):
+    _check_tensor("counter", counter.reshape(-1), (1,), _get_torch().int64, dev)
 
 
 def dropout(x, p, seed, offset=0, *, counter=None, out=None, stream=None):
@@ -656,17 +674,18 @@ def dropout(x, p, seed, offset=0, *, counter=None, out=None, stream=None):
     torch = _torch or _get_torch()
     t, shape = x.dtype, x.shape
     dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else _dtype_of("x", x)
-    if not x.is_cuda or not x.is_contiguous():
-        _check_tensor("x", x, shape, t)
+    dev = _device("x", x)
+    if not x.is_contiguous():
+        _check_tensor("x", x, shape, t, dev)
     if counter is not None:
-        _check_counter(counter)
+        _check_counter(counter, dev)
     if out is not None:
-        _check_tensor("out", out, shape, t)
+        _check_tensor("out", out, shape, t, dev)
     else:
         out = _empty(stream, shape, t, x.device)
     _call(13, _DROPOUT(x.data_ptr(), x.numel(), dtype, p, seed, offset,
                        0 if counter is None else counter.data_ptr(), out.data_ptr(),
-                       _stream(stream)))
+                       _stream(stream, dev)))
     return out
 
 
@@ -715,8 +734,9 @@ def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
     Qout, kh, kw, Qin = wr.shape
     if kh != 1 or kw != 1:
         raise ValueError("the letters of a pointwise layer are [Cout/4, 1, 1, Cin/4]")
+    dev = _device("wr", wr)
     for name, w in (("wr", wr), ("wi", wi), ("wj", wj), ("wk", wk)):
-        _check_tensor(name, w, wr.shape, torch.bfloat16)
+        _check_tensor(name, w, wr.shape, torch.bfloat16, dev)
     n, k = (Qin, Qout) if transpose else (Qout, Qin)
     need = quan_f8_weights_bytes(4 * Qin, 4 * Qout, transpose)
     if need == 0:
@@ -727,28 +747,28 @@ def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
     return F8Weights(q, scale, 4 * Qin, 4 * Qout, bool(transpose))
 
 
-def _qpoint_f8(x, q, scale, K, N, workspace, out, stream):
+def _qpoint_f8(x, q, scale, K, N, workspace, out, stream, dev):
     """rows, workspace, its bytes and the output of one 8-bit product of K input and N output
     channels with the letters q, scale, which are looked at too."""
     torch = _torch or _get_torch()
     shape, bf16 = x.shape, torch.bfloat16
-    if x.dtype is not bf16 or shape[-1] != K or not x.is_cuda or not x.is_contiguous():
-        _check_tensor("x", x, shape[:-1] + (K,), bf16)
+    if x.dtype is not bf16 or shape[-1] != K or not x.is_contiguous():
+        _check_tensor("x", x, shape[:-1] + (K,), bf16, dev)
     # (pitch K / 4 rounded up to 16, a scale for each 128 x 128)
     blocks = ((N + 511) // 512, (K + 511) // 512)
     if q.numel() != N * 16 * ((K + 63) // 64) or q.dtype is not torch.float8_e4m3fn or \
-            not q.is_cuda or not q.is_contiguous():
-        _check_tensor("w.q", q, (4, N // 4, 16 * ((K + 63) // 64)), torch.float8_e4m3fn)
+            q.get_device() != dev or not q.is_contiguous():
+        _check_tensor("w.q", q, (4, N // 4, 16 * ((K + 63) // 64)), torch.float8_e4m3fn, dev)
     if scale.numel() != 4 * blocks[0] * blocks[1] or scale.dtype is not torch.float32 or \
-            not scale.is_cuda or not scale.is_contiguous():
-        _check_tensor("w.scale", scale, (4,) + blocks, torch.float32)
+            scale.get_device() != dev or not scale.is_contiguous():
+        _check_tensor("w.scale", scale, (4,) + blocks, torch.float32, dev)
     rows = x.numel() // K
     if out is None:
         out = _empty(stream, shape[:-1] + (N,), bf16, x.device)
     else:
-        _check_tensor("out", out, shape[:-1] + (N,), bf16)
+        _check_tensor("out", out, shape[:-1] + (N,), bf16, dev)
     if workspace is not None:
-        return rows, workspace, _workspace_bytes(workspace), out
+        return rows, workspace, _workspace_bytes(workspace, dev), out
     nbytes = (_lib or load()).quan_qpoint_f8_workspace_size(rows, K, N)
     if nbytes:
         workspace = _empty(stream, nbytes, torch.uint8, x.device)
@@ -765,16 +785,17 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
     if w.transposed:
         raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
     q, wscale, Cin, Cout, _ = w
+    dev = _device("x", x)
     if bias is not None or scale is not None or shift is not None:
         f32 = (_torch or _get_torch()).float32
         for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
             if v is not None:
-                _check_tensor(name, v, (Cout,), f32)
+                _check_tensor(name, v, (Cout,), f32, dev)
     rows, workspace, nbytes, out = _qpoint_f8(x, q, wscale, Cin, Cout, workspace, out,
-                                              stream)
+                                              stream, dev)
     _call(16, _QPOINT_F8(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), _addr(bias), _addr(scale),
                          _addr(shift), rows, Cin, Cout, act, _addr(workspace), nbytes,
-                         out.data_ptr(), _stream(stream)))
+                         out.data_ptr(), _stream(stream, dev)))
     return out
 
 
@@ -784,14 +805,15 @@ def qpointwise_f8_backward_data(dy, w, *, workspace=None, out=None, stream=None)
     if not w.transposed:
         raise ValueError("w holds the forward letters: quantize_f8_weights(..., transpose=True)")
     q, wscale, Cin, Cout, _ = w
+    dev = _device("dy", dy)
     rows, workspace, nbytes, out = _qpoint_f8(dy, q, wscale, Cout, Cin, workspace, out,
-                                              stream)
+                                              stream, dev)
     _call(17, _QPOINT_F8_BWD(dy.data_ptr(), q.data_ptr(), wscale.data_ptr(), rows, Cin, Cout,
-                             _addr(workspace), nbytes, out.data_ptr(), _stream(stream)))
+                             _addr(workspace), nbytes, out.data_ptr(), _stream(stream, dev)))
     return out
 
 
-def _join_shape(like, shape, post, gate, pre):
+def _join_shape(like, shape, post, gate, pre, dev):
     """(rows, C, images) of a join's tensors, its vectors checked."""
     f32 = (_torch or _get_torch()).float32
     C = shape[-1]
@@ -801,15 +823,15 @@ def _join_shape(like, shape, post, gate, pre):
         if gate.dim() != 1:
             images = shape[0]
             want = (images, C)
-        if gate.dtype is not f32 or gate.shape != want or not gate.is_cuda or \
+        if gate.dtype is not f32 or gate.shape != want or gate.get_device() != dev or \
                 not gate.is_contiguous():
-            _check_tensor("gate", gate, want, f32)
-    if post is not None and (post.dtype is not f32 or post.shape != vec or not post.is_cuda or
-                             not post.is_contiguous()):
-        _check_tensor("post", post, vec, f32)
-    if pre is not None and (pre.dtype is not f32 or pre.shape != vec or not pre.is_cuda or
-                            not pre.is_contiguous()):
-        _check_tensor("pre", pre, vec, f32)
+            _check_tensor("gate", gate, want, f32, dev)
+    if post is not None and (post.dtype is not f32 or post.shape != vec or
+                             post.get_device() != dev or not post.is_contiguous()):
+        _check_tensor("post", post, vec, f32, dev)
+    if pre is not None and (pre.dtype is not f32 or pre.shape != vec or
+                            pre.get_device() != dev or not pre.is_contiguous()):
+        _check_tensor("pre", pre, vec, f32, dev)
     return like.numel() // C if C else 0, C, max(images, 1)
 
 
@@ -824,27 +846,28 @@ def residual_join(x, h=None, *, post=None, gate=None, pre=None, alpha=1.0, group
     torch = _torch or _get_torch()
     t, shape = x.dtype, x.shape
     dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else _dtype_of("x", x)
-    if not x.is_cuda or not x.is_contiguous():
-        _check_tensor("x", x, shape, t)
-    rows, C, images = _join_shape(x, shape, post, gate, pre)
+    dev = _device("x", x)
+    if not x.is_contiguous():
+        _check_tensor("x", x, shape, t, dev)
+    rows, C, images = _join_shape(x, shape, post, gate, pre, dev)
     if counter is not None:
-        _check_counter(counter)
+        _check_counter(counter, dev)
     if h is not None:
-        if h.dtype is not t or h.shape != shape or not h.is_cuda or not h.is_contiguous():
-            _check_tensor("h", h, shape, t)
+        if h.dtype is not t or h.shape != shape or h.get_device() != dev or not h.is_contiguous():
+            _check_tensor("h", h, shape, t, dev)
         if y is None:
             y = _empty(stream, shape, t, x.device)
         else:
-            _check_tensor("y", y, shape, t)
+            _check_tensor("y", y, shape, t, dev)
     elif y is not None:
         raise ValueError("y is given without h")
     if n is not None:
-        _check_tensor("n", n, shape, t)
+        _check_tensor("n", n, shape, t, dev)
     elif pre is not None:
         n = _empty(stream, shape, t, x.device)
     _call(14, _JOIN_FWD(x.data_ptr(), _addr(h), _addr(post), _addr(gate), _addr(pre), rows, images,
                         C, groups, dtype, alpha, eps, p, seed, offset, _addr(counter), _addr(y),
-                        _addr(n), _stream(stream)))
+                        _addr(n), _stream(stream, dev)))
     return y, n
 
 
@@ -862,13 +885,14 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
     t, shape, device = like.dtype, like.shape, like.device
     dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else \
         _dtype_of("dy" if dy is not None else "dn", like)
-    rows, C, images = _join_shape(like, shape, post, gate, pre)
+    dev = _device("dy" if dy is not None else "dn", like)
+    rows, C, images = _join_shape(like, shape, post, gate, pre, dev)
     if counter is not None:
-        _check_counter(counter)
+        _check_counter(counter, dev)
     for name, v in (("dy", dy), ("dn", dn), ("y", y), ("h", h), ("dx", dx), ("dh", dh)):
-        if v is not None and (v.dtype is not t or v.shape != shape or not v.is_cuda or
+        if v is not None and (v.dtype is not t or v.shape != shape or v.get_device() != dev or
                               not v.is_contiguous()):
-            _check_tensor(name, v, shape, t)
+            _check_tensor(name, v, shape, t, dev)
     if pre is None:
         y = None
         if h is None and post is None and gate is None and dn is None and dx is None and \
@@ -887,9 +911,9 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
         if nbytes:
             workspace = _empty(stream, nbytes, torch.uint8, device)
     else:
-        nbytes = _workspace_bytes(workspace)
+        nbytes = _workspace_bytes(workspace, dev)
     _call(15, _JOIN_BWD(_addr(dy), _addr(dn), _addr(y), _addr(h), _addr(post), _addr(gate),
                         _addr(pre), rows, images, C, groups, dtype, alpha, eps, p, seed, offset,
                         _addr(counter), _addr(workspace), nbytes, _addr(dx), _addr(dh),
-                        _addr(dpost), _addr(dgate), _addr(dpre), _stream(stream)))
+                        _addr(dpost), _addr(dgate), _addr(dpre), _stream(stream, dev)))
     return (dy if dx is None else dx, dh, dpost, dgate, dpre)

@@ -153,3 +153,42 @@ def test_channel_counts_that_the_letters_do_not_have(calls):
     with pytest.raises(ValueError, match="w.scale"):
         product(w=w._replace(scale=letters(64, 128).scale))
     assert not calls
+
+
+def test_tensors_of_another_device_are_refused(calls, monkeypatch):
+    # a launch goes to the current device, where another one's memory need not be mapped
+    here = dict(x=Device((1000, 64), BF16), w=letters(64, 128))
+    there = Device((128,), F32, cuda=1)
+    with pytest.raises(ValueError, match="bias"):
+        product(**here, bias=there)
+    with pytest.raises(ValueError, match="w.q"):
+        product(w=letters(64, 128, q=dict(cuda=1)))
+    with pytest.raises(ValueError, match="w.scale"):
+        gradient(w=letters(64, 128, True, scale=dict(cuda=1)))
+    with pytest.raises(ValueError, match="workspace"):
+        product(**here, workspace=Device((1 << 20,), torch.uint8, cuda=1))
+    with pytest.raises(ValueError, match="out"):
+        product(**here, out=Device((1000, 128), BF16, cuda=1))
+    x, v = Device((1000, 64), F32), Device((64,), F32)
+    far = Device((1000, 64), F32, cuda=1)
+    for bad in (dict(h=far), dict(h=x, y=far), dict(pre=Device((64,), F32, cuda=1)),
+                dict(pre=v, n=far), dict(h=x, post=Device((64,), F32, cuda=1)),
+                dict(h=x, gate=Device((64,), F32, cuda=1)),
+                dict(h=x, counter=Device((1,), torch.int64, cuda=1))):
+        with pytest.raises(ValueError, match="must be a contiguous CUDA tensor"):
+            quan.residual_join(x, **bad)
+    for bad in (dict(dn=far), dict(y=far), dict(h=far), dict(dx=far), dict(h=x, dh=far)):
+        with pytest.raises(ValueError, match="must be a contiguous CUDA tensor"):
+            quan.residual_join_backward(x, **dict(dict(dn=x, y=x, pre=v), **bad))
+    with pytest.raises(ValueError, match="out"):
+        quan.dropout(x, 0.5, 1, out=far)
+    w = [Device((32, 1, 1, 16), BF16, cuda=int(k == 2)) for k in range(4)]
+    with pytest.raises(ValueError, match="wj"):
+        quan.quantize_f8_weights(*w)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: product(**here), lambda: gradient(), lambda: quan.residual_join(x, pre=v),
+                 lambda: quan.residual_join_backward(x, x, x, pre=v),
+                 lambda: quan.dropout(x, 0.5, 1), lambda: quan.quantize_f8_weights(*w)):
+        with pytest.raises(ValueError, match="current device is cuda:1"):
+            call()
+    assert not calls
