@@ -10,6 +10,10 @@
 //
 // Layouts: q_x [row][4][Kp] and q_w [4][Nq][Kp] with Kp = Kq rounded up to 16, zeros in the
 // padding; s_x [4][blocks][rows rounded up to 128], s_w [4][ceil(Nq / 128)][blocks].
+//
+// Inputs are read with plain loads only: these grids start while the one before them may still
+// write what they read, and the read-only path may be used only for what nothing writes while
+// the kernel runs.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -191,8 +195,8 @@ __device__ __forceinline__ float f8_act(float z, int act) {
 __device__ __forceinline__ void f8_store(const F8Params& p, long long row, int co, int n,
                                          float acc) {
     const int c = co * p.Nq + n;
-    if (p.ep.bias) acc += __ldg(p.ep.bias + c);
-    if (p.ep.scale) acc = fmaf(__ldg(p.ep.scale + c), acc, __ldg(p.ep.shift + c));
+    if (p.ep.bias) acc += p.ep.bias[c];
+    if (p.ep.scale) acc = fmaf(p.ep.scale[c], acc, p.ep.shift[c]);
     p.out[row * (4LL * p.Nq) + c] = __float2bfloat16_rn(f8_act(acc, p.act));
 }
 
@@ -243,12 +247,12 @@ __global__ void __launch_bounds__(256) qpoint_rows_kernel(const F8Params p) {
             const int kb = k0 / F8_BLOCK + b, k = kb * F8_BLOCK + lane * 4;
 #pragma unroll
             for (int L = 0; L < 4; ++L) {
-                q[b][L] = k < p.Kp ? __ldg(reinterpret_cast<const uint32_t*>(
-                                         p.wq + (static_cast<long long>(L) * p.Nq + n) * p.Kp + k))
+                q[b][L] = k < p.Kp ? *reinterpret_cast<const uint32_t*>(
+                                         p.wq + (static_cast<long long>(L) * p.Nq + n) * p.Kp + k)
                                    : 0u;
                 sw[b][L] = kb < p.kblk
-                               ? __ldg(p.ws + (static_cast<long long>(L) * p.nblk + n / F8_BLOCK) *
-                                                  p.kblk + kb)
+                               ? p.ws[(static_cast<long long>(L) * p.nblk + n / F8_BLOCK) *
+                                          p.kblk + kb]
                                : 0.0f;
             }
         }

@@ -418,8 +418,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                 float w[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    x[k] = __ldg(reinterpret_cast<const float4*>(xs + k * p.kblk * p.pitch));
-                    w[k] = __ldg(ws + static_cast<long long>(k) * p.nblk * p.kblk);
+                    x[k] = *reinterpret_cast<const float4*>(xs + k * p.kblk * p.pitch);
+                    w[k] = ws[static_cast<long long>(k) * p.nblk * p.kblk];
                 }
                 ok = __all_sync(0xffffffffu,
                                 wait(empty_s + 8u * ss, phase ^ 1u, STATUS_TIMEOUT_PRODUCER));
@@ -466,10 +466,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                     const int n = n0 + (j & (BNQ - 1));
                     const int c = (co0 + j / BNQ) * p.Nq + n;
                     const bool col = n < p.Nq;
-                    const float sc = p.ep.scale && col ? __ldg(p.ep.scale + c) : 1.0f;
-                    const float b = p.ep.bias && col ? __ldg(p.ep.bias + c) : 0.0f;
+                    const float sc = p.ep.scale && col ? p.ep.scale[c] : 1.0f;
+                    const float b = p.ep.bias && col ? p.ep.bias[c] : 0.0f;
                     scale[j] = sc;
-                    shift[j] = fmaf(sc, b, p.ep.scale && col ? __ldg(p.ep.shift + c) : 0.0f);
+                    shift[j] = fmaf(sc, b, p.ep.scale && col ? p.ep.shift[c] : 0.0f);
                 }
                 __syncwarp();
             }

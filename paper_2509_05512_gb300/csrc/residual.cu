@@ -192,7 +192,8 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int tps, float (&both)[
     }
 }
 
-// A thread's share of a per-channel vector (1 without one).
+// A thread's share of a per-channel vector (1 without one).  A plain load: the grid before this
+// one may be its writer, and the read-only path is for what nothing writes while the kernel runs.
 template <int NC>
 __device__ __forceinline__ void load_columns(const float* v, const JoinParams& p, const Place& q,
                                              float scale, float (&out)[NC][8]) {
@@ -201,7 +202,7 @@ __device__ __forceinline__ void load_columns(const float* v, const JoinParams& p
         const int col = (q.ts + c * p.tps) * 8;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            out[c][j] = (v && col + j < p.S) ? scale * __ldg(v + q.seg * p.S + col + j) : scale;
+            out[c][j] = (v && col + j < p.S) ? scale * v[q.seg * p.S + col + j] : scale;
     }
 }
 
