@@ -305,6 +305,11 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
+    // what an abort has to wait for: the stages that were filled and the parities of their last
+    // fills, and whether this thread issued an MMA
+    uint32_t filled_a = 0, parity_a = 0, filled_b = 0, parity_b = 0;
+    bool issued = false;
+
     if (warp < F8_EPI_WARP0)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F8_REGS_ISSUE));
     if (warp == 0) {
@@ -312,7 +317,6 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         if (lane == 0) {
             griddep_wait();  // the quantised rows are complete
             const uint64_t pol_x = l2_policy_evict_normal(), pol_w = l2_policy_evict_last();
-            uint32_t filled_a = 0, parity_a = 0, filled_b = 0, parity_b = 0;
             uint32_t phase_a = 0, phase_b = 0;
             int sa = 0, sb = 0;
             bool ok = true;
@@ -343,17 +347,12 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                     }
                 }
             }
-            if (!ok || *abort_flag) {
-                tc::drain_fills(full_a, C::A_STAGES, filled_a, parity_a, limit);
-                tc::drain_fills(full_b, C::B_STAGES, filled_b, parity_b, limit);
-            }
         }
     } else if (warp <= 2) {
         // ------------------------------------------------------------ MMA issuers
         if (lane == 0) {
             const int buf = warp - 1;  // this issuer's TMEM buffer, and its partials' parity
             bool ok = true;
-            int issued = 0;
             if (p.inject_stall) {
                 // Failure injection: wait on a barrier nothing arrives on.
                 wait(drain_bar, 0, STATUS_TIMEOUT_MMA);
@@ -383,23 +382,12 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                         for (int kk = 0; kk < steps; ++kk)  // 32 channels: 32 bytes into a row
                             umma_f8(d, a_lo + 2 * kk, b_lo + 2 * kk, C::DESC_HI, C::IDESC,
                                     kk != 0 ? 1u : 0u);
-                        ++issued;
+                        issued = true;
                         umma_commit(done_a + 8u * sa);
                         if (half == 1) umma_commit(empty_b + 8u * sb);
                         if ((sa += 2) >= C::A_STAGES) sa = buf, phase_a ^= 1u;
                     }
                     if (++sb == C::B_STAGES) sb = 0, phase_b ^= 1u;
-                }
-            }
-            if (!ok && issued > 0) {
-                // let the issued MMAs finish before TMEM is released
-                umma_commit(drain_bar + 8u * buf);
-                const uint64_t t1 = global_timer_ns();
-                while (!mbar_try_wait(drain_bar + 8u * buf, 0u)) {
-                    if (global_timer_ns() - t1 > limit) {
-                        atomicOr(&g_status, STATUS_TIMEOUT_DRAIN);
-                        break;
-                    }
                 }
             }
         }
@@ -528,6 +516,20 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
 
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) {
+        // Behind the barrier, for a role may end before another gives up: no copy may land in
+        // shared memory that is another CTA's by then, and no MMA write TMEM that was released.
+        if (threadIdx.x == 0) {
+            tc::drain_fills(full_a, C::A_STAGES, filled_a, parity_a, limit);
+            tc::drain_fills(full_b, C::B_STAGES, filled_b, parity_b, limit);
+        }
+        if (issued) {
+            const uint32_t bar = drain_bar + 8u * (warp - 1);
+            umma_commit(bar);
+            tc::drain_fills(bar, 1, 1u, 0u, limit);
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();

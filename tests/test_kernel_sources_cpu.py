@@ -22,3 +22,17 @@ def test_no_load_through_the_read_only_path(name):
     # inside the kernel.  __ldg and ld.global.nc promise memory that nothing writes while the kernel
     # runs, and such a load may be moved in front of the wait.
     assert not re.search(r"__ldg\b|ld\.global\.nc|const\s+\w+\s*\*\s*__restrict__", source(name))
+
+
+def test_the_8_bit_product_drains_after_its_roles():
+    # A role that has nothing left to do may leave before another one gives up, with its copies or
+    # products still under way.  So they are waited for behind the barrier that ends the roles, where
+    # the abort flag is final, and in front of the release of TMEM.
+    text = source("qpoint_f8_tc.cuh")
+    roles_end = text.index("__syncthreads();", text.index("setmaxnreg.inc"))
+    flag = text.index("if (*abort_flag)", roles_end)
+    release = text.index("tmem_dealloc", flag)
+    drains = [m.start() for m in re.finditer(r"drain_fills\(|umma_commit\(drain_bar", text)]
+    assert len(drains) == 3 and all(flag < d < release for d in drains)
+    # nobody releases anything before the drains have ended
+    assert "__syncthreads();" in text[max(drains):release]
