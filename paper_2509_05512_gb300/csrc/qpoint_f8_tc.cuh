@@ -450,14 +450,22 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
             const int n0 = nt * BNQ;
             if constexpr (AFFINE) {
                 __syncwarp();  // the previous tile's reads
-                for (int j = lane; j < 2 * BNQ; j += 32) {
-                    const int n = n0 + (j & (BNQ - 1));
+                // (every load before the first store, which the compiler has to take for one to
+                // these vectors)
+                float sc[2 * BNQ / 32], b[2 * BNQ / 32], sh[2 * BNQ / 32];
+#pragma unroll
+                for (int k = 0; k < 2 * BNQ / 32; ++k) {
+                    const int j = lane + 32 * k, n = n0 + (j & (BNQ - 1));
                     const int c = (co0 + j / BNQ) * p.Nq + n;
                     const bool col = n < p.Nq;
-                    const float sc = p.ep.scale && col ? p.ep.scale[c] : 1.0f;
-                    const float b = p.ep.bias && col ? p.ep.bias[c] : 0.0f;
-                    scale[j] = sc;
-                    shift[j] = fmaf(sc, b, p.ep.scale && col ? p.ep.shift[c] : 0.0f);
+                    sc[k] = p.ep.scale && col ? p.ep.scale[c] : 1.0f;
+                    sh[k] = p.ep.scale && col ? p.ep.shift[c] : 0.0f;
+                    b[k] = p.ep.bias && col ? p.ep.bias[c] : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 2 * BNQ / 32; ++k) {
+                    scale[lane + 32 * k] = sc[k];
+                    shift[lane + 32 * k] = fmaf(sc[k], b[k], sh[k]);
                 }
                 __syncwarp();
             }

@@ -751,7 +751,7 @@ def _qpoint_f8(x, q, scale, K, N, workspace, out, stream, dev):
     """rows, workspace, its bytes and the output of one 8-bit product of K input and N output
     channels with the letters q, scale, which are looked at too."""
     torch = _torch or _get_torch()
-    shape, bf16 = x.shape, torch.bfloat16
+    shape, bf16 = tuple(x.shape), torch.bfloat16  # (torch.empty takes a tuple 1 us faster)
     if x.dtype is not bf16 or shape[-1] != K or not x.is_contiguous():
         _check_tensor("x", x, shape[:-1] + (K,), bf16, dev)
     # (pitch K / 4 rounded up to 16, a scale for each 128 x 128)
@@ -763,10 +763,11 @@ def _qpoint_f8(x, q, scale, K, N, workspace, out, stream, dev):
             scale.get_device() != dev or not scale.is_contiguous():
         _check_tensor("w.scale", scale, (4,) + blocks, torch.float32, dev)
     rows = x.numel() // K
+    shape = shape[:-1] + (N,)
     if out is None:
-        out = _empty(stream, shape[:-1] + (N,), bf16, x.device)
+        out = _empty(stream, shape, bf16, x.device)
     else:
-        _check_tensor("out", out, shape[:-1] + (N,), bf16, dev)
+        _check_tensor("out", out, shape, bf16, dev)
     if workspace is not None:
         return rows, workspace, _workspace_bytes(workspace, dev), out
     nbytes = (_lib or load()).quan_qpoint_f8_workspace_size(rows, K, N)
@@ -786,16 +787,17 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
         raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
     q, wscale, Cin, Cout, _ = w
     dev = _device("x", x)
+    vectors = (0, 0, 0)
     if bias is not None or scale is not None or shift is not None:
         f32 = (_torch or _get_torch()).float32
         for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
             if v is not None:
                 _check_tensor(name, v, (Cout,), f32, dev)
+        vectors = (_addr(bias), _addr(scale), _addr(shift))
     rows, workspace, nbytes, out = _qpoint_f8(x, q, wscale, Cin, Cout, workspace, out,
                                               stream, dev)
-    _call(16, _QPOINT_F8(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), _addr(bias), _addr(scale),
-                         _addr(shift), rows, Cin, Cout, act, _addr(workspace), nbytes,
-                         out.data_ptr(), _stream(stream, dev)))
+    _call(16, _QPOINT_F8(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), *vectors, rows, Cin, Cout,
+                         act, _addr(workspace), nbytes, out.data_ptr(), _stream(stream, dev)))
     return out
 
 
