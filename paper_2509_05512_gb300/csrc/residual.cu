@@ -194,6 +194,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int tps, float (&both)[
 
 // A thread's share of a per-channel vector (1 without one).  A plain load: the grid before this
 // one may be its writer, and the read-only path is for what nothing writes while the kernel runs.
+// (32 x 56 x 56 x 256 bf16: 38.9 and 64.7 us; 39.3 and 65.3 where the compiler places the loads.)
 template <int NC>
 __device__ __forceinline__ void load_columns(const float* v, const JoinParams& p, const Place& q,
                                              float scale, float (&out)[NC][8]) {
@@ -202,7 +203,8 @@ __device__ __forceinline__ void load_columns(const float* v, const JoinParams& p
         const int col = (q.ts + c * p.tps) * 8;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            out[c][j] = (v && col + j < p.S) ? scale * v[q.seg * p.S + col + j] : scale;
+            out[c][j] = (v && col + j < p.S) ? scale * ld_global_f32(v + q.seg * p.S + col + j)
+                                             : scale;
     }
 }
 
