@@ -2,6 +2,7 @@
 // hot entry point packed as 64-bit words.  A ctypes call converts every argument by itself,
 // about 6 us for the 20 of a convolution; packing them with one struct.pack and passing one
 // pointer takes about 2.  Not part of the public header.
+#include <climits>
 #include <cstring>
 
 #include "quan.h"
@@ -19,7 +20,12 @@ struct Args {
     void* ptr() { return reinterpret_cast<void*>(next()); }
     float* f32() { return static_cast<float*>(ptr()); }
     quan_stream_t stream() { return static_cast<quan_stream_t>(ptr()); }
-    int num() { return static_cast<int>(next()); }
+    // A size past an int becomes the least int, which every entry refuses as it does any negative
+    // size; cut to 32 bits it could pass for another one.
+    int num() {
+        const long long v = next();
+        return v > INT_MAX || v < INT_MIN ? INT_MIN : static_cast<int>(v);
+    }
     float real() {
         double d;
         memcpy(&d, a + i++, sizeof(d));

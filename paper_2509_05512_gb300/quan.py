@@ -738,6 +738,8 @@ def quantize_f8_weights(wr, wi, wj, wk, *, transpose=False, stream=None):
     for name, w in (("wr", wr), ("wi", wi), ("wj", wj), ("wk", wk)):
         _check_tensor(name, w, wr.shape, torch.bfloat16, dev)
     n, k = (Qin, Qout) if transpose else (Qout, Qin)
+    if 4 * max(n, k) >= 1 << 31:  # (past the arguments' int; the library's own limit is lower)
+        raise ValueError("a layer of %d -> %d channels is too large" % (4 * Qin, 4 * Qout))
     need = quan_f8_weights_bytes(4 * Qin, 4 * Qout, transpose)
     if need == 0:
         raise ValueError("a layer has at least four input and output channels")

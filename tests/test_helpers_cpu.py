@@ -192,3 +192,34 @@ def test_tensors_of_another_device_are_refused(calls, monkeypatch):
         with pytest.raises(ValueError, match="current device is cuda:1"):
             call()
     assert not calls
+
+
+def test_sizes_past_32_bits_are_not_cut():
+    # the packed entry takes 64-bit words: a size that the C function's int does not hold is refused,
+    # not taken modulo 2^32.  Without rows nothing would be launched.
+    build.build_library()
+    quan.load()
+    for C in ((1 << 32) + 64, (1 << 32), -(1 << 32) + 64, 1 << 62):
+        with pytest.raises(quan.QuanError):
+            quan.quan_residual_join_fwd(None, None, None, None, None, 0, C, 4, 1, 0, 1.0, 1e-5, 0.0,
+                                        1, 0, None, None, None, 0)
+        with pytest.raises(quan.QuanError):
+            quan.quan_residual_join_bwd(None, None, None, None, None, None, None, 0, C, 4, 1, 0,
+                                        1.0, 1e-5, 0.0, 1, 0, None, None, 0, None, None, None, None,
+                                        None, 0)
+        with pytest.raises(quan.QuanError):
+            quan.quan_qpoint_f8_fwd(None, None, None, None, None, None, 0, C, 64, 0, None, 0, None,
+                                    0)
+        with pytest.raises(quan.QuanError):
+            quan.quan_qpoint_f8_bwd_data(None, None, None, 0, 64, C, None, 0, None, 0)
+
+
+def test_letters_past_32_bits_are_refused(calls, monkeypatch):
+    made = []
+    monkeypatch.setattr(quan, "quan_f8_weights", lambda *a: made.append(a))
+    w = [Device((16, 1, 1, (1 << 30) + 16), BF16) for _ in range(4)]  # Cin = 2^32 + 64
+    for transpose in (False, True):
+        with pytest.raises(ValueError, match="channels"):
+            quan.quantize_f8_weights(*w, transpose=transpose)
+    quan.quantize_f8_weights(*[Device((16, 1, 1, 16), BF16) for _ in range(4)])
+    assert len(made) == 1
