@@ -164,7 +164,14 @@ def _addr(t):
     """_ptr as an integer (None: 0)."""
     if t is None:
         return 0
-    return t if t.__class__ is int else t.data_ptr()
+    if t.__class__ is int:
+        return t
+    try:
+        return t.data_ptr()
+    except AttributeError:
+        if isinstance(t, int):
+            return t
+        raise
 
 
 _raw_stream = None

@@ -223,3 +223,14 @@ def test_letters_past_32_bits_are_refused(calls, monkeypatch):
             quan.quantize_f8_weights(*w, transpose=transpose)
     quan.quantize_f8_weights(*[Device((16, 1, 1, 16), BF16) for _ in range(4)])
     assert len(made) == 1
+
+
+def test_addresses_of_integer_types():
+    # what the raw functions take for a tensor: an address of int or a type derived from it
+    class Address(int):
+        pass
+
+    assert quan._addr(Address(0x1000)) == 0x1000 and quan._addr(0x1000) == 0x1000
+    assert quan._addr(Device((1,), F32, at=0x2000)) == 0x2000 and quan._addr(None) == 0
+    with pytest.raises(AttributeError):
+        quan._addr("x")
