@@ -78,7 +78,7 @@ struct F8Cfg {
     static constexpr int SCALES = S_STAGES * S_STAGE;
     // full and done (A), full and empty (B, factors), acce (2 buffers), drain (2 issuers)
     static constexpr int NUM_BARS = 2 * (A_STAGES + B_STAGES + S_STAGES) + 2 + 2;
-    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + OUT + VEC + NUM_BARS * 8 + 16;
+    static constexpr int SMEM_BYTES = 1024 + RING + SCALES + OUT + VEC + NUM_BARS * 8 + 32;
     static constexpr uint32_t DESC_HI = tc::desc_hi(8 * 128, tc::desc_layout(128));
     static constexpr uint32_t TMEM_COLS = 2 * 4 * BNQ;  // 512, 256 or 128
     // kind::f8f6f4: e4m3 A and B (format 0), fp32 D, both K-major
@@ -259,6 +259,9 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::SCALES + C::VEC + C::OUT);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    // what an abort has to wait for, written by the roles as they end: the stages of rows that were
+    // filled and the parities of their last fills, the same of letters; whether MMAs were issued
+    volatile uint32_t* left = tmem_slot + 2;  // [4], [2]
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t full_a = bar0, done_a = full_a + 8u * C::A_STAGES;
     const uint32_t full_b = done_a + 8u * C::A_STAGES, empty_b = full_b + 8u * C::B_STAGES;
@@ -305,11 +308,6 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
-    // what an abort has to wait for: the stages that were filled and the parities of their last
-    // fills, and whether this thread issued an MMA
-    uint32_t filled_a = 0, parity_a = 0, filled_b = 0, parity_b = 0;
-    bool issued = false;
-
     if (warp < F8_EPI_WARP0)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F8_REGS_ISSUE));
     if (warp == 0) {
@@ -317,6 +315,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         if (lane == 0) {
             griddep_wait();  // the quantised rows are complete
             const uint64_t pol_x = l2_policy_evict_normal(), pol_w = l2_policy_evict_last();
+            uint32_t filled_a = 0, parity_a = 0, filled_b = 0, parity_b = 0;
             uint32_t phase_a = 0, phase_b = 0;
             int sa = 0, sb = 0;
             bool ok = true;
@@ -347,12 +346,13 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                     }
                 }
             }
+            left[0] = filled_a, left[1] = parity_a, left[2] = filled_b, left[3] = parity_b;
         }
     } else if (warp <= 2) {
         // ------------------------------------------------------------ MMA issuers
         if (lane == 0) {
             const int buf = warp - 1;  // this issuer's TMEM buffer, and its partials' parity
-            bool ok = true;
+            bool ok = true, issued = false;
             if (p.inject_stall) {
                 // Failure injection: wait on a barrier nothing arrives on.
                 wait(drain_bar, 0, STATUS_TIMEOUT_MMA);
@@ -390,6 +390,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
                     if (++sb == C::B_STAGES) sb = 0, phase_b ^= 1u;
                 }
             }
+            left[4 + buf] = issued;
         }
     } else if (warp == 3) {
         // ------------------------------------------------------------ factors
@@ -528,10 +529,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1)
         // Behind the barrier, for a role may end before another gives up: no copy may land in
         // shared memory that is another CTA's by then, and no MMA write TMEM that was released.
         if (threadIdx.x == 0) {
-            tc::drain_fills(full_a, C::A_STAGES, filled_a, parity_a, limit);
-            tc::drain_fills(full_b, C::B_STAGES, filled_b, parity_b, limit);
+            tc::drain_fills(full_a, C::A_STAGES, left[0], left[1], limit);
+            tc::drain_fills(full_b, C::B_STAGES, left[2], left[3], limit);
         }
-        if (issued) {
+        if ((warp == 1 || warp == 2) && lane == 0 && left[3 + warp]) {
             const uint32_t bar = drain_bar + 8u * (warp - 1);
             umma_commit(bar);
             tc::drain_fills(bar, 1, 1u, 0u, limit);
