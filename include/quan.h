@@ -507,7 +507,8 @@ quan_status_t quan_residual_join_bwd(const void* dy, const void* dn, const void*
  * channels of a letter, and 128 channels of one component of one pixel of the input (the last
  * ones of a row or column are smaller).  Products are exact, sums fp32; the output is bf16.  A
  * block that holds an infinity or a NaN has scale NaN: every output computed from it is NaN.
- * Where the scales of a product of blocks multiply to more than fp32 holds (2^128), so do outputs.
+ * Where the scales of a product of blocks multiply to more than fp32 holds (2^128), so do outputs;
+ * where they multiply to less than 2^-149, that product may count as 0.
  *
  * quan_f8_weights quantises the letters once, for quan_qpoint_f8_fwd (transpose 0) or
  * quan_qpoint_f8_bwd_data (transpose 1; the same 8-bit values and scales, the letters' axes

@@ -21,10 +21,11 @@
 // registers for all of its block's rows; blocks leave one row of partial sums each, added in a fixed
 // order by a second launch, so that repeated calls give the same bits.
 //
-// Measured on 32 x 56 x 56 x 256 bf16 with dropout: forward 38.6 us, 5.3 TB/s, bound by HBM with the
+// Measured on 32 x 56 x 56 x 256 bf16 with dropout: forward 38.2 us, 5.4 TB/s, bound by HBM with the
 // generator's integer work beside it (two rows under way a thread: 55 without the row ahead);
-// gradients 64 us, 4.8 TB/s, bound by issue, about 470 instructions for eight elements of four
-// tensors (the row ahead: 85 without; three blocks an SM spill: 89).
+// gradients 64 us, 4.8 TB/s, at no single limit: about 470 instructions for eight elements of four
+// tensors take two thirds of the issue slots, HBM is at half, and 16 warps an SM leave fixed
+// latencies uncovered (the row ahead: 85 without; three blocks an SM spill: 89).
 #include <cuda_bf16.h>
 
 #include <atomic>
