@@ -553,6 +553,42 @@ quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const floa
                                       long long rows, int Cin, int Cout, void* workspace,
                                       size_t workspace_bytes, void* dx, quan_stream_t stream);
 
+/*
+ * Distillation from a teacher's top logits (the loss that trains one classifier from another): a row
+ * has `classes` logits z and `top` slots, each a class and the teacher's logit t of it.  With
+ * p = softmax(t / T) over the row's slots and q = softmax(z / T) over its classes,
+ *   loss = T^2 sum_k p_k (ln p_k - ln q_(class k))          (T: temperature)
+ *   dz_v = g T (q_v - sum of p_k over the slots of class v),  g = scale * dloss
+ * A slot whose class is outside [0, classes) or whose t is -infinity is empty; a row of empty slots
+ * has loss 0 and gradient 0, and a row with g = 0 gradient 0, whatever their logits are.  A class may
+ * stand in several slots.  A logit of -infinity is a class that cannot be (q = 0; a slot with p > 0 of
+ * it makes the loss infinite).  +infinity, NaN, or no finite logit in a row that counts give NaN.
+ * Arithmetic is fp32; the gradient is rounded once.  Repeated calls give the same bits.
+ *   z, dz     [rows][pitch] of dtype (quan_dtype_t), the row's first `classes` elements its logits;
+ *             dz's others become 0.  dz may be z itself (in place), no other overlap
+ *   index     [rows][top] classes, index_bits (32 or 64) wide, signed
+ *   teacher   [rows][top] of teacher_dtype
+ *   dloss     fp32 [rows], dL/dloss, or NULL: 1
+ *   loss, lse fp32 [rows]; lse = ln of the sum of e^(z / T), which quan_distill_bwd reads
+ * quan_distill_fwd_bwd is both in one pass over z (its lse is not kept).  top <= 256, pitch < 2^24,
+ * rows < 2^31, fewer than 2^40 logits, else QUAN_ERR_UNSUPPORTED; 1e-6 <= T <= 1e6; scale finite.
+ * rows = 0 is a no-op.
+ */
+quan_status_t quan_distill_fwd(const void* z, const void* index, const void* teacher,
+                               long long rows, int classes, int pitch, int top, int dtype,
+                               int teacher_dtype, int index_bits, float temperature, float* loss,
+                               float* lse, quan_stream_t stream);
+quan_status_t quan_distill_bwd(const float* dloss, const void* z, const float* lse,
+                               const void* index, const void* teacher, long long rows,
+                               int classes, int pitch, int top, int dtype, int teacher_dtype,
+                               int index_bits, float temperature, float scale, void* dz,
+                               quan_stream_t stream);
+quan_status_t quan_distill_fwd_bwd(const void* z, const void* index, const void* teacher,
+                                   const float* dloss, long long rows, int classes, int pitch,
+                                   int top, int dtype, int teacher_dtype, int index_bits,
+                                   float temperature, float scale, float* loss, void* dz,
+                                   quan_stream_t stream);
+
 /* Select the path of later quan_qconv2d_fwd / _res calls in this process (default AUTO). */
 quan_status_t quan_set_path(int path);
 /* Path (quan_path_t, TC or SIMT) the last successful convolution call of this thread ran. */

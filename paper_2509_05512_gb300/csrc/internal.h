@@ -232,6 +232,20 @@ size_t join_bwd_workspace_bytes(long long rows, int C, int groups, long long ima
 cudaError_t launch_join_bwd(const JoinArgs& a, float* workspace, float* dpost, float* dgate,
                             float* dpre, int num_sms, cudaStream_t stream);
 
+// Distillation from a teacher's top logits (distill.cu): the loss (dz null), its gradient (loss null,
+// lse_in given) or both.
+struct DistillArgs {
+    const void *z, *index, *teacher;
+    const float *lse_in, *dloss;
+    float *loss, *lse;
+    void* dz;
+    long long rows, pitch;
+    int classes, top;
+    bool f32, teacher_f32, index64;
+    float temperature, scale;
+};
+cudaError_t launch_distill(const DistillArgs& a, int num_sms, cudaStream_t stream);
+
 // The pointwise product in 8-bit floating point (qpoint_f8.cu) of Kq input and Nq output
 // quaternion channels.  f8_pitch: bytes of a row of 8-bit channels of one component.
 int f8_pitch(int Kq);

@@ -52,7 +52,8 @@ struct Conv {
     c.x, c.w[0], c.w[1], c.w[2], c.w[3], c.bias, c.scale, c.shift, c.v[0], c.v[1], c.v[2],  \
         c.v[3], c.v[4], c.v[5], c.v[6], c.v[7], c.v[8], c.v[9]
 
-// The random numbers of a dropout, and the arguments both directions of a join share.
+// The random numbers of a dropout, and the arguments that the calls of a join and of a distillation
+// share.
 struct Draw {
     unsigned long long seed, offset;
     const unsigned long long* counter;
@@ -76,6 +77,19 @@ struct Join {
 #define QUAN_JOIN_ARGS                                                                       \
     j.post, j.gate, j.pre, j.rows, j.C, j.groups, j.images, j.dtype, j.alpha, j.eps, j.p,    \
         j.d.seed, j.d.offset, j.d.counter
+
+struct Distill {
+    void *z, *index, *teacher;
+    long long rows;
+    int classes, pitch, top, dtype, teacher_dtype, index_bits;
+    float temperature;
+    explicit Distill(Args& g)
+        : z(g.ptr()), index(g.ptr()), teacher(g.ptr()), rows(g.next()), classes(g.num()),
+          pitch(g.num()), top(g.num()), dtype(g.num()), teacher_dtype(g.num()),
+          index_bits(g.num()), temperature(g.real()) {}
+};
+#define QUAN_DISTILL_ARGS                                                                   \
+    d.rows, d.classes, d.pitch, d.top, d.dtype, d.teacher_dtype, d.index_bits, d.temperature
 
 }  // namespace
 
@@ -234,6 +248,31 @@ extern "C" int quan_packed_call(int op, const long long* words) {
             void* dx = g.ptr();
             return quan_qpoint_f8_bwd_data(dy, wq, scale, rows, Cin, Cout, ws, bytes, dx,
                                            g.stream());
+        }
+        case 18: {
+            const Distill d(g);
+            float* loss = g.f32();
+            float* lse = g.f32();
+            return quan_distill_fwd(d.z, d.index, d.teacher, QUAN_DISTILL_ARGS, loss, lse,
+                                    g.stream());
+        }
+        case 19: {
+            const Distill d(g);
+            const float scale = g.real();
+            float* dloss = g.f32();
+            float* lse = g.f32();
+            void* dz = g.ptr();
+            return quan_distill_bwd(dloss, d.z, lse, d.index, d.teacher, QUAN_DISTILL_ARGS, scale,
+                                    dz, g.stream());
+        }
+        case 20: {
+            const Distill d(g);
+            const float scale = g.real();
+            float* dloss = g.f32();
+            float* loss = g.f32();
+            void* dz = g.ptr();
+            return quan_distill_fwd_bwd(d.z, d.index, d.teacher, dloss, QUAN_DISTILL_ARGS, scale,
+                                        loss, dz, g.stream());
         }
         default:
             return QUAN_ERR_INVALID_ARG;

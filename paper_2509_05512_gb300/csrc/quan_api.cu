@@ -477,6 +477,51 @@ quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
     return QUAN_OK;
 }
 
+// Both directions of the distillation loss; `a` holds everything but the flags of its types.
+quan_status_t run_distill(quan::DistillArgs a, int dtype, int teacher_dtype, int index_bits,
+                          quan_stream_t stream) {
+    if ((dtype != QUAN_DTYPE_BF16 && dtype != QUAN_DTYPE_F32) ||
+        (teacher_dtype != QUAN_DTYPE_BF16 && teacher_dtype != QUAN_DTYPE_F32) ||
+        (index_bits != 32 && index_bits != 64))
+        return fail(QUAN_ERR_INVALID_ARG, "unknown dtype %d, teacher dtype %d or %d-bit classes",
+                    dtype, teacher_dtype, index_bits);
+    if (a.rows < 0 || a.classes < 1 || a.pitch < a.classes || a.top < 1)
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "rows=%lld must be >= 0, classes=%d and top=%d positive, pitch=%lld at least "
+                    "classes",
+                    a.rows, a.classes, a.top, a.pitch);
+    if (!(a.temperature >= 1e-6f && a.temperature <= 1e6f) || !std::isfinite(a.scale))
+        return fail(QUAN_ERR_INVALID_ARG, "temperature must be in [1e-6, 1e6], scale finite");
+    if (a.pitch >= (1LL << 24) || a.rows >= (1LL << 31) || a.rows >= (1LL << 40) / a.pitch ||
+        a.top > 256)
+        return fail(QUAN_ERR_UNSUPPORTED, "tensor too large, or more than 256 slots a row");
+    if (a.rows == 0) return QUAN_OK;
+    if (!a.z || !a.index || !a.teacher)
+        return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    a.f32 = dtype == QUAN_DTYPE_F32;
+    a.teacher_f32 = teacher_dtype == QUAN_DTYPE_F32;
+    a.index64 = index_bits == 64;
+    const size_t e = a.f32 ? 4 : 2, te = a.teacher_f32 ? 4 : 2, ie = a.index64 ? 8 : 4;
+    const void* tensors[] = {a.z, a.dz};
+    const void* vectors[] = {a.lse_in, a.dloss, a.loss, a.lse};
+    if (misaligned(tensors, 2, e) || misaligned(&a.index, 1, ie) ||
+        misaligned(&a.teacher, 1, te) || misaligned(vectors, 4, 4))
+        return fail(QUAN_ERR_INVALID_ARG, "tensors must be aligned to their elements");
+    const size_t n = static_cast<size_t>(a.rows), zb = n * a.pitch * e, rb = n * 4;
+    const Span outs[] = {{a.dz, zb}, {a.loss, rb}, {a.lse, rb}};
+    const Span ins[] = {{a.z, zb}, {a.index, n * a.top * ie}, {a.teacher, n * a.top * te},
+                        {a.lse_in, rb}, {a.dloss, rb}};
+    const unsigned equal[] = {1u, 0u, 0u};
+    if (clash(outs, 3, ins, 5, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "an output overlaps another tensor");
+    int num_sms = 0, cc = 0;
+    cudaError_t ce;
+    if (!device_info(&num_sms, &cc, &ce)) return cuda_fail(ce, "device query");
+    ce = quan::launch_distill(a, num_sms, reinterpret_cast<cudaStream_t>(stream));
+    if (ce != cudaSuccess) return cuda_fail(ce, "distillation launch");
+    return QUAN_OK;
+}
+
 }  // namespace
 
 thread_local const char* quan::last_variant = "";
@@ -1132,6 +1177,69 @@ quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const floa
                                       size_t workspace_bytes, void* dx, quan_stream_t stream) {
     return run_qpoint_f8(dy, wq, wscale, {nullptr, nullptr, nullptr, nullptr}, rows, Cout, Cin,
                          QUAN_ACT_NONE, true, workspace, workspace_bytes, dx, stream);
+}
+
+quan_status_t quan_distill_fwd(const void* z, const void* index, const void* teacher,
+                               long long rows, int classes, int pitch, int top, int dtype,
+                               int teacher_dtype, int index_bits, float temperature, float* loss,
+                               float* lse, quan_stream_t stream) {
+    if (rows > 0 && (!loss || !lse)) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    quan::DistillArgs a = {};
+    a.z = z;
+    a.index = index;
+    a.teacher = teacher;
+    a.loss = loss;
+    a.lse = lse;
+    a.rows = rows;
+    a.pitch = pitch;
+    a.classes = classes;
+    a.top = top;
+    a.temperature = temperature;
+    return run_distill(a, dtype, teacher_dtype, index_bits, stream);
+}
+
+quan_status_t quan_distill_bwd(const float* dloss, const void* z, const float* lse,
+                               const void* index, const void* teacher, long long rows,
+                               int classes, int pitch, int top, int dtype, int teacher_dtype,
+                               int index_bits, float temperature, float scale, void* dz,
+                               quan_stream_t stream) {
+    if (rows > 0 && (!lse || !dz)) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    quan::DistillArgs a = {};
+    a.z = z;
+    a.index = index;
+    a.teacher = teacher;
+    a.lse_in = lse;
+    a.dloss = dloss;
+    a.dz = dz;
+    a.rows = rows;
+    a.pitch = pitch;
+    a.classes = classes;
+    a.top = top;
+    a.temperature = temperature;
+    a.scale = scale;
+    return run_distill(a, dtype, teacher_dtype, index_bits, stream);
+}
+
+quan_status_t quan_distill_fwd_bwd(const void* z, const void* index, const void* teacher,
+                                   const float* dloss, long long rows, int classes, int pitch,
+                                   int top, int dtype, int teacher_dtype, int index_bits,
+                                   float temperature, float scale, float* loss, void* dz,
+                                   quan_stream_t stream) {
+    if (rows > 0 && (!loss || !dz)) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    quan::DistillArgs a = {};
+    a.z = z;
+    a.index = index;
+    a.teacher = teacher;
+    a.dloss = dloss;
+    a.loss = loss;
+    a.dz = dz;
+    a.rows = rows;
+    a.pitch = pitch;
+    a.classes = classes;
+    a.top = top;
+    a.temperature = temperature;
+    a.scale = scale;
+    return run_distill(a, dtype, teacher_dtype, index_bits, stream);
 }
 
 quan_status_t quan_set_path(int path) {

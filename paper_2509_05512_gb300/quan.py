@@ -110,6 +110,10 @@ def load():
                                                 [_vp] * 2)
         lib.quan_qpoint_f8_workspace_size.argtypes = [_ll, _i, _i]
         lib.quan_qpoint_f8_workspace_size.restype = ctypes.c_size_t
+        _distill_sizes = [_ll] + [_i] * 6 + [_f]
+        lib.quan_distill_fwd.argtypes = [_vp] * 3 + _distill_sizes + [_vp] * 3
+        lib.quan_distill_bwd.argtypes = [_vp] * 5 + _distill_sizes + [_f] + [_vp] * 2
+        lib.quan_distill_fwd_bwd.argtypes = [_vp] * 4 + _distill_sizes + [_f] + [_vp] * 3
         lib.quan_set_path.argtypes = [_i]
         lib.quan_last_path.argtypes = []
         lib.quan_last_kernel.argtypes = []
@@ -140,7 +144,8 @@ def load():
                      "quan_qconv2d_maxpool_fwd", "quan_qconv2d_maxpool_rgb_fwd",
                      "quan_iqbn_train_fwd", "quan_dropout", "quan_residual_join_fwd",
                      "quan_residual_join_bwd", "quan_f8_weights", "quan_qpoint_f8_fwd",
-                     "quan_qpoint_f8_bwd_data",
+                     "quan_qpoint_f8_bwd_data", "quan_distill_fwd", "quan_distill_bwd",
+                     "quan_distill_fwd_bwd",
                      "quan_qconv2d_sep_bwd_weight",
                      "quan_maxpool2d_fwd", "quan_set_path", "quan_set_tc_tiles",
                      "quan_set_wait_limit_ns", "quan_device_status", "quan_set_fault_injection",
@@ -213,6 +218,8 @@ _JOIN_FWD = struct.Struct("10q3d2Q4q").pack
 _QPOINT_F8 = struct.Struct("14q").pack
 _QPOINT_F8_BWD = struct.Struct("10q").pack
 _JOIN_BWD = struct.Struct("12q3d2Q9q").pack
+_DISTILL_FWD = struct.Struct("10qd3q").pack
+_DISTILL_BWD = struct.Struct("10q2d4q").pack
 
 
 def _call(op: int, words: bytes) -> None:
@@ -928,3 +935,117 @@ def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None,
                         _addr(counter), _addr(workspace), nbytes, _addr(dx), _addr(dh),
                         _addr(dpost), _addr(dgate), _addr(dpre), _stream(stream, dev)))
     return (dy if dx is None else dx, dh, dpost, dgate, dpre)
+
+
+# ------------------------------------------------------------------ distillation
+
+def quan_distill_fwd(z, index, teacher, rows, classes, pitch, top, dtype, teacher_dtype, index_bits,
+                     temperature, loss, lse, stream=None) -> None:
+    _call(18, _DISTILL_FWD(_addr(z), _addr(index), _addr(teacher), rows, classes, pitch, top, dtype,
+                           teacher_dtype, index_bits, temperature, _addr(loss), _addr(lse),
+                           _stream(stream)))
+
+
+def quan_distill_bwd(dloss, z, lse, index, teacher, rows, classes, pitch, top, dtype, teacher_dtype,
+                     index_bits, temperature, scale, dz, stream=None) -> None:
+    _call(19, _DISTILL_BWD(_addr(z), _addr(index), _addr(teacher), rows, classes, pitch, top, dtype,
+                           teacher_dtype, index_bits, temperature, scale, _addr(dloss), _addr(lse),
+                           _addr(dz), _stream(stream)))
+
+
+def quan_distill_fwd_bwd(z, index, teacher, dloss, rows, classes, pitch, top, dtype, teacher_dtype,
+                         index_bits, temperature, scale, loss, dz, stream=None) -> None:
+    _call(20, _DISTILL_BWD(_addr(z), _addr(index), _addr(teacher), rows, classes, pitch, top, dtype,
+                           teacher_dtype, index_bits, temperature, scale, _addr(dloss), _addr(loss),
+                           _addr(dz), _stream(stream)))
+
+
+def _distill(logits, index, teacher, classes):
+    """The device, the leading shape and the packed sizes of a distillation's tensors, checked."""
+    torch = _torch or _get_torch()
+    t, shape = logits.dtype, logits.shape
+    dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else _dtype_of("logits", logits)
+    dev = _device("logits", logits)
+    if not logits.is_contiguous():
+        _check_tensor("logits", logits, shape, t, dev)
+    lead, pitch = shape[:-1], shape[-1]
+    slots = index.shape
+    if slots[:-1] != lead or index.get_device() != dev or not index.is_contiguous() or \
+            (index.dtype is not torch.int64 and index.dtype is not torch.int32):
+        _check_tensor("index", index, lead + slots[-1:], torch.int64, dev)
+    teacher_dtype = QUAN_DTYPE_BF16 if teacher.dtype is torch.bfloat16 else \
+        _dtype_of("teacher", teacher)
+    if teacher.shape != slots or teacher.get_device() != dev or not teacher.is_contiguous():
+        _check_tensor("teacher", teacher, slots, teacher.dtype, dev)
+    if classes is None:
+        classes = pitch
+    rows = logits.numel() // pitch if pitch else 0
+    return dev, lead, (rows, classes, pitch, slots[-1], dtype, teacher_dtype,
+                       64 if index.dtype is torch.int64 else 32)
+
+
+def distill_loss(logits, index, teacher, *, classes=None, temperature=1.0, loss=None, lse=None,
+                 stream=None):
+    """The loss of each row of bf16 or fp32 logits [..., C] (CUDA) against a teacher's top logits:
+    teacher [..., K] (bf16 or fp32) and their classes, index [..., K] (int64 or int32), as
+    torch.topk gives them (K up to 256):
+        p = softmax(teacher / T),  q = softmax(logits / T),  T^2 sum_k p_k (ln p_k - ln q_index_k)
+    classes: the first so many channels are the classes (all by default), the others padding.
+    Slots with a class outside [0, classes) are empty; a row of empty slots (an ignored pixel) has
+    loss 0.  Returns (loss, lse), fp32 [...]; lse is for distill_loss_backward."""
+    f32 = (_torch or _get_torch()).float32
+    dev, lead, sizes = _distill(logits, index, teacher, classes)
+    if loss is None:
+        loss = _empty(stream, lead, f32, logits.device)
+    else:
+        _check_tensor("loss", loss, lead, f32, dev)
+    if lse is None:
+        lse = _empty(stream, lead, f32, logits.device)
+    else:
+        _check_tensor("lse", lse, lead, f32, dev)
+    _call(18, _DISTILL_FWD(logits.data_ptr(), index.data_ptr(), teacher.data_ptr(), *sizes,
+                           temperature, loss.data_ptr(), lse.data_ptr(), _stream(stream, dev)))
+    return loss, lse
+
+
+def distill_loss_backward(dloss, logits, lse, index, teacher, *, classes=None, temperature=1.0,
+                          scale=1.0, out=None, stream=None):
+    """Gradient of distill_loss with respect to its logits, times scale: from dloss, fp32 [...]
+    (None: 1), and the forward call's lse and arguments.  Channels behind the classes get 0.  out
+    may be logits (in place)."""
+    f32 = (_torch or _get_torch()).float32
+    dev, lead, sizes = _distill(logits, index, teacher, classes)
+    if dloss is not None:
+        _check_tensor("dloss", dloss, lead, f32, dev)
+    _check_tensor("lse", lse, lead, f32, dev)
+    if out is None:
+        out = _empty(stream, logits.shape, logits.dtype, logits.device)
+    else:
+        _check_tensor("out", out, logits.shape, logits.dtype, dev)
+    _call(19, _DISTILL_BWD(logits.data_ptr(), index.data_ptr(), teacher.data_ptr(), *sizes,
+                           temperature, scale, _addr(dloss), lse.data_ptr(), out.data_ptr(),
+                           _stream(stream, dev)))
+    return out
+
+
+def distill_loss_and_gradient(logits, index, teacher, dloss=None, *, classes=None,
+                              temperature=1.0, scale=1.0, loss=None, out=None, stream=None):
+    """distill_loss and distill_loss_backward in one pass over the logits: (loss, dlogits), for a
+    dloss (a row's weight in the sum that is minimised; None: 1) that is known beforehand.  out may
+    be logits (in place)."""
+    f32 = (_torch or _get_torch()).float32
+    dev, lead, sizes = _distill(logits, index, teacher, classes)
+    if dloss is not None:
+        _check_tensor("dloss", dloss, lead, f32, dev)
+    if loss is None:
+        loss = _empty(stream, lead, f32, logits.device)
+    else:
+        _check_tensor("loss", loss, lead, f32, dev)
+    if out is None:
+        out = _empty(stream, logits.shape, logits.dtype, logits.device)
+    else:
+        _check_tensor("out", out, logits.shape, logits.dtype, dev)
+    _call(20, _DISTILL_BWD(logits.data_ptr(), index.data_ptr(), teacher.data_ptr(), *sizes,
+                           temperature, scale, _addr(dloss), loss.data_ptr(), out.data_ptr(),
+                           _stream(stream, dev)))
+    return loss, out
