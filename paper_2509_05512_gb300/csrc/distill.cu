@@ -13,6 +13,8 @@
 // adds the others' p in their order, so that no sum depends on which thread comes first.
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "internal.h"
 #include "ptx.cuh"
 #include "vec_io.cuh"
@@ -21,6 +23,7 @@ namespace quan {
 namespace {
 
 constexpr float LOG2E = 1.44269504f;
+constexpr int DISTILL_TOP = 256;    // slots a row at most
 constexpr int LOSS = 1, GRAD = 2;  // what a launch computes: one of them, or both
 
 struct DistillParams {
@@ -39,9 +42,9 @@ struct DistillParams {
 template <typename T>
 struct RowView {
     static constexpr int E = 16 / static_cast<int>(sizeof(T));
-    const T* base;   // the first chunk
-    int head, n;     // the row is elements head .. head + n - 1 from there
-    const T *first, *last;  // the tensor
+    const T* base;           // the first chunk
+    int head, n;             // the row is elements head .. head + n - 1 from there
+    const T *first, *last;   // the tensor
     __device__ __forceinline__ RowView(const T* tensor, long long elements, long long at, int len) {
         first = tensor;
         last = tensor + elements;
@@ -51,55 +54,54 @@ struct RowView {
         n = len;
     }
     __device__ __forceinline__ int chunks() const { return (head + n + E - 1) / E; }
-    // A chunk as it is in memory.  Only one that reaches past the tensor's ends goes element by
-    // element.
-    __device__ __forceinline__ void load(int chunk, Raw<T, E>& r) const {
+    // All of a chunk is in the row's first `len` elements; some of it is past the tensor's ends.
+    __device__ __forceinline__ bool whole(int chunk, int len) const {
+        return chunk * E >= head && (chunk + 1) * E <= head + len;
+    }
+    __device__ __forceinline__ bool outside(int chunk) const {
         const T* p = base + chunk * E;
-        if (p >= first && p + E <= last) {
-            r.load(p);
+        return p < first || p + E > last;
+    }
+    // A chunk as it is in memory, element by element where it reaches past the tensor's ends.
+    __device__ __forceinline__ void load(int chunk, Raw<T, E>& r) const {
+        if (!outside(chunk)) {
+            r.load(base + chunk * E);
         } else {
-            float v[E];
+            load_masked(chunk, n, r);
+        }
+    }
+    // A chunk of which not all is in the row's first `len` elements, the others -inf.
+    __device__ __forceinline__ void load_masked(int chunk, int len, Raw<T, E>& r) const {
+        const T* p = base + chunk * E;
+        const int lo = head - chunk * E, hi = lo + len;
+        float v[E];
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                Raw<T, 1> e;
-                float w[1] = {0.0f};
-                if (p + j >= first && p + j < last) {
-                    e.load(p + j);
-                    e.values(w);
-                }
-                v[j] = w[0];
+        for (int j = 0; j < E; ++j) {
+            Raw<T, 1> e;
+            float w[1] = {-INFINITY};
+            if (j >= lo && j < hi) {
+                e.load(p + j);
+                e.values(w);
             }
-            r.set(v);
+            v[j] = w[0];
         }
+        r.set(v);
     }
-    // A chunk's values, -inf outside the row's first `len` elements.
-    __device__ __forceinline__ void values(int chunk, const Raw<T, E>& r, int len,
-                                           float (&v)[E]) const {
-        r.values(v);
-        const int lo = head - chunk * E, hi = head + len - chunk * E;
-        if (lo > 0 || hi < E) {
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (j < lo || j >= hi) v[j] = -INFINITY;
-        }
-    }
-    // Writes a chunk's values to the row's place in `out`, a tensor laid out as this one.
-    __device__ __forceinline__ void store(int chunk, const float (&v)[E], T* out_row) const {
+    // Writes what the row has of a chunk to its place in `out`, element by element: 0 past the
+    // first `len`.
+    __device__ __forceinline__ void store_part(int chunk, const Raw<T, E>& r, int len,
+                                               T* out_row) const {
         T* p = out_row - head + chunk * E;
-        const int lo = head - chunk * E, hi = head + n - chunk * E;
-        if (lo <= 0 && hi >= E && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-            Raw<T, E> r;
-            r.set(v);
-            r.store(p);
-        } else {
+        const int lo = head - chunk * E;
+        float v[E];
+        r.values(v);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                if (j < lo || j >= hi) continue;
-                Raw<T, 1> e;
-                const float w[1] = {v[j]};
-                e.set(w);
-                e.store(p + j);
-            }
+        for (int j = 0; j < E; ++j) {
+            if (j < lo || j >= lo + n) continue;
+            Raw<T, 1> e;
+            const float w[1] = {j < lo + len ? v[j] : 0.0f};
+            e.set(w);
+            e.store(p + j);
         }
     }
 };
@@ -122,13 +124,22 @@ __device__ __forceinline__ void put(T* p, float x) {
 }
 
 // Slot k of a row: its class (-1 when empty) and the teacher's logit.
-__device__ __forceinline__ int slot(const DistillParams& p, long long row, int k, float& t) {
+__device__ __forceinline__ long long slot_class(const DistillParams& p, long long row, int k) {
     const long long at = row * p.top + k;
-    const long long id = p.index64 ? static_cast<const long long*>(p.index)[at]
-                                   : static_cast<const int*>(p.index)[at];
-    t = p.teacher_f32 ? element(static_cast<const float*>(p.teacher) + at)
-                      : element(static_cast<const __nv_bfloat16*>(p.teacher) + at);
+    return p.index64 ? static_cast<const long long*>(p.index)[at]
+                     : static_cast<const int*>(p.index)[at];
+}
+__device__ __forceinline__ float slot_logit(const DistillParams& p, long long row, int k) {
+    const long long at = row * p.top + k;
+    return p.teacher_f32 ? element(static_cast<const float*>(p.teacher) + at)
+                         : element(static_cast<const __nv_bfloat16*>(p.teacher) + at);
+}
+__device__ __forceinline__ int slot_id(const DistillParams& p, long long id, float t) {
     return id >= 0 && id < p.classes && t != -INFINITY ? static_cast<int>(id) : -1;
+}
+__device__ __forceinline__ int slot(const DistillParams& p, long long row, int k, float& t) {
+    t = slot_logit(p, row, k);
+    return slot_id(p, slot_class(p, row, k), t);
 }
 
 // A sum of 2^((z - m) c) for another maximum.  (Without a number so far, m = -inf, it is 0, or NaN
@@ -137,158 +148,850 @@ __device__ __forceinline__ float shifted(float s, float m, float top, float c) {
     return m == -INFINITY ? s : s * ex2_approx_ftz((m - top) * c);
 }
 
-constexpr int DISTILL_THREADS = 256;
-constexpr int DISTILL_WARPS = DISTILL_THREADS / 32;
-
-__device__ __forceinline__ float warp_max(float v) {
+// Max and sum over the lanes of a group of `lanes` (a power of two) of a warp.
+__device__ __forceinline__ float lanes_max(float v, int lanes) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < lanes) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
-__device__ __forceinline__ float warp_sum(float v) {
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// Max and sum over the block; `sm` holds a word a warp.
-template <bool MAX>
-__device__ __forceinline__ float block_reduce(float v, float* sm) {
-    v = MAX ? warp_max(v) : warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    v = lane < DISTILL_WARPS ? sm[lane] : (MAX ? -INFINITY : 0.0f);
-    return MAX ? warp_max(v) : warp_sum(v);
+// A row's slots, `top4` (top rounded up to 4) each: the class or -1, the teacher's logit and then p,
+// the student's logit of the class.
+struct Slots {
+    int* id;
+    float *p, *z;
+    int top, top4;
+};
+
+// The teacher's side of a row by `lanes` lanes of a warp: p of each slot, and the sum of p ln p.
+__device__ __forceinline__ float teacher_side(const Slots& s, const DistillParams& p, int lane,
+                                              int lanes, bool& some) {
+    float m = -INFINITY, sum = 0.0f, h = 0.0f;
+    bool any = false;
+    for (int k = lane; k < s.top; k += lanes)
+        if (s.id[k] >= 0) {
+            m = fmaxf(m, s.p[k]);
+            any = true;
+        }
+    m = lanes_max(m, lanes);
+    const unsigned votes = __ballot_sync(0xffffffffu, any);
+    some = ((votes >> ((threadIdx.x & 31) - lane)) & (0xffffffffu >> (32 - lanes))) != 0;
+    for (int k = lane; k < s.top; k += lanes)
+        if (s.id[k] >= 0) sum += ex2_approx_ftz((s.p[k] - m) * p.c);
+    sum = lanes_sum(sum, lanes);
+    const float ln_sum = logf(sum), inv = 1.0f / sum;
+    for (int k = lane; k < s.top; k += lanes)
+        if (s.id[k] >= 0) {
+            const float x = s.p[k] - m, pk = ex2_approx_ftz(x * p.c) * inv;
+            s.p[k] = pk;
+            // (a slot whose share has vanished has no part, be its class impossible)
+            if (!(pk == 0.0f)) h = fmaf(pk, fmaf(x, p.inv_t, -ln_sum), h);
+        }
+    return lanes_sum(h, lanes);
 }
 
-// A block a row; the logits are read once for the sums and once for the gradient.  Loss and gradient
-// of 4096 x 32768 bf16: 149 us (the second reading mostly from L2); of 100,352 x 100: 403 us, where a
-// block has 13 chunks to read and a dozen barriers.
-template <typename T, int MODE>
-__global__ void __launch_bounds__(DISTILL_THREADS) distill_kernel(const DistillParams p) {
+// What all slots of slot k's class put on it, or -1 where an earlier slot has that class.
+__device__ __forceinline__ float class_share(const Slots& s, int k) {
+    const int id = s.id[k];
+    int same = 0;
+    for (int j = 0; j < s.top4; j += 4) {
+        const int4 o = *reinterpret_cast<const int4*>(s.id + j);
+        same += (o.x == id) + (o.y == id) + (o.z == id) + (o.w == id);
+    }
+    if (same == 1) return s.p[k];
+    float share = 0.0f;
+#pragma unroll 1
+    for (int j = 0; j < s.top; ++j)
+        if (s.id[j] == id) {
+            if (j < k) return -1.0f;
+            share += s.p[j];
+        }
+    return share;
+}
+
+// 16 bytes to shared memory, asynchronously; a thread waits for its own copies with copies_wait.
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_commit() {
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// Two floats at a time.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+// v becomes 2^((v - at) c); `sum` takes its elements by twos.
+template <int N>
+__device__ __forceinline__ void powers(float (&v)[N], float at, float c, float2& sum) {
+    const float2 a = make_float2(-at, -at), cc = make_float2(c, c);
+#pragma unroll
+    for (int j = 0; j + 1 < N; j += 2) {
+        const float2 x = mul2(add2(make_float2(v[j], v[j + 1]), a), cc);
+        v[j] = ex2_approx_ftz(x.x);
+        v[j + 1] = ex2_approx_ftz(x.y);
+        sum = add2(sum, make_float2(v[j], v[j + 1]));
+    }
+    if constexpr (N % 2 == 1) {
+        v[N - 1] = ex2_approx_ftz((v[N - 1] - at) * c);
+        sum.x += v[N - 1];
+    }
+}
+template <int N>
+__device__ __forceinline__ void times(float (&v)[N], float f) {
+    const float2 ff = make_float2(f, f);
+#pragma unroll
+    for (int j = 0; j + 1 < N; j += 2) {
+        const float2 x = mul2(make_float2(v[j], v[j + 1]), ff);
+        v[j] = x.x;
+        v[j + 1] = x.y;
+    }
+    if constexpr (N % 2 == 1) v[N - 1] *= f;
+}
+
+// Largest of the elements seen so far; bf16 by twos.
+template <typename T, int N>
+struct Largest;
+template <int N>
+struct Largest<float, N> {
+    float m = -INFINITY;
+    __device__ __forceinline__ void add(const Raw<float, N>& r) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = fmaxf(m, __uint_as_float(r.w[j]));
+    }
+    __device__ __forceinline__ float get() const { return m; }
+};
+template <int N>
+struct Largest<__nv_bfloat16, N> {
+    uint32_t m = 0xFF80FF80u;  // -inf
+    __device__ __forceinline__ void add(const Raw<__nv_bfloat16, N>& r) {
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j)
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(r.w[j]));
+    }
+    __device__ __forceinline__ float get() const {
+        float lo, hi;
+        bf16x2_to_f32(m, lo, hi);
+        return fmaxf(lo, hi);
+    }
+};
+
+// ------------------------------------------------------------------ long rows
+
+constexpr int ROW_THREADS = 512, ROW_WARPS = ROW_THREADS / 32, ROW_CLUSTER = 8;
+
+// A row by `parts` blocks of a cluster, NCH chunks of it a thread, which stay in registers between the
+// sums and the gradient (what a row has beyond that is read twice).  The first warp does the teacher's
+// side while the row's loads are under way; maximum and sum are joined over warps and, pushed into the
+// other blocks' shared memory, over the cluster.
+template <typename T, int MODE, int NCH>
+__global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const DistillParams p,
+                                                                     int parts) {
     constexpr int E = RowView<T>::E;
-    extern __shared__ float slots[];  // p_k, the row's logit at class k, class k
-    float *sp = slots, *sz = slots + p.top;
-    int* si = reinterpret_cast<int*>(slots + 2 * p.top);
-    __shared__ float sm[DISTILL_WARPS];
+    extern __shared__ int4 dynamic[];
+    __shared__ float warp_m[ROW_WARPS], warp_s[ROW_WARPS], part_m[ROW_CLUSTER], part_s[ROW_CLUSTER];
+    __shared__ float entropy, counts;
+    Slots s;
+    s.top = p.top;
+    s.top4 = (p.top + 3) & ~3;
+    s.id = reinterpret_cast<int*>(dynamic);
+    s.p = reinterpret_cast<float*>(s.id + s.top4);
+    s.z = s.p + s.top4;
+    float* share = s.z + s.top4;
     griddep_launch_dependents();
     griddep_wait();
-    const long long row = blockIdx.x;
+    const long long row = blockIdx.x / static_cast<unsigned>(parts);
+    const int part = static_cast<int>(blockIdx.x - row * parts);
+    const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
     const T* z = static_cast<const T*>(p.z);
     const RowView<T> view(z, p.rows * p.pitch, row * p.pitch,
                           MODE & GRAD ? static_cast<int>(p.pitch) : p.classes);
-    const T* zrow = z + row * p.pitch;
-    // the teacher's side
-    float tm = -INFINITY, some = 0.0f;
-    for (int k = threadIdx.x; k < p.top; k += DISTILL_THREADS) {
-        float t;
-        const int id = slot(p, row, k, t);
-        si[k] = id;
-        sp[k] = t;
-        if (id >= 0) {
-            sz[k] = element(zrow + id);
-            tm = fmaxf(tm, t);
-            some = 1.0f;
+    const int chunks = view.chunks(), per = (chunks + parts - 1) / parts;
+    const int first = part * per, end = first + per < chunks ? first + per : chunks;
+    auto fetch = [&](int i, Raw<T, E>& q) {
+        if (view.whole(i, p.classes))
+            q.load(view.base + i * E);
+        else
+            view.load_masked(i, p.classes, q);
+    };
+    Raw<T, E> r[NCH];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+        const int i = first + tid + k * static_cast<int>(blockDim.x);
+        if (i < end) fetch(i, r[k]);
+    }
+    const int rest = first + tid + NCH * static_cast<int>(blockDim.x);
+    const float g_row = MODE & GRAD && p.dloss ? p.dloss[row] : 1.0f;
+    if ((MODE & LOSS) && parts > 1)  // (every block runs: it may be written to)
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    // this block's part of the row, for slots: chunk of a class
+    auto here = [&](int id) {
+        const int chunk = (view.head + id) / E;
+        return chunk >= first && chunk < end;
+    };
+    if (tid < 32) {
+        const T* zrow = z + row * p.pitch;
+        for (int k = lane; k < s.top4; k += 32) {
+            float t = 0.0f;
+            const int id = k < s.top ? slot(p, row, k, t) : -1;
+            s.id[k] = id;
+            s.p[k] = t;
+            if (id >= 0 && (((MODE & LOSS) && part == 0) || here(id))) s.z[k] = element(zrow + id);
+        }
+        __syncwarp();
+        bool some;
+        const float h = teacher_side(s, p, lane, 32, some);
+        if (lane == 0) {
+            entropy = h;
+            counts = some ? 1.0f : 0.0f;
         }
     }
-    tm = block_reduce<true>(tm, sm);
-    some = block_reduce<true>(some, sm);
-    float ts = 0.0f;
-    for (int k = threadIdx.x; k < p.top; k += DISTILL_THREADS)
-        if (si[k] >= 0) ts += expf((sp[k] - tm) * p.inv_t);
-    ts = block_reduce<false>(ts, sm);
-    const float ln_ts = logf(ts);
-    // the student's
-    float m = 0.0f, ln_s = 0.0f, inv_s = 1.0f, lse = 0.0f;
-    const int chunks = view.chunks();
+    float m = -INFINITY, sum = 0.0f;
     if (MODE & LOSS) {
-        m = -INFINITY;
-        float s = 0.0f;
-        for (int i = threadIdx.x; i < chunks; i += DISTILL_THREADS) {
-            Raw<T, E> r;
-            float v[E], top = m;
-            view.load(i, r);
-            view.values(i, r, p.classes, v);
+        Largest<T, E> largest;
 #pragma unroll
-            for (int j = 0; j < E; ++j) top = fmaxf(top, v[j]);
-            const float at = top == -INFINITY ? 0.0f : top;
-            s = shifted(s, m, at, p.c);
+        for (int k = 0; k < NCH; ++k)
+            if (first + tid + k * static_cast<int>(blockDim.x) < end) largest.add(r[k]);
+        m = largest.get();
+        const float at = m == -INFINITY ? 0.0f : m;
+        float2 sums = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int j = 0; j < E; ++j) s += ex2_approx_ftz((v[j] - at) * p.c);
+        for (int k = 0; k < NCH; ++k) {
+            if (first + tid + k * static_cast<int>(blockDim.x) >= end) continue;
+            float v[E];
+            r[k].values(v);
+            powers(v, at, p.c, sums);
+        }
+        sum = sums.x + sums.y;
+#pragma unroll 1
+        for (int i = rest; i < end; i += blockDim.x) {
+            Raw<T, E> q;
+            Largest<T, E> other;
+            float v[E];
+            fetch(i, q);
+            other.add(q);
+            const float top = fmaxf(m, other.get()), now = top == -INFINITY ? 0.0f : top;
+            sums = make_float2(shifted(sum, m, now, p.c), 0.0f);
+            q.values(v);
+            powers(v, now, p.c, sums);
+            sum = sums.x + sums.y;
             m = top;
         }
-        const float top = block_reduce<true>(m, sm);
-        s = block_reduce<false>(shifted(s, m, top, p.c), sm);
-        m = top;
-        inv_s = 1.0f / s;
-        ln_s = logf(s);
-        lse = fmaf(m, p.inv_t, ln_s);
-        float loss = 0.0f;
-        for (int k = threadIdx.x; k < p.top; k += DISTILL_THREADS) {
-            if (si[k] < 0) continue;
-            const float lnp = (sp[k] - tm) * p.inv_t - ln_ts, pk = expf(lnp);
-            // (a slot whose share has vanished has no part, be its class impossible)
-            if (!(pk == 0.0f)) loss = fmaf(pk, lnp - ((sz[k] - m) * p.inv_t - ln_s), loss);
+        const float top = lanes_max(m, 32);
+        sum = lanes_sum(shifted(sum, m, top, p.c), 32);
+        if (lane == 0) {
+            warp_m[tid >> 5] = top;
+            warp_s[tid >> 5] = sum;
         }
-        loss = block_reduce<false>(loss, sm);
-        if (threadIdx.x == 0) {
-            p.loss[row] = some > 0.0f ? p.t2 * loss : 0.0f;
-            if (p.lse) p.lse[row] = lse;
+    }
+    __syncthreads();
+    const bool some = counts > 0.0f;
+    // the shares of classes, for the loss and the gradient (their slots' first ones')
+    for (int k = tid; k < s.top; k += blockDim.x)
+        share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
+    float inv_s = 1.0f, lse = 0.0f;
+    if (MODE & LOSS) {
+        const float wm = lane < warps ? warp_m[lane] : -INFINITY;
+        m = lanes_max(wm, 32);
+        sum = lanes_sum(lane < warps ? shifted(warp_s[lane], wm, m, p.c) : 0.0f, 32);
+        if (parts > 1) {
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+            if (tid < parts) {
+                st_shared_cluster(mapa_shared(smem_u32(part_m + part), tid), __float_as_uint(m));
+                st_shared_cluster(mapa_shared(smem_u32(part_s + part), tid), __float_as_uint(sum));
+            }
+            cluster_sync_all();
+            const float pm = lane < parts ? part_m[lane] : -INFINITY;
+            m = lanes_max(pm, 32);
+            sum = lanes_sum(lane < parts ? shifted(part_s[lane], pm, m, p.c) : 0.0f, 32);
+        }
+        inv_s = 1.0f / sum;
+        const float ln_s = logf(sum);
+        lse = fmaf(m, p.inv_t, ln_s);
+        if (part == 0) {
+            __syncthreads();  // (share)
+            if (tid < 32) {
+                float loss = 0.0f;
+                for (int k = lane; k < s.top; k += 32)
+                    if (share[k] > 0.0f || share[k] != share[k])
+                        loss = fmaf(-share[k], (s.z[k] - m) * p.inv_t - ln_s, loss);
+                loss = lanes_sum(loss, 32) + entropy;
+                if (lane == 0) {
+                    p.loss[row] = some ? p.t2 * loss : 0.0f;
+                    if (p.lse) p.lse[row] = lse;
+                }
+            }
         }
     } else {
         lse = p.lse_in[row];
     }
     if (MODE & GRAD) {
         T* out = static_cast<T*>(p.dz) + row * p.pitch;
-        const float g = some > 0.0f ? (p.dloss ? p.dloss[row] : 1.0f) * p.scale : 0.0f;
+        const float g = some ? g_row * p.scale : 0.0f;
         auto q_of = [&](float v) {
             return MODE & LOSS ? ex2_approx_ftz((v - m) * p.c) * inv_s
                                : ex2_approx_ftz(fmaf(v, p.inv_t, -lse) * LOG2E);
         };
-        // the slots' elements, before any of the row is written (dz may be z)
-        __syncthreads();
-        for (int k = threadIdx.x; k < p.top; k += DISTILL_THREADS)
-            if (si[k] >= 0) sp[k] = expf((sp[k] - tm) * p.inv_t - ln_ts);
-        for (int i = threadIdx.x; i < chunks; i += DISTILL_THREADS) {
-            Raw<T, E> r;
+        const bool aligned = (reinterpret_cast<uintptr_t>(out - view.head) & 15u) == 0;
+        auto write = [&](int i, const Raw<T, E>& q) {
             float v[E];
-            view.load(i, r);
-            view.values(i, r, p.classes, v);
-            const int behind = view.head + p.classes - i * E;  // from here on: padding
+            q.values(v);
+            if constexpr (MODE & LOSS) {
+                float2 sums = make_float2(0.0f, 0.0f);
+                powers(v, m, p.c, sums);
+                times(v, g * inv_s);
+            } else {
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float d = g * q_of(v[j]);
-                v[j] = g == 0.0f || j >= behind ? 0.0f : d;
+                for (int j = 0; j < E; ++j) v[j] = g * q_of(v[j]);
             }
-            view.store(i, v, out);
+            if (g == 0.0f) {
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[j] = 0.0f;
+            }
+            Raw<T, E> o;
+            o.set(v);
+            if (aligned && view.whole(i, p.classes))
+                o.store(out - view.head + i * E);
+            else
+                view.store_part(i, o, p.classes, out);
+        };
+#pragma unroll
+        for (int k = 0; k < NCH; ++k) {
+            const int i = first + tid + k * static_cast<int>(blockDim.x);
+            if (i < end) write(i, r[k]);
         }
-        __syncthreads();
-        if (g != 0.0f) {
-            for (int k = threadIdx.x; k < p.top; k += DISTILL_THREADS) {
-                const int id = si[k];
-                if (id < 0) continue;
-                float share = 0.0f;
-                bool mine = true;
-                for (int j = 0; j < p.top; ++j) {
-                    if (si[j] != id) continue;
-                    if (j < k) mine = false;
-                    share += sp[j];
-                }
-                if (mine) put(out + id, g * (q_of(sz[k]) - share));
-            }
+#pragma unroll 1
+        for (int i = rest; i < end; i += blockDim.x) {
+            Raw<T, E> q;
+            fetch(i, q);
+            write(i, q);
+        }
+        __syncthreads();  // the slots' classes, over what was just written
+        for (int k = tid; k < s.top && g != 0.0f; k += blockDim.x) {
+            const int id = s.id[k];
+            if (id >= 0 && share[k] != -1.0f && here(id))
+                put(out + id, g * (q_of(s.z[k]) - share[k]));
         }
     }
 }
 
+// ------------------------------------------------------------------ many long rows
+
+__device__ __forceinline__ void named_bar_arrive(int id, int count) {
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(count) : "memory");
+}
+
+// Whole rows, one after the other, by CT threads with NCH chunks each at most and H warps beside
+// them for the slots.  Two rows are on their way into shared memory while one is worked on: a thread
+// copies, and later reads, its own chunks, so no barrier stands between.  It takes its powers against
+// its own maximum and keeps them: one power an element, and a factor a thread,
+// 2^((own max - max) c) g / S, once the row's maximum and sum are known.  Helper warp h does the
+// slots of every H-th row ahead of time, the loss, and the classes' elements behind the others.
+template <int CT_>
+struct RingCfg {
+    static constexpr int CT = CT_, NCH = 8, H = CT == 512 ? 4 : 2;  // helper warps
+    static constexpr int THREADS = CT + 32 * H;
+    static constexpr int STAGES = 3;
+    static constexpr int STAGE_CHUNKS = NCH * CT;
+    static constexpr int SUMS = H + 1;  // a row's sums are not overwritten before row + H's helper ran
+    // Blocks an SM, by the powers that a thread keeps: 64 of them leave room for 113 registers.
+    static constexpr int blocks(bool kept64) { return kept64 && CT == 128 ? 3 : 512 / CT; }
+    static size_t smem(int top) {
+        return size_t(16) * STAGES * STAGE_CHUNKS + size_t(16) * H * ((top + 3) & ~3);
+    }
+};
+
+// `most`: chunks of any row at most.
+template <typename T, int MODE, int CT>
+__global__ void __launch_bounds__(RingCfg<CT>::THREADS,
+                                  RingCfg<CT>::blocks((MODE & GRAD) && sizeof(T) == 2))
+    distill_ring_kernel(const DistillParams p, int most) {
+    using C = RingCfg<CT>;
+    constexpr int E = RowView<T>::E, H = C::H, NCH = C::NCH, WARPS = CT / 32;
+    extern __shared__ int4 dynamic[];
+    __shared__ float sum_m[C::SUMS][WARPS], sum_s[C::SUMS][WARPS], factor[H];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int tid = threadIdx.x, lane = tid & 31;
+    const T* z = static_cast<const T*>(p.z);
+    const long long step = gridDim.x;
+    const int len = MODE & GRAD ? static_cast<int>(p.pitch) : p.classes;
+    // maximum and sum of a row, from its warps'
+    auto joined = [&](int buf, float& m, float& s) {
+        const float wm = lane < WARPS ? sum_m[buf][lane] : -INFINITY;
+        m = lanes_max(wm, 32);
+        s = lanes_sum(lane < WARPS ? shifted(sum_s[buf][lane], wm, m, p.c) : 0.0f, 32);
+    };
+    if (tid < CT) {
+        int4* ring = dynamic + tid;
+        auto view_of = [&](long long row) {
+            return RowView<T>(z, p.rows * p.pitch, row * p.pitch, len);
+        };
+        // Of a thread's chunks, the first `wholes` are all classes (but for chunk 0 of a row that does
+        // not begin on a chunk).
+        auto wholes = [&](const RowView<T>& view) {
+            const int n = (view.head + p.classes) / E - tid + CT - 1;
+            return n < CT ? 0 : n / CT;
+        };
+        auto fetch = [&](long long row, int stage) {
+            if (row < p.rows) {
+                const RowView<T> view = view_of(row);
+                const int n = wholes(view);
+                const bool part0 = tid == 0 && view.head != 0;
+                int4* dst = ring + stage * C::STAGE_CHUNKS;
+                const T* src = view.base + tid * E;
+#pragma unroll
+                for (int k = 0; k < NCH; ++k)
+                    if (k < n && !(k == 0 && part0)) copy_async(dst + k * CT, src + k * CT * E);
+                // its other chunks, up to what any row has: -inf where there is no class
+                if (part0) {
+                    Raw<T, E> r;
+                    view.load_masked(0, p.classes, r);
+                    r.store(reinterpret_cast<T*>(dst));
+                }
+#pragma unroll 1
+                for (int i = tid + (n == 0 && part0 ? 1 : n) * CT; i < most; i += CT) {
+                    Raw<T, E> r;
+                    view.load_masked(i, p.classes, r);
+                    r.store(reinterpret_cast<T*>(dst + (i - tid)));
+                }
+            }
+            copies_commit();
+        };
+        // chunks that no row has
+        for (int i = tid + (most - tid + CT - 1) / CT * CT; i < C::STAGES * C::STAGE_CHUNKS; i += CT)
+            if (i % C::STAGE_CHUNKS >= most) {
+                Raw<T, E> r;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r.w[j] = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+                r.store(reinterpret_cast<T*>(dynamic + i));
+            }
+        long long row = blockIdx.x;
+        fetch(row, 0);
+        fetch(row + step, 1);
+        int stage = 0, h = 0, buf = 0;
+        for (; row < p.rows; row += step) {
+            copies_wait<1>();
+            // (the stage that this overwrites was read a row ago, by this thread)
+            fetch(row + 2 * step, stage == 0 ? 2 : stage - 1);
+            T* mine = reinterpret_cast<T*>(ring + stage * C::STAGE_CHUNKS);
+            float e[NCH][E];
+            Largest<T, E> largest;
+#pragma unroll
+            for (int k = 0; k < NCH; ++k)
+                if (k * CT < most) {
+                    Raw<T, E> r;
+                    r.load(mine + k * CT * E);
+                    largest.add(r);
+                }
+            const float m = largest.get(), at = m == -INFINITY ? 0.0f : m;
+            float2 sums = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < NCH; ++k)
+                if (k * CT < most) {
+                    Raw<T, E> r;
+                    r.load(mine + k * CT * E);
+                    r.values(e[k]);
+                    powers(e[k], at, p.c, sums);
+                }
+            float sum = sums.x + sums.y;
+            stage = stage == 2 ? 0 : stage + 1;
+            const float top = lanes_max(m, 32);
+            sum = lanes_sum(shifted(sum, m, top, p.c), 32);
+            if (lane == 0) {
+                sum_m[buf][tid >> 5] = top;
+                sum_s[buf][tid >> 5] = sum;
+            }
+            named_bar_sync(1 + h, CT + 32);
+            if (MODE & GRAD) {
+                float all, s;
+                joined(buf, all, s);
+                const float g = factor[h];
+                const float f = ex2_approx_ftz((at - all) * p.c) * (g * (1.0f / s));
+                const RowView<T> view = view_of(row);
+                T* out = static_cast<T*>(p.dz) + row * p.pitch;
+                T* place = out - view.head + tid * E;
+                const bool part0 = tid == 0 && view.head != 0;
+                const int n = (reinterpret_cast<uintptr_t>(place) & 15u) == 0 ? wholes(view) : 0;
+                const uint32_t keep = g == 0.0f ? 0u : ~0u;  // (0 whatever the logits are)
+#pragma unroll
+                for (int k = 0; k < NCH; ++k)
+                    if (k * CT < most) {
+                        Raw<T, E> o;
+                        times(e[k], f);
+                        o.set(e[k]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o.w[j] &= keep;
+                        if (k < n && !(k == 0 && part0))
+                            o.store(place + k * CT * E);
+                        else  // back to its place in the ring, which nothing overwrites yet
+                            o.store(mine + k * CT * E);
+                    }
+                const int chunks = view.chunks();
+                auto part = [&](int i) {
+                    Raw<T, E> o;
+                    o.load(mine + (i - tid) * E);
+                    view.store_part(i, o, p.classes, out);
+                };
+                if (part0 && n > 0) part(0);
+#pragma unroll 1
+                for (int i = tid + n * CT; i < chunks; i += CT) part(i);
+                named_bar_arrive(1 + H + h, CT + 32);
+            }
+            h = h == H - 1 ? 0 : h + 1;
+            buf = buf == C::SUMS - 1 ? 0 : buf + 1;
+        }
+        return;
+    }
+    const int h = (tid - CT) >> 5;
+    Slots s;
+    s.top = p.top;
+    s.top4 = (p.top + 3) & ~3;
+    s.id = reinterpret_cast<int*>(dynamic + C::STAGES * C::STAGE_CHUNKS) + h * s.top4 * 4;
+    s.p = reinterpret_cast<float*>(s.id + s.top4);
+    s.z = s.p + s.top4;
+    float* share = s.z + s.top4;
+    int buf = h;
+    // A lane's first slot and the row's weight are loaded a turn ahead, the student's logit behind
+    // the loss (a row's logits are overwritten only after its helper has come to its sums).
+    long long row = blockIdx.x + h * step, raw = -1;
+    float t0 = 0.0f, z0 = 0.0f, weight = 1.0f;
+    auto ahead = [&](long long r) {
+        raw = -1;
+        if (r >= p.rows) return;
+        if (MODE & GRAD && p.dloss) weight = p.dloss[r];
+        if (lane < s.top) {
+            raw = slot_class(p, r, lane);
+            t0 = slot_logit(p, r, lane);
+        }
+    };
+    auto gather = [&](long long r) {
+        const int id = slot_id(p, raw, t0);
+        if (id >= 0) z0 = element(z + r * p.pitch + id);
+    };
+    ahead(row);
+    gather(row);
+    for (; row < p.rows; row += H * step) {
+        const T* zrow = z + row * p.pitch;
+        const float g_row = weight;
+        if (lane < s.top4) {
+            s.id[lane] = slot_id(p, raw, t0);
+            s.p[lane] = t0;
+            s.z[lane] = z0;
+        }
+        ahead(row + H * step);
+        for (int k = lane + 32; k < s.top4; k += 32) {
+            float t = 0.0f;
+            const int id = k < s.top ? slot(p, row, k, t) : -1;
+            s.id[k] = id;
+            s.p[k] = t;
+            if (id >= 0) s.z[k] = element(zrow + id);
+        }
+        __syncwarp();
+        bool some;
+        const float entropy = teacher_side(s, p, lane, 32, some);
+        __syncwarp();
+        for (int k = lane; k < s.top; k += 32)
+            share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
+        const float g = some ? g_row * p.scale : 0.0f;
+        if (lane == 0) factor[h] = g;
+        named_bar_sync(1 + h, CT + 32);
+        float m, sum, loss = 0.0f;
+        joined(buf, m, sum);
+        const float ln_s = logf(sum);
+        for (int k = lane; k < s.top; k += 32)
+            if (share[k] > 0.0f || share[k] != share[k])
+                loss = fmaf(-share[k], (s.z[k] - m) * p.inv_t - ln_s, loss);
+        loss = lanes_sum(loss, 32) + entropy;
+        if (lane == 0) {
+            p.loss[row] = some ? p.t2 * loss : 0.0f;
+            if (p.lse) p.lse[row] = fmaf(m, p.inv_t, ln_s);
+        }
+        gather(row + H * step);
+        if (MODE & GRAD) {
+            named_bar_sync(1 + H + h, CT + 32);
+            T* out = static_cast<T*>(p.dz) + row * p.pitch;
+            const float inv_s = 1.0f / sum;
+            for (int k = lane; k < s.top && g != 0.0f; k += 32)
+                if (s.id[k] >= 0 && share[k] != -1.0f)
+                    put(out + s.id[k],
+                        g * (ex2_approx_ftz((s.z[k] - m) * p.c) * inv_s - share[k]));
+        }
+        __syncwarp();
+        buf += H;
+        if (buf >= C::SUMS) buf -= C::SUMS;
+    }
+}
+
+// Chunks of a row at most: one more than its bytes where rows do not begin on a chunk.
+int row_chunks(const DistillParams& p, int size) {
+    const long long bytes = p.pitch * size;
+    const bool whole = (static_cast<uintptr_t>(bytes) | reinterpret_cast<uintptr_t>(p.z)) % 16 == 0;
+    return static_cast<int>((bytes + 15) / 16) + (whole ? 0 : 1);
+}
+
+template <typename T, int MODE, int CT>
+cudaError_t launch_distill_ring(const DistillParams& p, int num_sms, cudaStream_t stream) {
+    using C = RingCfg<CT>;
+    auto* kern = distill_ring_kernel<T, MODE, CT>;
+    static std::atomic<unsigned long long> ready{0};  // once a device: the shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !((ready.load(std::memory_order_acquire) >> dev) & 1ull)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(C::smem(DISTILL_TOP)));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+    }
+    const long long most = static_cast<long long>(num_sms) * C::blocks((MODE & GRAD) && sizeof(T) == 2);
+    const dim3 g(static_cast<unsigned>(p.rows < most ? p.rows : most));
+    return launch_pdl(kern, g, dim3(C::THREADS), C::smem(p.top), stream, p,
+                      row_chunks(p, sizeof(T)));
+}
+
+// ------------------------------------------------------------------ short rows
+
+constexpr int TILE_THREADS = 256;
+
+// A tile of 256 / LANES rows a block.  The rows lie one after the other, so the tile is read and
+// written in whole chunks wherever its rows begin; in shared memory a row is LANES lanes of a warp, at
+// most W of its 4-byte words each, whose powers stay in registers, and the gradient takes the logits'
+// place.
+template <typename T, int MODE, int LANES, int W>
+__global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const DistillParams p) {
+    constexpr int E = RowView<T>::E, N = 4 / static_cast<int>(sizeof(T));
+    constexpr int ROWS = TILE_THREADS / LANES;
+    extern __shared__ int4 dynamic[];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int tid = threadIdx.x, tr = tid / LANES, lane = tid % LANES;
+    const long long row0 = static_cast<long long>(blockIdx.x) * ROWS, row = row0 + tr;
+    const int rows = p.rows - row0 < ROWS ? static_cast<int>(p.rows - row0) : ROWS;
+    const int pitch = static_cast<int>(p.pitch), top4 = (p.top + 3) & ~3;
+    const RowView<T> view(static_cast<const T*>(p.z), p.rows * p.pitch, row0 * p.pitch,
+                          rows * pitch);
+    const int chunks = view.chunks();
+    int4* tile = dynamic;
+    Slots s;
+    s.top = p.top;
+    s.top4 = top4;
+    s.id = reinterpret_cast<int*>(tile + (ROWS * pitch + E - 1) / E + 1) + tr * 4 * top4;
+    s.p = reinterpret_cast<float*>(s.id + top4);
+    s.z = s.p + top4;
+    float* share = s.z + top4;
+    // the logits and the slots
+    for (int i = tid; i < chunks; i += TILE_THREADS) {
+        if (!view.outside(i)) {
+            copy_async(tile + i, view.base + i * E);
+        } else {
+            Raw<T, E> r;
+            view.load_masked(i, view.n, r);
+            r.store(reinterpret_cast<T*>(tile + i));
+        }
+    }
+    copies_commit();
+    const bool active = tr < rows;
+    for (int k = lane; k < top4; k += LANES) {
+        float t = 0.0f;
+        s.id[k] = active && k < p.top ? slot(p, row, k, t) : -1;
+        s.p[k] = t;
+    }
+    float g = MODE & GRAD && p.dloss && active ? p.dloss[row] : 1.0f;
+    float lse = MODE == GRAD && active ? p.lse_in[row] : 0.0f;
+    __syncwarp();  // (a row's slots are its warp's own)
+    bool some;
+    const float entropy = teacher_side(s, p, lane, LANES, some);
+    copies_wait<0>();
+    __syncthreads();
+    // the row's words: `odd` elements of the row before it stand in the first one
+    T* mine = reinterpret_cast<T*>(tile) + view.head + tr * pitch;
+    const int odd = N == 2 ? (view.head + tr * pitch) & 1 : 0;
+    T* words = mine - odd;
+    float v[W][N];
+    Largest<T, N> largest;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        const int e0 = N * (lane + j * LANES) - odd;  // element of the word's first
+        Raw<T, N> r;
+        r.w[0] = N == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
+        if (active && e0 < p.classes) {
+            r.load(words + N * (lane + j * LANES));
+            if (N == 2) {
+                if (e0 < 0) r.w[0] = (r.w[0] & 0xFFFF0000u) | 0xFF80u;
+                if (e0 + 1 >= p.classes) r.w[0] = (r.w[0] & 0xFFFFu) | 0xFF800000u;
+            }
+        }
+        if (MODE & LOSS) largest.add(r);
+        r.values(v[j]);
+    }
+    float m = 0.0f, ln_s = 0.0f, inv_s = 1.0f;
+    if (MODE & LOSS) {
+        m = lanes_max(largest.get(), LANES);
+        const float at = m == -INFINITY ? 0.0f : m;
+        float2 sums = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < W; ++j) powers(v[j], at, p.c, sums);
+        const float sum = lanes_sum(sums.x + sums.y, LANES);
+        inv_s = 1.0f / sum;
+        ln_s = logf(sum);
+        lse = fmaf(m, p.inv_t, ln_s);
+    }
+    __syncwarp();  // (p of every slot)
+    g = some ? g * p.scale : 0.0f;
+    auto q_of = [&](float x) {
+        return MODE & LOSS ? ex2_approx_ftz((x - m) * p.c) * inv_s
+                           : ex2_approx_ftz(fmaf(x, p.inv_t, -lse) * LOG2E);
+    };
+    float loss = 0.0f;
+    for (int k = lane; k < p.top; k += LANES) {
+        share[k] = -1.0f;
+        if (s.id[k] < 0) continue;
+        const float f = class_share(s, k), zk = element(mine + s.id[k]);
+        share[k] = f;
+        s.z[k] = zk;
+        if (f > 0.0f || f != f) loss = fmaf(-f, (zk - m) * p.inv_t - ln_s, loss);
+    }
+    if (MODE & LOSS) {
+        loss = lanes_sum(loss, LANES) + entropy;
+        if (active && lane == 0) {
+            p.loss[row] = some ? p.t2 * loss : 0.0f;
+            if (p.lse) p.lse[row] = lse;
+        }
+    }
+    if (MODE & GRAD) {
+        __syncwarp();  // every slot's logit is read
+        const float gs = g * inv_s;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int e0 = N * (lane + j * LANES) - odd;
+            if (!active || e0 >= pitch) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (!(MODE & LOSS)) v[j][i] = q_of(v[j][i]);
+                v[j][i] = g == 0.0f || e0 + i >= p.classes ? 0.0f : v[j][i] * gs;
+            }
+            T* at = words + N * (lane + j * LANES);
+            if (N == 1 || (e0 >= 0 && e0 + 1 < pitch)) {
+                Raw<T, N> r;
+                r.set(v[j]);
+                r.store(at);
+            } else {  // a word that two rows share
+                if (e0 >= 0) put(at, v[j][0]);
+                else put(at + 1, v[j][N - 1]);
+            }
+        }
+        __syncwarp();
+        for (int k = lane; k < p.top && g != 0.0f; k += LANES)
+            if (s.id[k] >= 0 && share[k] != -1.0f)
+                put(mine + s.id[k], g * (q_of(s.z[k]) - share[k]));
+        __syncthreads();
+        T* out = static_cast<T*>(p.dz) + row0 * p.pitch;
+        const bool aligned = (reinterpret_cast<uintptr_t>(out - view.head) & 15u) == 0;
+        for (int i = tid; i < chunks; i += TILE_THREADS) {
+            Raw<T, E> r;
+            r.load(reinterpret_cast<const T*>(tile + i));
+            if (aligned && view.whole(i, view.n))
+                r.store(out - view.head + i * E);
+            else
+                view.store_part(i, r, view.n, out);
+        }
+    }
+}
+
+size_t tile_bytes(const DistillParams& p, int size, int lanes) {
+    const size_t rows = TILE_THREADS / lanes, top4 = (p.top + 3) & ~3;
+    return ((rows * p.pitch * size + 15) / 16 + 1) * 16 + rows * top4 * 16;
+}
+
+template <typename T, int MODE, int LANES, int W>
+cudaError_t launch_distill_tile(const DistillParams& p, cudaStream_t stream) {
+    constexpr int ROWS = TILE_THREADS / LANES;
+    return launch_pdl(distill_tile_kernel<T, MODE, LANES, W>,
+                      dim3(static_cast<unsigned>((p.rows + ROWS - 1) / ROWS)), dim3(TILE_THREADS),
+                      tile_bytes(p, sizeof(T), LANES), stream, p);
+}
+
+template <typename T, int MODE>
+cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_t stream) {
+    constexpr int size = static_cast<int>(sizeof(T));
+    constexpr size_t SMEM = 46 << 10;
+    // a row's words, with one that it may share: eight a lane, up to 32 of a whole warp
+    const bool even = (static_cast<uintptr_t>(p.pitch * size) | reinterpret_cast<uintptr_t>(p.z)) % 4 == 0;
+    const long long words = p.pitch * size / 4 + (even ? 0 : 1);
+    if (words <= 32 * 32) {
+        int lanes = 4;
+        while (lanes < 32 && (8 * lanes < words || 8 * lanes < p.top ||
+                              tile_bytes(p, size, lanes) > SMEM))
+            lanes *= 2;
+        if (tile_bytes(p, size, lanes) <= SMEM) {
+            switch (lanes) {
+                case 4: return launch_distill_tile<T, MODE, 4, 8>(p, stream);
+                case 8: return launch_distill_tile<T, MODE, 8, 8>(p, stream);
+                case 16: return launch_distill_tile<T, MODE, 16, 8>(p, stream);
+                default:
+                    return words <= 32 * 8 ? launch_distill_tile<T, MODE, 32, 8>(p, stream)
+                                           : launch_distill_tile<T, MODE, 32, 32>(p, stream);
+            }
+        }
+    }
+    // blocks of a row: as many as its chunks need to stay in registers, more while there are
+    // fewer blocks than SMs and a block keeps 256 chunks
+    const int n = row_chunks(p, size);
+    int parts = 1;
+    while (parts < ROW_CLUSTER &&
+           (n > parts * ROW_THREADS * 8 || (2 * parts * p.rows <= num_sms && n >= 512 * parts)))
+        parts *= 2;
+    const int per = (n + parts - 1) / parts;
+    if ((MODE & LOSS) && parts == 1) {
+        if constexpr ((MODE & LOSS) != 0) {
+            if (n <= 1024) return launch_distill_ring<T, MODE, 128>(p, num_sms, stream);
+            if (n <= 2048) return launch_distill_ring<T, MODE, 256>(p, num_sms, stream);
+            return launch_distill_ring<T, MODE, 512>(p, num_sms, stream);
+        }
+    }
+    const bool wide = per > 4 * ROW_THREADS;
+    int threads = (per + (wide ? 8 : 4) - 1) / (wide ? 8 : 4);
+    threads = threads < 128 ? 128 : threads > ROW_THREADS ? ROW_THREADS : (threads + 31) & ~31;
+    const size_t smem = static_cast<size_t>((p.top + 3) & ~3) * 16;
+    const dim3 g(static_cast<unsigned>(p.rows * parts)), b(static_cast<unsigned>(threads));
+    const unsigned cluster = MODE & LOSS ? static_cast<unsigned>(parts) : 1u;
+    return wide ? launch_pdl_cluster(distill_row_kernel<T, MODE, 8>, g, b, cluster, smem, stream, p,
+                                     parts)
+                : launch_pdl_cluster(distill_row_kernel<T, MODE, 4>, g, b, cluster, smem, stream, p,
+                                     parts);
+}
+
 template <typename T>
-cudaError_t launch_distill_t(const DistillParams& p, cudaStream_t stream) {
-    const dim3 g(static_cast<unsigned>(p.rows)), b(DISTILL_THREADS);
-    const size_t smem = static_cast<size_t>(p.top) * 12;
-    if (!p.dz) return launch_pdl(distill_kernel<T, LOSS>, g, b, smem, stream, p);
-    return p.loss ? launch_pdl(distill_kernel<T, LOSS | GRAD>, g, b, smem, stream, p)
-                  : launch_pdl(distill_kernel<T, GRAD>, g, b, smem, stream, p);
+cudaError_t launch_distill_t(const DistillParams& p, int num_sms, cudaStream_t stream) {
+    if (!p.dz) return launch_distill_mode<T, LOSS>(p, num_sms, stream);
+    return p.loss ? launch_distill_mode<T, LOSS | GRAD>(p, num_sms, stream)
+                  : launch_distill_mode<T, GRAD>(p, num_sms, stream);
 }
 
 }  // namespace
@@ -314,7 +1017,8 @@ cudaError_t launch_distill(const DistillArgs& a, int num_sms, cudaStream_t strea
     p.c = static_cast<float>(1.4426950408889634 / static_cast<double>(a.temperature));
     p.t2 = a.temperature * a.temperature;
     p.scale = a.scale * a.temperature;
-    return a.f32 ? launch_distill_t<float>(p, stream) : launch_distill_t<__nv_bfloat16>(p, stream);
+    return a.f32 ? launch_distill_t<float>(p, num_sms, stream)
+                 : launch_distill_t<__nv_bfloat16>(p, num_sms, stream);
 }
 
 }  // namespace quan
