@@ -544,6 +544,37 @@ quan_status_t quan_qpoint_f8_fwd(const void* x, const void* wq, const float* wsc
                                  quan_stream_t stream);
 
 /*
+ * Rows (pixels) of C channels held in 8 bits, as that product quantises its input: the values
+ * q e4m3 [rows][4][pitch] (device, 16-byte aligned), pitch = C/4 rounded up to 16, padding zero, and
+ * scale fp32 [4][ceil(C/4 / 128)][rows rounded up to 128] (what stands past the rows is not used).
+ * quan_f8_rows_bytes is the size of q, quan_f8_rows_scales the number of scales.
+ *
+ * quan_residual_join_f8_fwd is quan_residual_join_fwd whose n comes out in 8 bits: rounded to bf16
+ * and then quantised, which with groups = 4 gives the bits that quan_residual_join_fwd and the
+ * product's own quantisation give.  n: bf16 [rows][C], may be h itself when that is bf16, or NULL: n
+ * in 8 bits only.  pre, q and scale are needed, C is a multiple of 4, rows < 2^31; the rest as in
+ * quan_residual_join_fwd, whose gradients are this call's too.
+ * quan_f8_rows_dequant reads rows back: out bf16 [rows][C] (exact; a block of scale NaN is NaN).
+ * quan_qpoint_f8_rows_fwd is quan_qpoint_f8_fwd of such rows: no workspace, the same bits.
+ */
+size_t quan_f8_rows_bytes(long long rows, int C);
+size_t quan_f8_rows_scales(long long rows, int C);
+quan_status_t quan_residual_join_f8_fwd(const void* x, const void* h, const float* post,
+                                        const float* gate, const float* pre, long long rows,
+                                        int C, int groups, long long images, int dtype,
+                                        float alpha, float eps, float p, unsigned long long seed,
+                                        unsigned long long offset,
+                                        const unsigned long long* counter, void* y, void* n,
+                                        void* q, float* scale, quan_stream_t stream);
+quan_status_t quan_f8_rows_dequant(const void* q, const float* scale, long long rows, int C,
+                                   void* out, quan_stream_t stream);
+quan_status_t quan_qpoint_f8_rows_fwd(const void* xq, const float* xscale, const void* wq,
+                                      const float* wscale, const float* bias,
+                                      const float* iqbn_scale, const float* iqbn_shift,
+                                      long long rows, int Cin, int Cout, int act, void* out,
+                                      quan_stream_t stream);
+
+/*
  * Input gradient of that product: dx = dL/dx, bf16 [rows][Cin], from dy = dL/d(x W), bf16
  * [rows][Cout], which is quantised in the call as x is, and the letters of quan_f8_weights with
  * transpose 1.  Cin and Cout are the forward call's; the workspace has

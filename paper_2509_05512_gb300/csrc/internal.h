@@ -236,6 +236,9 @@ struct JoinArgs {
     bool f32;
     float alpha, eps;
     DropoutArgs drop;
+    // forward: n in 8 bits, laid out as the 8-bit product's rows, and out_n, if given, in bf16
+    void* q8;
+    float* s8;
 };
 bool join_supported(int C, int groups);
 cudaError_t launch_join_fwd(const JoinArgs& a, int num_sms, cudaStream_t stream);
@@ -269,7 +272,12 @@ cudaError_t read_and_clear_status_f8(unsigned* status, cudaStream_t stream);
 bool encode_bytes_3d(CUtensorMap* map, const void* base, const unsigned long long dims[3],
                      const unsigned long long strides[2], const unsigned box[3]);
 size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq);
-cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
+// Rows in 8 bits: words between the scales of two blocks, and the rows read back to bf16.
+long long f8_scale_pitch(long long rows);
+cudaError_t launch_f8_dequant(const void* q, const float* scale, long long rows, int Kq, void* out,
+                              cudaStream_t stream);
+// xscale: x is rows in 8 bits already, and these are their scales; no workspace then.
+cudaError_t launch_qpoint_f8(const void* x, const float* xscale, const void* wq, const float* ws,
                              const EpilogueArgs& ep, long long rows, int Kq, int Nq, bool conj,
                              int act, void* workspace, void* out, int num_sms,
                              unsigned long long wait_limit_ns, int inject_stall,

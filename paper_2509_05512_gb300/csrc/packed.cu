@@ -274,6 +274,36 @@ extern "C" int quan_packed_call(int op, const long long* words) {
             return quan_distill_fwd_bwd(d.z, d.index, d.teacher, dloss, QUAN_DISTILL_ARGS, scale,
                                         loss, dz, g.stream());
         }
+        case 21: {
+            void* x = g.ptr();
+            void* h = g.ptr();
+            const Join j(g);
+            void* y = g.ptr();
+            void* n = g.ptr();
+            void* q = g.ptr();
+            float* scale = g.f32();
+            return quan_residual_join_f8_fwd(x, h, QUAN_JOIN_ARGS, y, n, q, scale, g.stream());
+        }
+        case 22: {
+            void* q = g.ptr();
+            float* scale = g.f32();
+            const long long rows = g.next();
+            const int C = g.num();
+            void* out = g.ptr();
+            return quan_f8_rows_dequant(q, scale, rows, C, out, g.stream());
+        }
+        case 23: {
+            void* xq = g.ptr();
+            float* xscale = g.f32();
+            void* wq = g.ptr();
+            float* v[4];
+            for (auto& p : v) p = g.f32();
+            const long long rows = g.next();
+            const int Cin = g.num(), Cout = g.num(), act = g.num();
+            void* out = g.ptr();
+            return quan_qpoint_f8_rows_fwd(xq, xscale, wq, v[0], v[1], v[2], v[3], rows, Cin, Cout,
+                                           act, out, g.stream());
+        }
         default:
             return QUAN_ERR_INVALID_ARG;
     }

@@ -168,7 +168,10 @@ __global__ void __launch_bounds__(256) f8_letters_kernel(const F8Letters p) {
 // ------------------------------------------------------------------ the product
 
 struct F8Params {
-    const __nv_bfloat16* x;  // [rows][4 Kq]
+    const __nv_bfloat16* x;  // [rows][4 Kq], or null:
+    const uint8_t* xq;       // [rows][4][Kp]
+    const float* xs;         // [4][kblk][pitch]
+    long long pitch;
     const uint8_t* wq;       // [4][Nq][Kp]
     const float* ws;         // [4][nblk][kblk]
     EpilogueArgs ep;
@@ -204,9 +207,9 @@ __device__ __forceinline__ void f8_store(const F8Params& p, long long row, int c
 // A warp per quaternion output channel, RT rows a block: the block quantises its rows' channels
 // 512 at a time into shared memory (as the values they stand for), each lane multiplies four
 // channels of a block of 128, and the warp adds its lanes at the end.  Every product is exact in
-// fp32.
+// fp32.  Q8: the rows come in 8 bits and are only read back.
 constexpr int ROWS_K = 512;
-template <int RT, bool VEC>
+template <int RT, bool VEC, bool Q8>
 __global__ void __launch_bounds__(256) qpoint_rows_kernel(const F8Params p) {
     __shared__ float xs[RT][4][ROWS_K];
     griddep_launch_dependents();
@@ -221,6 +224,23 @@ __global__ void __launch_bounds__(256) qpoint_rows_kernel(const F8Params p) {
         for (int u = half; u < RT * 16; u += 16) {
             const int r = u >> 4, ci = (u >> 2) & 3, b = u & 3;
             const int k = k0 + b * F8_BLOCK + hl * 8;
+            if constexpr (Q8) {
+                const int kb = k0 / F8_BLOCK + b;
+                uint2 w = make_uint2(0u, 0u);
+                float s = 0.0f;
+                if (row0 + r < p.rows && k < p.Kp) {
+                    w = *reinterpret_cast<const uint2*>(p.xq + ((row0 + r) * 4 + ci) * p.Kp + k);
+                    s = p.xs[(static_cast<long long>(ci) * p.kblk + kb) * p.pitch + row0 + r];
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float d[4];
+                    f8x4_to_f32(j ? w.y : w.x, d);
+                    *reinterpret_cast<float4*>(&xs[r][ci][b * F8_BLOCK + hl * 8 + 4 * j]) =
+                        make_float4(d[0] * s, d[1] * s, d[2] * s, d[3] * s);
+                }
+                continue;
+            }
             float v[8], inv;
             if (row0 + r < p.rows) {
                 load_x8<VEC>(p.x + (row0 + r) * (4LL * p.Kq) + ci * p.Kq, k, p.Kq, v);
@@ -311,8 +331,9 @@ template <int RT>
 cudaError_t launch_rows(const F8Params& p, bool vec, cudaStream_t stream) {
     const dim3 g(static_cast<unsigned>((p.rows + RT - 1) / RT),
                  static_cast<unsigned>((p.Nq + 7) / 8));
-    return vec ? launch_pdl(qpoint_rows_kernel<RT, true>, g, dim3(256), 0, stream, p)
-               : launch_pdl(qpoint_rows_kernel<RT, false>, g, dim3(256), 0, stream, p);
+    if (p.xq) return launch_pdl(qpoint_rows_kernel<RT, true, true>, g, dim3(256), 0, stream, p);
+    return vec ? launch_pdl(qpoint_rows_kernel<RT, true, false>, g, dim3(256), 0, stream, p)
+               : launch_pdl(qpoint_rows_kernel<RT, false, false>, g, dim3(256), 0, stream, p);
 }
 
 // ------------------------------------------------------------------ rows in 8 bits
@@ -394,6 +415,63 @@ cudaError_t launch_f8_rows(F8Rows r, cudaStream_t stream) {
     }
 }
 
+// Rows read back: a thread takes 16 channels of a component (a 16-byte load, LV channels a store) of
+// F8_ROWS_UNROLL rows, as above.  Bound by HBM: 1 byte read, 2 written a channel.
+struct F8Dequant {
+    const uint8_t* q;    // [rows][4][Kp]
+    const float* scale;  // [4][kblk][pitch]
+    __nv_bfloat16* out;  // [rows][4 Kq]
+    long long rows, pitch;
+    int Kq, Kp, kblk;
+    int group;  // rows side by side in a block of threads
+};
+
+template <int LV>
+__global__ void __launch_bounds__(256) f8_dequant_kernel(const F8Dequant p) {
+    griddep_launch_dependents();
+    griddep_wait();
+    const unsigned units = p.Kp / 16, per_row = 4u * units;
+    const unsigned unit = blockIdx.y * 256u + threadIdx.x;
+    const unsigned r0 = unit / per_row, rest = unit - r0 * per_row;
+    const unsigned ci = rest / units, k = (rest - ci * units) * 16;
+    if (r0 >= static_cast<unsigned>(p.group)) return;
+    const long long row0 = static_cast<long long>(blockIdx.x) * (p.group * F8_ROWS_UNROLL) + r0;
+    uint4 w[F8_ROWS_UNROLL];
+    float s[F8_ROWS_UNROLL];
+#pragma unroll
+    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
+        const long long row = row0 + i * p.group;
+        if (row >= p.rows) break;
+        w[i] = *reinterpret_cast<const uint4*>(p.q + (row * 4 + ci) * p.Kp + k);
+        s[i] = p.scale[(static_cast<long long>(ci) * p.kblk + k / F8_BLOCK) * p.pitch + row];
+    }
+#pragma unroll
+    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
+        const long long row = row0 + i * p.group;
+        if (row >= p.rows) break;
+        __nv_bfloat16* out = p.out + row * (4LL * p.Kq) + static_cast<long long>(ci) * p.Kq + k;
+        const uint32_t word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float d[4];
+            f8x4_to_f32(word[j], d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * j + e] = d[e] * s[i];
+        }
+#pragma unroll
+        for (int j = 0; j < 16; j += LV) {
+            if (static_cast<int>(k) + j >= p.Kq) break;
+            float part[LV];
+#pragma unroll
+            for (int e = 0; e < LV; ++e) part[e] = v[j + e];
+            Raw<__nv_bfloat16, LV> o;
+            o.set(part);
+            o.store(out + j);
+        }
+    }
+}
+
 #include "qpoint_f8_tc.cuh"
 
 int blocks_of(int q) { return (q + F8_BLOCK - 1) / F8_BLOCK; }
@@ -401,6 +479,26 @@ int blocks_of(int q) { return (q + F8_BLOCK - 1) / F8_BLOCK; }
 }  // namespace
 
 int f8_pitch(int Kq) { return (Kq + 15) / 16 * 16; }
+
+// Whole tiles of rows, so that a tile's scales are read without a bound (what stands past the rows is
+// never used).
+long long f8_scale_pitch(long long rows) { return (rows + F8_BM - 1) / F8_BM * F8_BM; }
+
+cudaError_t launch_f8_dequant(const void* q, const float* scale, long long rows, int Kq, void* out,
+                              cudaStream_t stream) {
+    F8Dequant p = {static_cast<const uint8_t*>(q), scale, static_cast<__nv_bfloat16*>(out), rows,
+                   f8_scale_pitch(rows), Kq, f8_pitch(Kq), blocks_of(Kq), 0};
+    const int per_row = p.Kp / 4;
+    p.group = per_row < 256 ? 256 / per_row : 1;
+    const dim3 g(static_cast<unsigned>((rows + p.group * F8_ROWS_UNROLL - 1) /
+                                       (p.group * F8_ROWS_UNROLL)),
+                 static_cast<unsigned>((per_row + 255) / 256));
+    switch (load_channels(Kq, reinterpret_cast<uintptr_t>(out))) {
+        case 8: return launch_pdl(f8_dequant_kernel<8>, g, dim3(256), 0, stream, p);
+        case 2: return launch_pdl(f8_dequant_kernel<2>, g, dim3(256), 0, stream, p);
+        default: return launch_pdl(f8_dequant_kernel<1>, g, dim3(256), 0, stream, p);
+    }
+}
 
 cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool transpose, void* q,
                               float* scale, cudaStream_t stream) {
@@ -441,10 +539,6 @@ bool f8_few_rows(long long rows, int Kq, int Nq) {
 size_t quantised_bytes(long long rows, int Kq) {
     return (static_cast<size_t>(rows) * 4 * f8_pitch(Kq) + 255) / 256 * 256;
 }
-
-// Rows of the scales: whole tiles, so that a tile's are read without a bound (what stands past the
-// rows is never used).
-long long scale_pitch(long long rows) { return (rows + F8_BM - 1) / F8_BM * F8_BM; }
 
 // Quaternion output channels of a tile, by the estimated time of the waves of tiles (1280 rows
 // 4096 -> 1024: 23.4, 18.8 and 25.3 us with 64, 32 and 16; 128 rows: 20.4, 15.9, 13.5; 20,000 rows
@@ -502,10 +596,10 @@ cudaError_t launch_f8_tc(const CUtensorMap& mx, const CUtensorMap& mw, const F8T
 
 size_t qpoint_f8_workspace_bytes(long long rows, int Kq, int Nq) {
     if (f8_few_rows(rows, Kq, Nq)) return 0;
-    return quantised_bytes(rows, Kq) + static_cast<size_t>(scale_pitch(rows)) * 4 * blocks_of(Kq) * 4;
+    return quantised_bytes(rows, Kq) + static_cast<size_t>(f8_scale_pitch(rows)) * 4 * blocks_of(Kq) * 4;
 }
 
-cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
+cudaError_t launch_qpoint_f8(const void* x, const float* xscale, const void* wq, const float* ws,
                              const EpilogueArgs& ep, long long rows, int Kq, int Nq, bool conj,
                              int act, void* workspace, void* out, int num_sms,
                              unsigned long long wait_limit_ns, int inject_stall,
@@ -514,19 +608,27 @@ cudaError_t launch_qpoint_f8(const void* x, const void* wq, const float* ws,
     const bool vec = Kq % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
     auto* xb = static_cast<const __nv_bfloat16*>(x);
     auto* ob = static_cast<__nv_bfloat16*>(out);
+    const long long pitch = f8_scale_pitch(rows);
     if (f8_few_rows(rows, Kq, Nq)) {
-        const F8Params p = {xb, static_cast<const uint8_t*>(wq), ws, ep, ob, rows, Kq, Nq, Kp,
-                            kblk, nblk, conj ? 1 : 0, act};
+        const F8Params p = {xscale ? nullptr : xb,
+                            xscale ? static_cast<const uint8_t*>(x) : nullptr,
+                            xscale, pitch, static_cast<const uint8_t*>(wq), ws, ep, ob, rows, Kq,
+                            Nq, Kp, kblk, nblk, conj ? 1 : 0, act};
         return rows == 1 ? launch_rows<1>(p, vec, stream) : launch_rows<4>(p, vec, stream);
     }
-    auto* xq = static_cast<uint8_t*>(workspace);
-    auto* xs = reinterpret_cast<float*>(xq + quantised_bytes(rows, Kq));
-    const long long pitch = scale_pitch(rows);
-    const F8Rows r = {xb, xq, xs, rows, pitch, Kq, Kp, kblk, 0};
-    const cudaError_t e = Kq <= 32   ? launch_f8_rows<4>(r, stream)
-                          : Kq <= 64 ? launch_f8_rows<8>(r, stream)
-                                     : launch_f8_rows<16>(r, stream);
-    if (e != cudaSuccess) return e;
+    const void* xq = x;
+    const float* xs = xscale;
+    if (!xscale) {
+        auto* q = static_cast<uint8_t*>(workspace);
+        auto* s = reinterpret_cast<float*>(q + quantised_bytes(rows, Kq));
+        const F8Rows r = {xb, q, s, rows, pitch, Kq, Kp, kblk, 0};
+        const cudaError_t e = Kq <= 32   ? launch_f8_rows<4>(r, stream)
+                              : Kq <= 64 ? launch_f8_rows<8>(r, stream)
+                                         : launch_f8_rows<16>(r, stream);
+        if (e != cudaSuccess) return e;
+        xq = q;
+        xs = s;
+    }
 
     const int bnq = f8_tile_width(rows, Kq, Nq, num_sms);
     CUtensorMap mx, mw;

@@ -422,9 +422,18 @@ bool misaligned(const void* const* t, int n, size_t align) {
 // Channel counts of the 8-bit product (its launches' grids hold more).
 constexpr int F8_MAX_CHANNELS = 1 << 20;
 
+// Bytes of rows of C channels in 8 bits, and the number of their scales.
+size_t f8_rows_bytes(long long rows, int C) {
+    return static_cast<size_t>(rows) * 4 * quan::f8_pitch(C / 4);
+}
+size_t f8_scales(long long rows, int C) {
+    return static_cast<size_t>(quan::f8_scale_pitch(rows)) * 4 * ((C / 4 + 127) / 128);
+}
+
 // The product both directions of the 8-bit pointwise convolution run: K input and N output
 // channels of the call.
-quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
+quan_status_t run_qpoint_f8(const void* x, const float* xscale, const void* wq,
+                            const float* wscale,
                             const quan::EpilogueArgs& ep, long long rows, int K, int N, int act,
                             bool conj, void* workspace, size_t workspace_bytes, void* out,
                             quan_stream_t stream) {
@@ -442,13 +451,13 @@ quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
     if (rows >= (1LL << 31) || rows >= (1LL << 40) / K || rows >= (1LL << 40) / N ||
         K > F8_MAX_CHANNELS || N > F8_MAX_CHANNELS)
         return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
-    const void* half[] = {x, out};
-    const void* vectors[] = {wscale, ep.bias, ep.scale, ep.shift};
-    if (misaligned(half, 2, 2) || misaligned(vectors, 4, 4) || misaligned(&wq, 1, 16))
+    const void* vectors[] = {wscale, ep.bias, ep.scale, ep.shift, xscale};
+    if (misaligned(&x, 1, xscale ? 16 : 2) || misaligned(&out, 1, 2) ||
+        misaligned(vectors, 5, 4) || misaligned(&wq, 1, 16))
         return fail(QUAN_ERR_INVALID_ARG,
-                    "tensors must be aligned to their elements, the 8-bit letters to 16 bytes");
+                    "tensors must be aligned to their elements, 8-bit ones to 16 bytes");
     const int Kq = K / 4, Nq = N / 4;
-    const size_t need = quan::qpoint_f8_workspace_bytes(rows, Kq, Nq);
+    const size_t need = xscale ? 0 : quan::qpoint_f8_workspace_bytes(rows, Kq, Nq);
     if (need > 0 && (!workspace || workspace_bytes < need ||
                      reinterpret_cast<uintptr_t>(workspace) % 256 != 0))
         return fail(QUAN_ERR_INVALID_ARG,
@@ -458,10 +467,11 @@ quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
     const size_t sb = size_t(16) * ((Nq + 127) / 128) * ((Kq + 127) / 128), cb = size_t(4) * N;
     const Span outs[] = {{out, static_cast<size_t>(rows) * N * 2},
                          {need ? workspace : nullptr, need}};
-    const Span ins[] = {{x, static_cast<size_t>(rows) * K * 2}, {wq, wb}, {wscale, sb},
-                        {ep.bias, cb}, {ep.scale, cb}, {ep.shift, cb}};
+    const Span ins[] = {{x, xscale ? f8_rows_bytes(rows, K) : static_cast<size_t>(rows) * K * 2},
+                        {wq, wb}, {wscale, sb}, {ep.bias, cb}, {ep.scale, cb}, {ep.shift, cb},
+                        {xscale, f8_scales(rows, K) * 4}};
     const unsigned equal[] = {0u, 0u};
-    if (clash(outs, 2, ins, 6, equal))
+    if (clash(outs, 2, ins, 7, equal))
         return fail(QUAN_ERR_INVALID_ARG, "out or the workspace overlaps another tensor");
     int num_sms = 0, cc = 0;
     cudaError_t e;
@@ -469,7 +479,7 @@ quan_status_t run_qpoint_f8(const void* x, const void* wq, const float* wscale,
     if (cc != 103)
         return fail(QUAN_ERR_UNSUPPORTED, "the 8-bit product needs sm_103 (device cc %d)", cc);
     char err[256] = "";
-    e = quan::launch_qpoint_f8(x, wq, wscale, ep, rows, Kq, Nq, conj, act, workspace, out,
+    e = quan::launch_qpoint_f8(x, xscale, wq, wscale, ep, rows, Kq, Nq, conj, act, workspace, out,
                                num_sms, g_wait_limit.load(), g_inject.load(),
                                reinterpret_cast<cudaStream_t>(stream), err, sizeof(err));
     if (err[0] != '\0') return fail(QUAN_ERR_UNSUPPORTED, "%s", err);
@@ -1054,6 +1064,56 @@ quan_status_t quan_residual_join_fwd(const void* x, const void* h, const float* 
     return QUAN_OK;
 }
 
+quan_status_t quan_residual_join_f8_fwd(const void* x, const void* h, const float* post,
+                                        const float* gate, const float* pre, long long rows,
+                                        int C, int groups, long long images, int dtype,
+                                        float alpha, float eps, float p, unsigned long long seed,
+                                        unsigned long long offset,
+                                        const unsigned long long* counter, void* y, void* n,
+                                        void* q, float* scale, quan_stream_t stream) {
+    quan::JoinArgs a = {};
+    const quan_status_t st = check_join(&a, rows, C, groups, images, dtype, alpha, eps, p, seed,
+                                        offset, counter);
+    if (st != QUAN_OK) return st;
+    if (C % 4) return fail(QUAN_ERR_INVALID_ARG, "C=%d must be a multiple of 4", C);
+    if (rows >= (1LL << 31) || !quan::join_supported(C, 4))
+        return fail(QUAN_ERR_UNSUPPORTED, "tensor too large for 8-bit rows");
+    if (rows == 0) return QUAN_OK;
+    if (!x || (h != nullptr) != (y != nullptr) || !pre || !q || !scale || (!h && (post || gate)))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "x, pre, q and scale are needed, y exactly with h, post and gate only with h");
+    const size_t e = a.f32 ? 4 : 2, t = static_cast<size_t>(rows) * C * e;
+    const void* tensors[] = {x, h, y};
+    const void* vectors[] = {post, gate, pre, scale};
+    if (misaligned(tensors, 3, e) || misaligned(vectors, 4, 4) ||
+        misaligned(const_cast<const void* const*>(&n), 1, 2) ||
+        misaligned(const_cast<const void* const*>(&q), 1, 16))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "tensors must be aligned to their elements, 8-bit rows to 16 bytes");
+    const size_t cb = static_cast<size_t>(C) * 4;
+    const Span outs[] = {{y, t}, {n, static_cast<size_t>(rows) * C * 2},
+                         {q, f8_rows_bytes(rows, C)}, {scale, f8_scales(rows, C) * 4}};
+    const Span ins[] = {{x, t}, {h, t}, {post, cb}, {gate, cb * images}, {pre, cb}, {counter, 8}};
+    const unsigned equal[] = {1u, a.f32 ? 0u : 2u, 0u, 0u};
+    if (clash(outs, 4, ins, 6, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "an output overlaps another tensor");
+    int num_sms = 0, cc = 0;
+    cudaError_t ce;
+    if (!device_info(&num_sms, &cc, &ce)) return cuda_fail(ce, "device query");
+    a.x = x;
+    a.h = h;
+    a.post = post;
+    a.gate = gate;
+    a.pre = pre;
+    a.out_y = y;
+    a.out_n = n;
+    a.q8 = q;
+    a.s8 = scale;
+    ce = quan::launch_join_fwd(a, num_sms, reinterpret_cast<cudaStream_t>(stream));
+    if (ce != cudaSuccess) return cuda_fail(ce, "residual join launch");
+    return QUAN_OK;
+}
+
 size_t quan_residual_join_bwd_workspace_size(long long rows, int C, int groups,
                                              long long images) {
     if (rows < 0 || C < 1 || (groups != 1 && groups != 4) || C % groups != 0 || images < 1 ||
@@ -1168,14 +1228,56 @@ quan_status_t quan_qpoint_f8_fwd(const void* x, const void* wq, const float* wsc
                                  const float* iqbn_shift, long long rows, int Cin, int Cout,
                                  int act, void* workspace, size_t workspace_bytes, void* out,
                                  quan_stream_t stream) {
-    return run_qpoint_f8(x, wq, wscale, {bias, iqbn_scale, iqbn_shift, nullptr}, rows, Cin, Cout,
+    return run_qpoint_f8(x, nullptr, wq, wscale, {bias, iqbn_scale, iqbn_shift, nullptr}, rows, Cin, Cout,
                          act, false, workspace, workspace_bytes, out, stream);
+}
+
+quan_status_t quan_qpoint_f8_rows_fwd(const void* xq, const float* xscale, const void* wq,
+                                      const float* wscale, const float* bias,
+                                      const float* iqbn_scale, const float* iqbn_shift,
+                                      long long rows, int Cin, int Cout, int act, void* out,
+                                      quan_stream_t stream) {
+    if (rows > 0 && !xscale) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    return run_qpoint_f8(xq, xscale, wq, wscale, {bias, iqbn_scale, iqbn_shift, nullptr}, rows,
+                         Cin, Cout, act, false, nullptr, 0, out, stream);
+}
+
+size_t quan_f8_rows_bytes(long long rows, int C) {
+    return rows < 1 || C < 1 || C % 4 ? 0 : f8_rows_bytes(rows, C);
+}
+
+size_t quan_f8_rows_scales(long long rows, int C) {
+    return rows < 1 || C < 1 || C % 4 ? 0 : f8_scales(rows, C);
+}
+
+quan_status_t quan_f8_rows_dequant(const void* q, const float* scale, long long rows, int C,
+                                   void* out, quan_stream_t stream) {
+    if (rows < 0 || C < 1 || C % 4)
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "rows=%lld must be >= 0, C=%d a positive multiple of 4", rows, C);
+    if (rows == 0) return QUAN_OK;
+    if (!q || !scale || !out) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    if (rows >= (1LL << 31) || rows >= (1LL << 40) / C || C > F8_MAX_CHANNELS)
+        return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
+    if (misaligned(&q, 1, 16) || reinterpret_cast<uintptr_t>(scale) % 4 != 0 ||
+        misaligned(const_cast<const void* const*>(&out), 1, 2))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "the 8-bit rows must be 16-byte aligned, scales and out to their elements");
+    const Span outs[] = {{out, static_cast<size_t>(rows) * C * 2}};
+    const Span ins[] = {{q, f8_rows_bytes(rows, C)}, {scale, f8_scales(rows, C) * 4}};
+    const unsigned equal[] = {0u};
+    if (clash(outs, 1, ins, 2, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "out overlaps the 8-bit rows or their scales");
+    const cudaError_t e = quan::launch_f8_dequant(q, scale, rows, C / 4, out,
+                                                  reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "f8 rows launch");
+    return QUAN_OK;
 }
 
 quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const float* wscale,
                                       long long rows, int Cin, int Cout, void* workspace,
                                       size_t workspace_bytes, void* dx, quan_stream_t stream) {
-    return run_qpoint_f8(dy, wq, wscale, {nullptr, nullptr, nullptr, nullptr}, rows, Cout, Cin,
+    return run_qpoint_f8(dy, nullptr, wq, wscale, {nullptr, nullptr, nullptr, nullptr}, rows, Cout, Cin,
                          QUAN_ACT_NONE, true, workspace, workspace_bytes, dx, stream);
 }
 

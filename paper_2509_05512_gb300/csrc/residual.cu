@@ -30,6 +30,7 @@
 
 #include <atomic>
 
+#include "f8.cuh"
 #include "internal.h"
 #include "philox.cuh"
 #include "ptx.cuh"
@@ -140,6 +141,11 @@ struct JoinParams {
     long long part_stride;             // between the rows of two blocks
     float alpha, eps, inv_s;
     DropoutArgs drop;
+    // the norm in 8 bits as well: its values, scales and the lanes that a statistic takes (below)
+    uint8_t* q8;
+    float* s8;
+    long long s8_pitch;
+    int q8_pitch, kblk, red;
 };
 
 // Where a thread stands: its slot (row of the block's rows), group and chunks.
@@ -225,8 +231,51 @@ __device__ __forceinline__ void draw_from(Dropout8& m, const DropoutArgs& d,
     }
 }
 
-template <typename T, int LV, int NC, bool CROSS>
+// A thread's eight channels from `col` on of the norm, in 8 bits: rounded to bf16 first, so that the
+// values are those that quantising the bf16 norm gives; the largest magnitude of a block of 128 by
+// the up to 16 lanes that hold it.
+template <int LV>
+__device__ __forceinline__ void store_f8(const JoinParams& p, const Place& q, long long row, int col,
+                                         int left, bool active, const float (&v)[8],
+                                         __nv_bfloat16* n) {
+    uint32_t w[4], m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        w[j] = f32_to_bf16x2(2 * j < left ? v[2 * j] : 0.0f, 2 * j + 1 < left ? v[2 * j + 1] : 0.0f);
+        m = __vmaxu2(m, w[j] & 0x7FFF7FFFu);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1)
+        if (o < p.tps) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float inv;
+    const float s = f8_scale(__uint_as_float(max(m << 16, m & 0xFFFF0000u)), inv);
+    uint32_t h[4];
+    float r[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        bf16x2_to_f32(w[j], r[2 * j], r[2 * j + 1]);
+        h[j] = f8x2_from_f32(r[2 * j] * inv, r[2 * j + 1] * inv);
+    }
+    if (!active) return;
+    if (col % F8_BLOCK == 0 && left > 0)
+        p.s8[(static_cast<long long>(q.seg) * p.kblk + col / F8_BLOCK) * p.s8_pitch + row] = s;
+    if (col < p.q8_pitch)
+        *reinterpret_cast<uint2*>(p.q8 + (row * 4 + q.seg) * p.q8_pitch + col) =
+            make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+    if (p.tps == 1)  // (one lane, the other half of 16 channels)
+        *reinterpret_cast<uint2*>(p.q8 + (row * 4 + q.seg) * p.q8_pitch + 8) = make_uint2(0u, 0u);
+    if (n) {
+        Chunk<__nv_bfloat16, LV> o;
+        o.set_store(r, n + row * p.C + q.seg * p.S + col, left);
+    }
+}
+
+// F8: the norm in 8 bits, and in bf16 where out_n is given.  A row is cut into its four components
+// whatever its statistics are, so that a block of 128 is 16 neighbouring lanes; a statistic of the
+// whole row takes the lanes of all four.
+template <typename T, int LV, int NC, bool CROSS, bool F8>
 __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinParams p) {
+    const int red = F8 ? p.red : p.tps;
     __shared__ float sm[2][96];
     int turn = 0;
     griddep_launch_dependents();
@@ -291,7 +340,7 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
                 for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) ss[0] = fmaf(u[c][j], u[c][j], ss[0]);
-                group_sum<CROSS, 1>(ss, p.tps, sm, turn);
+                group_sum<CROSS, 1>(ss, red, sm, turn);
                 r1 = rsqrtf(fmaf(ss[0], p.inv_s, p.eps));
             }
 #pragma unroll
@@ -309,19 +358,23 @@ __global__ void __launch_bounds__(CROSS ? 512 : 256) join_fwd_kernel(const JoinP
                 o.set_store(v[c], y + at + col, left[c]);
             }
         }
-        if (n) {
+        if (F8 || n) {
             float ss[1] = {0.0f};
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) ss[0] = fmaf(v[c][j], v[c][j], ss[0]);
-            group_sum<CROSS, 1>(ss, p.tps, sm, turn);
+            group_sum<CROSS, 1>(ss, red, sm, turn);
             const float r2 = rsqrtf(fmaf(ss[0], p.inv_s, p.eps));
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[c][j] *= r2 * pre[c][j];
-                o.set_store(v[c], n + at + (q.ts + c * p.tps) * 8, left[c]);
+                if constexpr (F8)
+                    store_f8<LV>(p, q, row, (q.ts + c * p.tps) * 8, left[c], active, v[c],
+                                 static_cast<__nv_bfloat16*>(p.out_n));
+                else
+                    o.set_store(v[c], n + at + (q.ts + c * p.tps) * 8, left[c]);
             }
         }
     }
@@ -617,6 +670,25 @@ int load_width(int S, int C, const void* const* t, int n) {
 // where its sums cross warps.  Forward, a block takes rows until none is left, and there are as many
 // blocks as run at once (`blocks` at most): with twice as many the last ones run by themselves
 // (32 x 56 x 56 x 256: 40 us, 38 with one wave).
+template <typename T, int LV, int NC, bool CROSS, bool F8>
+cudaError_t launch_join_fwd_nc(const JoinParams& p, const JoinPlan& pl, long long blocks,
+                               int num_sms, cudaStream_t stream) {
+    auto* kern = join_fwd_kernel<T, LV, NC, CROSS, F8>;
+    static std::atomic<int> at_once[2];  // blocks an SM, of 256 and of 512 threads
+    std::atomic<int>& known = at_once[pl.threads > 256];
+    int per_sm = known.load(std::memory_order_relaxed);
+    if (per_sm == 0) {
+        const cudaError_t e =
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, pl.threads, 0);
+        if (e != cudaSuccess) return e;
+        if (per_sm < 1) per_sm = 1;
+        known.store(per_sm, std::memory_order_relaxed);
+    }
+    const long long cap = static_cast<long long>(num_sms) * per_sm;
+    return launch_pdl(kern, dim3(static_cast<unsigned>(blocks < cap ? blocks : cap)),
+                      dim3(static_cast<unsigned>(pl.threads)), 0, stream, p);
+}
+
 template <typename T, int LV, int NC, bool CROSS>
 cudaError_t launch_join_nc(const JoinParams& p, const JoinPlan& pl, bool backward,
                            long long blocks, int num_sms, cudaStream_t stream) {
@@ -626,19 +698,8 @@ cudaError_t launch_join_nc(const JoinParams& p, const JoinPlan& pl, bool backwar
         return launch_pdl(join_bwd_kernel<T, LV, NC, CROSS>,
                           dim3(static_cast<unsigned>(blocks)), b, smem, stream, p);
     }
-    static std::atomic<int> at_once[2];  // blocks an SM, of 256 and of 512 threads
-    std::atomic<int>& known = at_once[pl.threads > 256];
-    int per_sm = known.load(std::memory_order_relaxed);
-    if (per_sm == 0) {
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(
-            &per_sm, join_fwd_kernel<T, LV, NC, CROSS>, pl.threads, 0);
-        if (e != cudaSuccess) return e;
-        if (per_sm < 1) per_sm = 1;
-        known.store(per_sm, std::memory_order_relaxed);
-    }
-    const long long cap = static_cast<long long>(num_sms) * per_sm;
-    return launch_pdl(join_fwd_kernel<T, LV, NC, CROSS>,
-                      dim3(static_cast<unsigned>(blocks < cap ? blocks : cap)), b, 0, stream, p);
+    return p.q8 ? launch_join_fwd_nc<T, LV, NC, CROSS, true>(p, pl, blocks, num_sms, stream)
+                : launch_join_fwd_nc<T, LV, NC, CROSS, false>(p, pl, blocks, num_sms, stream);
 }
 
 template <typename T, int LV>
@@ -646,7 +707,7 @@ cudaError_t launch_join_lv(const JoinParams& p, const JoinPlan& pl, bool backwar
                            long long blocks, int num_sms, cudaStream_t stream) {
     if (pl.nc == 2)
         return launch_join_nc<T, LV, 2, true>(p, pl, backward, blocks, num_sms, stream);
-    return pl.tps > 32
+    return (p.q8 ? p.red : pl.tps) > 32
                ? launch_join_nc<T, LV, 1, true>(p, pl, backward, blocks, num_sms, stream)
                : launch_join_nc<T, LV, 1, false>(p, pl, backward, blocks, num_sms, stream);
 }
@@ -675,16 +736,33 @@ void fill(JoinParams* p, const JoinArgs& a, const JoinPlan& pl) {
     p->C = a.C;
     p->S = a.C / a.groups;
     p->groups = a.groups;
+    p->red = pl.tps;
+    if (a.q8) {
+        p->S = a.C / 4;
+        p->groups = 4;
+        if (a.groups == 1) p->red = 4 * pl.tps;
+        p->q8 = static_cast<uint8_t*>(a.q8);
+        p->s8 = a.s8;
+        p->s8_pitch = f8_scale_pitch(a.rows);
+        p->q8_pitch = f8_pitch(p->S);
+        p->kblk = (p->S + F8_BLOCK - 1) / F8_BLOCK;
+    }
     p->tps = pl.tps;
     p->slots = pl.slots;
     p->alpha = a.alpha;
     p->eps = a.eps;
-    p->inv_s = 1.0f / static_cast<float>(p->S);
+    p->inv_s = 1.0f / static_cast<float>(a.C / a.groups);
     p->drop = a.drop;
 }
 
 int join_load_width(const JoinArgs& a) {
     const void* t[] = {a.x, a.h, a.y, a.dy, a.dn, a.out_y, a.out_n};
+    if (a.q8) {  // its rows begin with each component, and n is bf16
+        const int S = a.C / 4, n = load_width<__nv_bfloat16>(S, a.C, t + 6, 1);
+        const int w = a.f32 ? load_width<float>(S, a.C, t, 6)
+                            : load_width<__nv_bfloat16>(S, a.C, t, 6);
+        return n < w ? n : w;
+    }
     return a.f32 ? load_width<float>(a.C / a.groups, a.C, t, 7)
                  : load_width<__nv_bfloat16>(a.C / a.groups, a.C, t, 7);
 }
@@ -734,7 +812,7 @@ bool join_supported(int C, int groups) {
 cudaError_t launch_join_fwd(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     if (a.rows == 0) return cudaSuccess;
     JoinPlan pl;
-    join_plan(a.C, a.groups, &pl);
+    join_plan(a.C, a.q8 ? 4 : a.groups, &pl);
     JoinParams p = {};
     fill(&p, a, pl);
     const long long blocks = (a.rows + pl.slots - 1) / pl.slots;

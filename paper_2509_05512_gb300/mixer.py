@@ -3,7 +3,9 @@ each joined to the stream with a norm, a gate and dropout, and followed by the n
 
     n_0 = norm(x);   h_l = n_l W_l;   y_l, n_(l+1) = join(y_(l-1), h_l)      (y_(-1) = x)
 
-One block is three launches forward (rows to 8 bits, product, join) and seven backward.  The
+One block is two launches forward, the product and the join, which writes the next block's rows in 8
+bits beside bf16 (for the weight gradient); with a statistic over the whole row (groups=1), where
+that join sums in another order, the product quantises its rows itself.  Backward it is seven.  The
 letters are kept in bf16 and quantised once per update (`quantize`), both ways round; the weight
 gradients come from the bf16 weight-gradient kernel.  Every mask is a function of the seed, the
 block and a device counter that `forward` leaves to `advance`, so that a captured training step
@@ -57,15 +59,22 @@ class Mixer:
         """bf16 x [N, H, W, channels] (CUDA) -> the last norm's output; keeps what `backward`
         needs."""
         self.training = training
-        _, n = quan.residual_join(x, pre=self.pre[0], groups=self.groups, eps=self.eps)
+        _, n, rows = self._norm(0, x, None, dict(pre=self.pre[0], groups=self.groups, eps=self.eps))
         self.y, self.h, self.n = [x], [], [n]
         for l in range(self.depth):
-            h = quan.qpointwise_f8(self.n[l], self.w[l])
-            y, n = quan.residual_join(self.y[l], h, **self._join(l, x.numel(), training))
+            h = quan.qpointwise_f8(rows, self.w[l])
+            y, n, rows = self._norm(l + 1, self.y[l], h, self._join(l, x.numel(), training))
             self.h.append(h)
             self.y.append(y)
             self.n.append(n)
         return self.n[-1]
+
+    def _norm(self, l: int, x, h, args):
+        """A join, and what block l's product reads: the norm in 8 bits, or in bf16."""
+        if self.groups == 4 and l < self.depth:
+            return quan.residual_join_f8(x, h, keep=True, **args)
+        y, n = quan.residual_join(x, h, **args)
+        return y, n, n
 
     def advance(self) -> None:
         """Moves the masks past this step's."""

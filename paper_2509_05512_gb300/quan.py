@@ -110,6 +110,13 @@ def load():
                                                 [_vp] * 2)
         lib.quan_qpoint_f8_workspace_size.argtypes = [_ll, _i, _i]
         lib.quan_qpoint_f8_workspace_size.restype = ctypes.c_size_t
+        lib.quan_residual_join_f8_fwd.argtypes = [_vp] * 2 + _join_args + [_vp] * 5
+        lib.quan_f8_rows_bytes.argtypes = [_ll, _i]
+        lib.quan_f8_rows_bytes.restype = ctypes.c_size_t
+        lib.quan_f8_rows_scales.argtypes = [_ll, _i]
+        lib.quan_f8_rows_scales.restype = ctypes.c_size_t
+        lib.quan_f8_rows_dequant.argtypes = [_vp] * 2 + [_ll, _i] + [_vp] * 2
+        lib.quan_qpoint_f8_rows_fwd.argtypes = [_vp] * 7 + [_ll, _i, _i, _i] + [_vp] * 2
         _distill_sizes = [_ll] + [_i] * 6 + [_f]
         lib.quan_distill_fwd.argtypes = [_vp] * 3 + _distill_sizes + [_vp] * 3
         lib.quan_distill_bwd.argtypes = [_vp] * 5 + _distill_sizes + [_f] + [_vp] * 2
@@ -145,7 +152,8 @@ def load():
                      "quan_iqbn_train_fwd", "quan_dropout", "quan_residual_join_fwd",
                      "quan_residual_join_bwd", "quan_f8_weights", "quan_qpoint_f8_fwd",
                      "quan_qpoint_f8_bwd_data", "quan_distill_fwd", "quan_distill_bwd",
-                     "quan_distill_fwd_bwd",
+                     "quan_distill_fwd_bwd", "quan_residual_join_f8_fwd", "quan_f8_rows_dequant",
+                     "quan_qpoint_f8_rows_fwd",
                      "quan_qconv2d_sep_bwd_weight",
                      "quan_maxpool2d_fwd", "quan_set_path", "quan_set_tc_tiles",
                      "quan_set_wait_limit_ns", "quan_device_status", "quan_set_fault_injection",
@@ -218,6 +226,9 @@ _JOIN_FWD = struct.Struct("10q3d2Q4q").pack
 _QPOINT_F8 = struct.Struct("14q").pack
 _QPOINT_F8_BWD = struct.Struct("10q").pack
 _JOIN_BWD = struct.Struct("12q3d2Q9q").pack
+_JOIN_F8 = struct.Struct("10q3d2Q6q").pack
+_F8_ROWS = struct.Struct("6q").pack
+_QPOINT_F8_ROWS = struct.Struct("13q").pack
 _DISTILL_FWD = struct.Struct("10qd3q").pack
 _DISTILL_BWD = struct.Struct("10q2d4q").pack
 
@@ -729,6 +740,74 @@ def quan_qpoint_f8_bwd_data(dy, wq, wscale, rows, Cin, Cout, workspace, workspac
                              _addr(workspace), workspace_bytes, _addr(dx), _stream(stream)))
 
 
+def quan_f8_rows_bytes(rows, C) -> int:
+    return load().quan_f8_rows_bytes(rows, C)
+
+
+def quan_f8_rows_scales(rows, C) -> int:
+    return load().quan_f8_rows_scales(rows, C)
+
+
+def quan_residual_join_f8_fwd(x, h, post, gate, pre, rows, C, groups, images, dtype, alpha, eps, p,
+                              seed, offset, counter, y, n, q, scale, stream=None) -> None:
+    _call(21, _JOIN_F8(_addr(x), _addr(h), _addr(post), _addr(gate), _addr(pre), rows, images, C,
+                       groups, dtype, alpha, eps, p, seed, offset, _addr(counter), _addr(y),
+                       _addr(n), _addr(q), _addr(scale), _stream(stream)))
+
+
+def quan_f8_rows_dequant(q, scale, rows, C, out, stream=None) -> None:
+    _call(22, _F8_ROWS(_addr(q), _addr(scale), rows, C, _addr(out), _stream(stream)))
+
+
+def quan_qpoint_f8_rows_fwd(xq, xscale, wq, wscale, bias, iqbn_scale, iqbn_shift, rows, Cin, Cout,
+                            act, out, stream=None) -> None:
+    _call(23, _QPOINT_F8_ROWS(_addr(xq), _addr(xscale), _addr(wq), _addr(wscale), _addr(bias),
+                              _addr(iqbn_scale), _addr(iqbn_shift), rows, Cin, Cout, act,
+                              _addr(out), _stream(stream)))
+
+
+class F8Rows(typing.NamedTuple):
+    """Rows (pixels) in 8-bit floating point, as residual_join_f8 writes them: q e4m3
+    [..., 4, pitch], scale fp32 [4, ceil(channels / 512), rows rounded up to 128]; component by
+    component, pitch = channels / 4 rounded up to 16."""
+    q: object
+    scale: object
+    channels: int
+
+
+def _f8_rows(name, x, dev):
+    """The leading shape and the number of 8-bit rows, which are looked at."""
+    torch = _torch or _get_torch()
+    q, scale, C = x
+    if C % 4 or C < 4:
+        raise ValueError("%s has %s channels, not a multiple of 4" % (name, C))
+    lead, pitch = tuple(q.shape[:-2]), (C + 63) // 64 * 16
+    if q.dtype is not torch.float8_e4m3fn or q.shape[-2:] != (4, pitch) or \
+            not q.is_contiguous():
+        _check_tensor(name + ".q", q, lead + (4, pitch), torch.float8_e4m3fn, dev)
+    rows = q.numel() // (4 * pitch)
+    want = (4, (C + 511) // 512, (rows + 127) // 128 * 128)
+    if scale.dtype is not torch.float32 or scale.shape != want or scale.get_device() != dev or \
+            not scale.is_contiguous():
+        _check_tensor(name + ".scale", scale, want, torch.float32, dev)
+    return lead, rows
+
+
+def dequantize_f8_rows(x, *, out=None, stream=None):
+    """F8Rows read back: bf16 [..., channels]."""
+    bf16 = (_torch or _get_torch()).bfloat16
+    dev = _device("x.q", x.q)
+    lead, rows = _f8_rows("x", x, dev)
+    shape = lead + (x.channels,)
+    if out is None:
+        out = _empty(stream, shape, bf16, x.q.device)
+    else:
+        _check_tensor("out", out, shape, bf16, dev)
+    _call(22, _F8_ROWS(x.q.data_ptr(), x.scale.data_ptr(), rows, x.channels, out.data_ptr(),
+                       _stream(stream, dev)))
+    return out
+
+
 class F8Weights(typing.NamedTuple):
     """Letters of a pointwise layer in 8-bit floating point, as quantize_f8_weights lays them
     out: q e4m3 [4, n, pitch], scale fp32 [4, ceil(n / 128), ceil(k / 128)]; n, k = Cout / 4,
@@ -770,14 +849,7 @@ def _qpoint_f8(x, q, scale, K, N, workspace, out, stream, dev):
     shape, bf16 = tuple(x.shape), torch.bfloat16  # (torch.empty takes a tuple 1 us faster)
     if x.dtype is not bf16 or shape[-1] != K or not x.is_contiguous():
         _check_tensor("x", x, shape[:-1] + (K,), bf16, dev)
-    # (pitch K / 4 rounded up to 16, a scale for each 128 x 128)
-    blocks = ((N + 511) // 512, (K + 511) // 512)
-    if q.numel() != N * 16 * ((K + 63) // 64) or q.dtype is not torch.float8_e4m3fn or \
-            q.get_device() != dev or not q.is_contiguous():
-        _check_tensor("w.q", q, (4, N // 4, 16 * ((K + 63) // 64)), torch.float8_e4m3fn, dev)
-    if scale.numel() != 4 * blocks[0] * blocks[1] or scale.dtype is not torch.float32 or \
-            scale.get_device() != dev or not scale.is_contiguous():
-        _check_tensor("w.scale", scale, (4,) + blocks, torch.float32, dev)
+    _f8_letters(q, scale, K, N, dev)
     rows = x.numel() // K
     shape = shape[:-1] + (N,)
     if out is None:
@@ -792,17 +864,32 @@ def _qpoint_f8(x, q, scale, K, N, workspace, out, stream, dev):
     return rows, workspace, nbytes, out
 
 
+def _f8_letters(q, scale, K, N, dev):
+    """Looks at the letters of an 8-bit product of K input and N output channels."""
+    torch = _torch or _get_torch()
+    # (pitch K / 4 rounded up to 16, a scale for each 128 x 128)
+    blocks = ((N + 511) // 512, (K + 511) // 512)
+    if q.numel() != N * 16 * ((K + 63) // 64) or q.dtype is not torch.float8_e4m3fn or \
+            q.get_device() != dev or not q.is_contiguous():
+        _check_tensor("w.q", q, (4, N // 4, 16 * ((K + 63) // 64)), torch.float8_e4m3fn, dev)
+    if scale.numel() != 4 * blocks[0] * blocks[1] or scale.dtype is not torch.float32 or \
+            scale.get_device() != dev or not scale.is_contiguous():
+        _check_tensor("w.scale", scale, (4,) + blocks, torch.float32, dev)
+
+
 def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE, workspace=None,
                   out=None, stream=None):
     """Pointwise quaternion convolution in 8-bit floating point: bf16 x [..., Cin] (CUDA), which
     is quantised in the call, and w = quantize_f8_weights(...) -> bf16 [..., Cout],
-    act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d.  Half the bytes of
+    act(scale * (x W + bias) + shift) with fp32 vectors [Cout] as in qconv2d.  x may be F8Rows
+    (residual_join_f8): no workspace, the same bits.  Half the bytes of
     bf16 letters; faster than qconv2d in wide layers only (25,600 rows: 4096 -> 4096 420 us
     against 485, 2048 -> 1024 86 against 78; 102,400 rows of 512 -> 1024 109 against 84)."""
     if w.transposed:
         raise ValueError("w holds transposed letters: quantize_f8_weights(..., transpose=False)")
     q, wscale, Cin, Cout, _ = w
-    dev = _device("x", x)
+    in8 = x.__class__ is F8Rows
+    dev = _device("x", x.q if in8 else x)
     vectors = (0, 0, 0)
     if bias is not None or scale is not None or shift is not None:
         f32 = (_torch or _get_torch()).float32
@@ -810,6 +897,21 @@ def qpointwise_f8(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
             if v is not None:
                 _check_tensor(name, v, (Cout,), f32, dev)
         vectors = (_addr(bias), _addr(scale), _addr(shift))
+    if in8:
+        if x.channels != Cin or workspace is not None:
+            raise ValueError("x has %d channels, w %d, and 8-bit rows need no workspace" %
+                             (x.channels, Cin))
+        lead, rows = _f8_rows("x", x, dev)
+        _f8_letters(q, wscale, Cin, Cout, dev)
+        shape, bf16 = lead + (Cout,), (_torch or _get_torch()).bfloat16
+        if out is None:
+            out = _empty(stream, shape, bf16, x.q.device)
+        else:
+            _check_tensor("out", out, shape, bf16, dev)
+        _call(23, _QPOINT_F8_ROWS(x.q.data_ptr(), x.scale.data_ptr(), q.data_ptr(),
+                                  wscale.data_ptr(), *vectors, rows, Cin, Cout, act,
+                                  out.data_ptr(), _stream(stream, dev)))
+        return out
     rows, workspace, nbytes, out = _qpoint_f8(x, q, wscale, Cin, Cout, workspace, out,
                                               stream, dev)
     _call(16, _QPOINT_F8(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), *vectors, rows, Cin, Cout,
@@ -887,6 +989,54 @@ def residual_join(x, h=None, *, post=None, gate=None, pre=None, alpha=1.0, group
                         C, groups, dtype, alpha, eps, p, seed, offset, _addr(counter), _addr(y),
                         _addr(n), _stream(stream, dev)))
     return y, n
+
+
+def residual_join_f8(x, h=None, *, post=None, gate=None, pre, alpha=1.0, groups=1, eps=1e-5,
+                     p=0.0, seed=0, offset=0, counter=None, keep=False, y=None, n=None, n8=None,
+                     stream=None):
+    """`residual_join` whose n comes out as F8Rows for qpointwise_f8, rounded to bf16 and then
+    quantised: the bits (groups=4) of residual_join and the product's own quantisation, without
+    that pass.  keep=True, or n given: n in bf16 too, for the weight gradient.  Returns (y, n, n8),
+    None for what is absent; y may be given as x, n as a bf16 h (in place), n8 as F8Rows to write
+    to.  The gradients are residual_join_backward's: the quantisation has none of its own."""
+    torch = _torch or _get_torch()
+    t, shape = x.dtype, x.shape
+    dtype = QUAN_DTYPE_BF16 if t is torch.bfloat16 else _dtype_of("x", x)
+    dev = _device("x", x)
+    if not x.is_contiguous():
+        _check_tensor("x", x, shape, t, dev)
+    if pre is None:
+        raise ValueError("pre is needed: the 8-bit rows are the norm")
+    rows, C, images = _join_shape(x, shape, post, gate, pre, dev)
+    if C % 4 or C < 4:
+        raise ValueError("x has %d channels, not a multiple of 4" % C)
+    if counter is not None:
+        _check_counter(counter, dev)
+    if h is not None:
+        if h.dtype is not t or h.shape != shape or h.get_device() != dev or not h.is_contiguous():
+            _check_tensor("h", h, shape, t, dev)
+        if y is None:
+            y = _empty(stream, shape, t, x.device)
+        else:
+            _check_tensor("y", y, shape, t, dev)
+    elif y is not None:
+        raise ValueError("y is given without h")
+    if n is not None:
+        _check_tensor("n", n, shape, torch.bfloat16, dev)
+    elif keep:
+        n = _empty(stream, shape, torch.bfloat16, x.device)
+    if n8 is None:
+        n8 = F8Rows(_empty(stream, tuple(shape[:-1]) + (4, (C + 63) // 64 * 16),
+                           torch.float8_e4m3fn, x.device),
+                    _empty(stream, (4, (C + 511) // 512, (rows + 127) // 128 * 128),
+                           torch.float32, x.device), C)
+    elif n8.channels != C or _f8_rows("n8", n8, dev)[0] != tuple(shape[:-1]) or \
+            n8.q.get_device() != dev:
+        raise ValueError("n8 does not have the rows and channels of x")
+    _call(21, _JOIN_F8(x.data_ptr(), _addr(h), _addr(post), _addr(gate), _addr(pre), rows, images,
+                       C, groups, dtype, alpha, eps, p, seed, offset, _addr(counter), _addr(y),
+                       _addr(n), n8.q.data_ptr(), n8.scale.data_ptr(), _stream(stream, dev)))
+    return y, n, n8
 
 
 def residual_join_backward(dy, dn, y, h=None, *, post=None, gate=None, pre=None, alpha=1.0,
