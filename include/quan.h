@@ -585,6 +585,37 @@ quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const floa
                                       size_t workspace_bytes, void* dx, quan_stream_t stream);
 
 /*
+ * The pointwise convolution of a few pixels with letters in 4 bits.  A group is `group` (32, 64 or
+ * 128) input channels of one output channel of one letter: its scale is max |v| / 7 rounded to bf16 (1
+ * where that is 0), its values are v / scale rounded to a whole number (-7 .. 7).  A group that holds
+ * an infinity or a NaN has scale NaN: every output computed from it is NaN.
+ *
+ * quan_w4_weights quantises the letters once, as the product reads them:
+ *   wr..wk   bf16 [Cout/4][1][1][Cin/4] (device), 2-byte aligned
+ *   q        quan_w4_weights_bytes(Cin, Cout) bytes (device, 16-byte aligned):
+ *            [4][ceil(Cout/4 / 16)][ceil(Cin/4 / 64)] blocks of 512 bytes, 16 output x 64 input
+ *            channels.  32-bit word s of the 16 bytes of g, t (4 g + t < 32) has, as value + 8,
+ *            outputs g and g + 8 and inputs k = 32 (s / 2) + 8 t + 4 (s mod 2) .. k + 3: bits 4 i are
+ *            output g + 8 (i mod 2), input k + 2 (i mod 4 / 2) + i / 4.  Padding is 0 (8)
+ *   scale    bf16 [4][ceil(Cout/4 / 16)][ceil(Cin/4 / group)][8][2] (device, 4-byte aligned),
+ *            quan_w4_weights_scales numbers: output g + 8 h of a block at [g][h]
+ *
+ * quan_qpoint_w4_fwd: out = act(iqbn_scale * (x W + bias) + iqbn_shift), the rest as in
+ * quan_qpoint_f8_fwd.  Sums are fp32.  x bf16 [rows][Cin], out bf16 [rows][Cout], no overlap with an
+ * input.  rows = 0 is a no-op; more than 2^20 rows or channels return QUAN_ERR_UNSUPPORTED (past about
+ * 64 rows quan_qpoint_f8_fwd is faster).
+ */
+size_t quan_w4_weights_bytes(int Cin, int Cout);
+size_t quan_w4_weights_scales(int Cin, int Cout, int group);
+quan_status_t quan_w4_weights(const void* wr, const void* wi, const void* wj, const void* wk,
+                              int Cin, int Cout, int group, void* q, void* scale,
+                              quan_stream_t stream);
+quan_status_t quan_qpoint_w4_fwd(const void* x, const void* wq, const void* wscale,
+                                 const float* bias, const float* iqbn_scale,
+                                 const float* iqbn_shift, long long rows, int Cin, int Cout,
+                                 int group, int act, void* out, quan_stream_t stream);
+
+/*
  * Distillation from a teacher's top logits (the loss that trains one classifier from another): a row
  * has `classes` logits z and `top` slots, each a class and the teacher's logit t of it.  With
  * p = softmax(t / T) over the row's slots and q = softmax(z / T) over its classes,

@@ -139,6 +139,28 @@ def f8_letter(w):
     return w, scales
 
 
+def w4_letter(w, group):
+    """(values, whole numbers, scales [Qout, groups]) of one letter [Qout, Qin] in 4 bits: `group`
+    inputs of an output share max / 7 in bf16 (1 for 0; NaN for an infinity or a NaN)."""
+    w = np.array(w, dtype=np.float64)
+    Qo, Qi = w.shape
+    q, scales = np.zeros_like(w), np.empty((Qo, -(-Qi // group)))
+    for b in range(scales.shape[1]):
+        part = w[:, b * group:(b + 1) * group]
+        a = _amax(part, 1)
+        ok = np.isfinite(a)
+        m, e = np.frexp(np.where(ok, a, 0.0) / 7.0)  # bf16: 8 significant bits, steps of 2^-133
+        unit = np.maximum(e - 8, -133)
+        s = np.ldexp(np.rint(np.ldexp(m, e - unit)), unit)
+        s = np.where(ok, np.where(s > 0, s, 1.0), np.nan)
+        scales[:, b] = s
+        good = np.where(ok, s, 1.0)[:, None]
+        v = np.clip(np.rint(np.where(ok[:, None], part, 0.0) / good), -7, 7)
+        q[:, b * group:(b + 1) * group] = v
+        part[:] = np.where(ok[:, None], v * good, np.nan)
+    return w, q, scales
+
+
 # Eq. 3: output component co takes input component ci through letter co xor ci.
 _SIGN = np.array([[1, -1, -1, -1], [1, 1, -1, 1], [1, 1, 1, -1], [1, -1, 1, 1]], dtype=np.float64)
 

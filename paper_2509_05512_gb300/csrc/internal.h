@@ -283,6 +283,15 @@ cudaError_t launch_qpoint_f8(const void* x, const float* xscale, const void* wq,
                              unsigned long long wait_limit_ns, int inject_stall,
                              cudaStream_t stream, char* err, size_t errlen);
 
+// The pointwise product with 4-bit letters (qpoint_w4.cu): bytes of the letters, number of scales.
+size_t w4_bytes(int Qi, int Qo);
+size_t w4_scales(int Qi, int Qo, int group);
+cudaError_t launch_w4_letters(const void* const w[4], int Qo, int Qi, int group, void* q,
+                              void* scale, cudaStream_t stream);
+cudaError_t launch_qpoint_w4(const void* x, const void* q, const void* scale,
+                             const EpilogueArgs& ep, long long rows, int Qi, int Qo, int group,
+                             int act, void* out, int num_sms, cudaStream_t stream);
+
 // Per-real-channel max pooling, bf16 NHWC.
 cudaError_t launch_maxpool_bf16(const void* x, int N, int H, int W, int C, int k, int stride,
                                 int pad, void* out, int num_sms, cudaStream_t stream);

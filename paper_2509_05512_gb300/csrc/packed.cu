@@ -304,6 +304,18 @@ extern "C" int quan_packed_call(int op, const long long* words) {
             return quan_qpoint_f8_rows_fwd(xq, xscale, wq, v[0], v[1], v[2], v[3], rows, Cin, Cout,
                                            act, out, g.stream());
         }
+        case 24: {
+            void* x = g.ptr();
+            void* wq = g.ptr();
+            void* wscale = g.ptr();
+            float* v[3];
+            for (auto& p : v) p = g.f32();
+            const long long rows = g.next();
+            const int Cin = g.num(), Cout = g.num(), group = g.num(), act = g.num();
+            void* out = g.ptr();
+            return quan_qpoint_w4_fwd(x, wq, wscale, v[0], v[1], v[2], rows, Cin, Cout, group, act,
+                                      out, g.stream());
+        }
         default:
             return QUAN_ERR_INVALID_ARG;
     }

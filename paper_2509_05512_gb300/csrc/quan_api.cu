@@ -487,6 +487,14 @@ quan_status_t run_qpoint_f8(const void* x, const float* xscale, const void* wq,
     return QUAN_OK;
 }
 
+// Pixels of the product with 4-bit letters, which is for few of them.
+constexpr long long W4_MAX_ROWS = 1 << 20;
+
+bool w4_sizes(int Cin, int Cout, int group) {
+    return Cin >= 1 && Cout >= 1 && Cin % 4 == 0 && Cout % 4 == 0 &&
+           (group == 32 || group == 64 || group == 128);
+}
+
 // Both directions of the distillation loss; `a` holds everything but the flags of its types.
 quan_status_t run_distill(quan::DistillArgs a, int dtype, int teacher_dtype, int index_bits,
                           quan_stream_t stream) {
@@ -1279,6 +1287,86 @@ quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const floa
                                       size_t workspace_bytes, void* dx, quan_stream_t stream) {
     return run_qpoint_f8(dy, nullptr, wq, wscale, {nullptr, nullptr, nullptr, nullptr}, rows, Cout, Cin,
                          QUAN_ACT_NONE, true, workspace, workspace_bytes, dx, stream);
+}
+
+size_t quan_w4_weights_bytes(int Cin, int Cout) {
+    return w4_sizes(Cin, Cout, 64) ? quan::w4_bytes(Cin / 4, Cout / 4) : 0;
+}
+
+size_t quan_w4_weights_scales(int Cin, int Cout, int group) {
+    return w4_sizes(Cin, Cout, group) ? quan::w4_scales(Cin / 4, Cout / 4, group) : 0;
+}
+
+quan_status_t quan_w4_weights(const void* wr, const void* wi, const void* wj, const void* wk,
+                              int Cin, int Cout, int group, void* q, void* scale,
+                              quan_stream_t stream) {
+    const void* w[4] = {wr, wi, wj, wk};
+    if (!wr || !wi || !wj || !wk || !q || !scale)
+        return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    if (!w4_sizes(Cin, Cout, group))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "Cin=%d and Cout=%d must be positive multiples of 4, group=%d 32, 64 or 128",
+                    Cin, Cout, group);
+    if (Cin > F8_MAX_CHANNELS || Cout > F8_MAX_CHANNELS)
+        return fail(QUAN_ERR_UNSUPPORTED, "letters too large");
+    if (misaligned(w, 4, 2) || reinterpret_cast<uintptr_t>(q) % 16 != 0 ||
+        reinterpret_cast<uintptr_t>(scale) % 4 != 0)
+        return fail(QUAN_ERR_INVALID_ARG, "letters must be 2-byte, q 16-byte, scale 4-byte aligned");
+    const size_t wb = size_t(Cin / 4) * (Cout / 4) * 2;
+    const Span outs[] = {{q, quan_w4_weights_bytes(Cin, Cout)},
+                         {scale, quan_w4_weights_scales(Cin, Cout, group) * 2}};
+    const Span ins[] = {{wr, wb}, {wi, wb}, {wj, wb}, {wk, wb}};
+    const unsigned equal[] = {0u, 0u};
+    if (clash(outs, 2, ins, 4, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "q or scale overlaps another tensor");
+    const cudaError_t e = quan::launch_w4_letters(w, Cout / 4, Cin / 4, group, q, scale,
+                                                  reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "w4 letters launch");
+    return QUAN_OK;
+}
+
+quan_status_t quan_qpoint_w4_fwd(const void* x, const void* wq, const void* wscale,
+                                 const float* bias, const float* iqbn_scale,
+                                 const float* iqbn_shift, long long rows, int Cin, int Cout,
+                                 int group, int act, void* out, quan_stream_t stream) {
+    if (rows < 0 || !w4_sizes(Cin, Cout, group))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "rows=%lld must be >= 0, the channel counts %d and %d positive multiples of 4, "
+                    "group=%d 32, 64 or 128",
+                    rows, Cin, Cout, group);
+    if ((iqbn_scale == nullptr) != (iqbn_shift == nullptr))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "iqbn_scale and iqbn_shift must both be given or both NULL");
+    if (act < QUAN_ACT_NONE || act > QUAN_ACT_SILU)
+        return fail(QUAN_ERR_INVALID_ARG, "unknown activation %d", act);
+    if (rows == 0) return QUAN_OK;
+    if (!x || !wq || !wscale || !out) return fail(QUAN_ERR_INVALID_ARG, "null tensor pointer");
+    if (rows > W4_MAX_ROWS || Cin > F8_MAX_CHANNELS || Cout > F8_MAX_CHANNELS ||
+        rows >= (1LL << 40) / Cin || rows >= (1LL << 40) / Cout)
+        return fail(QUAN_ERR_UNSUPPORTED, "tensor too large");
+    const void* half[] = {x, out};
+    const void* vectors[] = {wscale, bias, iqbn_scale, iqbn_shift};
+    if (misaligned(half, 2, 2) || misaligned(vectors, 4, 4) || misaligned(&wq, 1, 16))
+        return fail(QUAN_ERR_INVALID_ARG,
+                    "tensors must be aligned to their elements, scales to 4 bytes, the 4-bit "
+                    "letters to 16");
+    const size_t cb = size_t(4) * Cout;
+    const Span outs[] = {{out, static_cast<size_t>(rows) * Cout * 2}};
+    const Span ins[] = {{x, static_cast<size_t>(rows) * Cin * 2},
+                        {wq, quan_w4_weights_bytes(Cin, Cout)},
+                        {wscale, quan_w4_weights_scales(Cin, Cout, group) * 2},
+                        {bias, cb}, {iqbn_scale, cb}, {iqbn_shift, cb}};
+    const unsigned equal[] = {0u};
+    if (clash(outs, 1, ins, 6, equal))
+        return fail(QUAN_ERR_INVALID_ARG, "out overlaps another tensor");
+    int num_sms = 0, cc = 0;
+    cudaError_t e;
+    if (!device_info(&num_sms, &cc, &e)) return cuda_fail(e, "device query");
+    e = quan::launch_qpoint_w4(x, wq, wscale, {bias, iqbn_scale, iqbn_shift, nullptr}, rows, Cin / 4,
+                               Cout / 4, group, act, out, num_sms,
+                               reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "qpoint_w4 launch");
+    return QUAN_OK;
 }
 
 quan_status_t quan_distill_fwd(const void* z, const void* index, const void* teacher,

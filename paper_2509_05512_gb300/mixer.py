@@ -49,6 +49,21 @@ class Mixer:
         self.w = [quan.quantize_f8_weights(*w) for w in self.letters]
         self.wt = [quan.quantize_f8_weights(*w, transpose=True) for w in self.letters]
 
+    def quantize_4bit(self, group: int = 64) -> None:
+        """The letters in 4 bits, for `serve`, after they changed."""
+        self.w4 = [quan.quantize_w4_weights(*w, group=group) for w in self.letters]
+
+    def serve(self, x):
+        """The stack on a few pixels, bf16 x [..., channels] (CUDA), without dropout and with the
+        letters of quantize_4bit: an eighth of their bytes, which bound a single pixel.  Keeps
+        nothing."""
+        _, n = quan.residual_join(x, pre=self.pre[0], groups=self.groups, eps=self.eps)
+        y = x
+        for l in range(self.depth):
+            h = quan.qpointwise_w4(n, self.w4[l])
+            y, n = quan.residual_join(y, h, **self._join(l, x.numel(), False))
+        return n
+
     def _join(self, l: int, elements: int, training: bool) -> dict:
         """The keyword arguments of block l's join, both ways."""
         return dict(post=self.post[l], gate=self.gate[l], pre=self.pre[l + 1], alpha=self.alpha,

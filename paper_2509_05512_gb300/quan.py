@@ -117,6 +117,12 @@ def load():
         lib.quan_f8_rows_scales.restype = ctypes.c_size_t
         lib.quan_f8_rows_dequant.argtypes = [_vp] * 2 + [_ll, _i] + [_vp] * 2
         lib.quan_qpoint_f8_rows_fwd.argtypes = [_vp] * 7 + [_ll, _i, _i, _i] + [_vp] * 2
+        lib.quan_w4_weights_bytes.argtypes = [_i] * 2
+        lib.quan_w4_weights_bytes.restype = ctypes.c_size_t
+        lib.quan_w4_weights_scales.argtypes = [_i] * 3
+        lib.quan_w4_weights_scales.restype = ctypes.c_size_t
+        lib.quan_w4_weights.argtypes = [_vp] * 4 + [_i] * 3 + [_vp] * 3
+        lib.quan_qpoint_w4_fwd.argtypes = [_vp] * 6 + [_ll] + [_i] * 4 + [_vp] * 2
         _distill_sizes = [_ll] + [_i] * 6 + [_f]
         lib.quan_distill_fwd.argtypes = [_vp] * 3 + _distill_sizes + [_vp] * 3
         lib.quan_distill_bwd.argtypes = [_vp] * 5 + _distill_sizes + [_f] + [_vp] * 2
@@ -153,7 +159,7 @@ def load():
                      "quan_residual_join_bwd", "quan_f8_weights", "quan_qpoint_f8_fwd",
                      "quan_qpoint_f8_bwd_data", "quan_distill_fwd", "quan_distill_bwd",
                      "quan_distill_fwd_bwd", "quan_residual_join_f8_fwd", "quan_f8_rows_dequant",
-                     "quan_qpoint_f8_rows_fwd",
+                     "quan_qpoint_f8_rows_fwd", "quan_w4_weights", "quan_qpoint_w4_fwd",
                      "quan_qconv2d_sep_bwd_weight",
                      "quan_maxpool2d_fwd", "quan_set_path", "quan_set_tc_tiles",
                      "quan_set_wait_limit_ns", "quan_device_status", "quan_set_fault_injection",
@@ -229,6 +235,7 @@ _JOIN_BWD = struct.Struct("12q3d2Q9q").pack
 _JOIN_F8 = struct.Struct("10q3d2Q6q").pack
 _F8_ROWS = struct.Struct("6q").pack
 _QPOINT_F8_ROWS = struct.Struct("13q").pack
+_QPOINT_W4 = struct.Struct("13q").pack
 _DISTILL_FWD = struct.Struct("10qd3q").pack
 _DISTILL_BWD = struct.Struct("10q2d4q").pack
 
@@ -930,6 +937,97 @@ def qpointwise_f8_backward_data(dy, w, *, workspace=None, out=None, stream=None)
                                               stream, dev)
     _call(17, _QPOINT_F8_BWD(dy.data_ptr(), q.data_ptr(), wscale.data_ptr(), rows, Cin, Cout,
                              _addr(workspace), nbytes, out.data_ptr(), _stream(stream, dev)))
+    return out
+
+
+# ------------------------------------------------------------------ letters in 4 bits
+
+def quan_w4_weights(wr, wi, wj, wk, Cin, Cout, group, q, scale, stream=None) -> None:
+    _check(load().quan_w4_weights(_ptr(wr), _ptr(wi), _ptr(wj), _ptr(wk), Cin, Cout, group, _ptr(q),
+                                  _ptr(scale), _stream(stream)))
+
+
+def quan_w4_weights_bytes(Cin, Cout) -> int:
+    return load().quan_w4_weights_bytes(Cin, Cout)
+
+
+def quan_w4_weights_scales(Cin, Cout, group) -> int:
+    return load().quan_w4_weights_scales(Cin, Cout, group)
+
+
+def quan_qpoint_w4_fwd(x, wq, wscale, bias, iqbn_scale, iqbn_shift, rows, Cin, Cout, group, act,
+                       out, stream=None) -> None:
+    _call(24, _QPOINT_W4(_addr(x), _addr(wq), _addr(wscale), _addr(bias), _addr(iqbn_scale),
+                         _addr(iqbn_shift), rows, Cin, Cout, group, act, _addr(out),
+                         _stream(stream)))
+
+
+class W4Weights(typing.NamedTuple):
+    """Letters of a pointwise layer in 4 bits, as quantize_w4_weights lays them out: q uint8
+    [4, ceil(Cout / 64), ceil(Cin / 256), 512], scale bf16 [4, ceil(Cout / 64), groups, 16] (the
+    order inside is include/quan.h's)."""
+    q: object
+    scale: object
+    Cin: int
+    Cout: int
+    group: int
+
+
+def quantize_w4_weights(wr, wi, wj, wk, *, group=64, stream=None):
+    """The four letters [Cout/4, 1, 1, Cin/4] (bf16, CUDA) of a pointwise layer as W4Weights for
+    qpointwise_w4: whole numbers -7 .. 7 with a bf16 scale for each `group` (32, 64 or 128) input
+    channels of an output channel."""
+    import torch
+    Qout, kh, kw, Qin = wr.shape
+    if kh != 1 or kw != 1:
+        raise ValueError("the letters of a pointwise layer are [Cout/4, 1, 1, Cin/4]")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128 (got %s)" % (group,))
+    dev = _device("wr", wr)
+    for name, w in (("wr", wr), ("wi", wi), ("wj", wj), ("wk", wk)):
+        _check_tensor(name, w, wr.shape, torch.bfloat16, dev)
+    if min(Qin, Qout) < 1 or 4 * max(Qin, Qout) >= 1 << 31:
+        raise ValueError("a layer of %d -> %d channels is empty or too large" % (4 * Qin, 4 * Qout))
+    tiles = -(-Qout // 16)
+    q = _empty(stream, (4, tiles, -(-Qin // 64), 512), torch.uint8, wr.device)
+    scale = _empty(stream, (4, tiles, -(-Qin // group), 16), torch.bfloat16, wr.device)
+    quan_w4_weights(wr, wi, wj, wk, 4 * Qin, 4 * Qout, group, q, scale, stream)
+    return W4Weights(q, scale, 4 * Qin, 4 * Qout, group)
+
+
+def qpointwise_w4(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE, out=None,
+                  stream=None):
+    """Pointwise quaternion convolution of a few pixels with 4-bit letters: bf16 x [..., Cin] (CUDA)
+    and w = quantize_w4_weights(...) -> bf16 [..., Cout], act(scale * (x W + bias) + shift) with
+    fp32 vectors [Cout] as in qconv2d.  An eighth of the bytes of bf16 letters, for serving: past
+    about 64 pixels qpointwise_f8 is faster."""
+    torch = _torch or _get_torch()
+    q, wscale, Cin, Cout, group = w
+    dev, shape, bf16 = _device("x", x), tuple(x.shape), torch.bfloat16
+    if x.dtype is not bf16 or shape[-1] != Cin or not x.is_contiguous():
+        _check_tensor("x", x, shape[:-1] + (Cin,), bf16, dev)
+    tiles = (Cout + 63) // 64
+    want = (4, tiles, (Cin + 255) // 256, 512)
+    if q.dtype is not torch.uint8 or q.shape != want or q.get_device() != dev or \
+            not q.is_contiguous():
+        _check_tensor("w.q", q, want, torch.uint8, dev)
+    want = (4, tiles, (Cin + 4 * group - 1) // (4 * group), 16)
+    if wscale.dtype is not bf16 or wscale.shape != want or wscale.get_device() != dev or \
+            not wscale.is_contiguous():
+        _check_tensor("w.scale", wscale, want, bf16, dev)
+    vectors = (0, 0, 0)
+    if bias is not None or scale is not None or shift is not None:
+        for name, v in (("bias", bias), ("scale", scale), ("shift", shift)):
+            if v is not None:
+                _check_tensor(name, v, (Cout,), torch.float32, dev)
+        vectors = (_addr(bias), _addr(scale), _addr(shift))
+    shape = shape[:-1] + (Cout,)
+    if out is None:
+        out = _empty(stream, shape, bf16, x.device)
+    else:
+        _check_tensor("out", out, shape, bf16, dev)
+    _call(24, _QPOINT_W4(x.data_ptr(), q.data_ptr(), wscale.data_ptr(), *vectors, x.numel() // Cin,
+                         Cin, Cout, group, act, out.data_ptr(), _stream(stream, dev)))
     return out
 
 
