@@ -14,7 +14,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libquan.so")
 SOURCES = ["quan_api.cu", "packed.cu", "qconv_tc.cu", "qconv_simt.cu", "qconv_mma.cu", "qconv_bwd.cu", "maxpool.cu",
-           "poincare.cu", "iqbn.cu", "residual.cu",
+           "poincare.cu", "iqbn.cu", "residual.cu", "join_f8.cu",
            "qpoint_f8.cu", "qpoint_w4.cu", "distill.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -16,6 +16,7 @@
 #include <atomic>
 
 #include "internal.h"
+#include "pairs.cuh"
 #include "ptx.cuh"
 #include "vec_io.cuh"
 
@@ -123,14 +124,12 @@ __device__ __forceinline__ void put(T* p, float x) {
     e.store(p);
 }
 
-// Slot k of a row: its class (-1 when empty) and the teacher's logit.
-__device__ __forceinline__ long long slot_class(const DistillParams& p, long long row, int k) {
-    const long long at = row * p.top + k;
+// Slot k of a row: its class (-1 when empty) and the teacher's logit; `at`: row top + k.
+__device__ __forceinline__ long long slot_class(const DistillParams& p, long long at) {
     return p.index64 ? static_cast<const long long*>(p.index)[at]
                      : static_cast<const int*>(p.index)[at];
 }
-__device__ __forceinline__ float slot_logit(const DistillParams& p, long long row, int k) {
-    const long long at = row * p.top + k;
+__device__ __forceinline__ float slot_logit(const DistillParams& p, long long at) {
     return p.teacher_f32 ? element(static_cast<const float*>(p.teacher) + at)
                          : element(static_cast<const __nv_bfloat16*>(p.teacher) + at);
 }
@@ -138,8 +137,8 @@ __device__ __forceinline__ int slot_id(const DistillParams& p, long long id, flo
     return id >= 0 && id < p.classes && t != -INFINITY ? static_cast<int>(id) : -1;
 }
 __device__ __forceinline__ int slot(const DistillParams& p, long long row, int k, float& t) {
-    t = slot_logit(p, row, k);
-    return slot_id(p, slot_class(p, row, k), t);
+    t = slot_logit(p, row * p.top + k);
+    return slot_id(p, slot_class(p, row * p.top + k), t);
 }
 
 // A sum of 2^((z - m) c) for another maximum.  (Without a number so far, m = -inf, it is 0, or NaN
@@ -228,24 +227,6 @@ template <int N>
 __device__ __forceinline__ void copies_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// Two floats at a time.
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
-        "add.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
-        "mul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-
 // v becomes 2^((v - at) c); `sum` takes its elements by twos.
 template <int N>
 __device__ __forceinline__ void powers(float (&v)[N], float at, float c, float2& sum) {
@@ -686,8 +667,8 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
         if (r >= p.rows) return;
         if (MODE & GRAD && p.dloss) weight = p.dloss[r];
         if (lane < s.top) {
-            raw = slot_class(p, r, lane);
-            t0 = slot_logit(p, r, lane);
+            raw = slot_class(p, r * p.top + lane);
+            t0 = slot_logit(p, r * p.top + lane);
         }
     };
     auto gather = [&](long long r) {
@@ -781,9 +762,10 @@ constexpr int TILE_THREADS = 256;
 
 // A tile of 256 / LANES rows a block.  The rows lie one after the other, so the tile is read and
 // written in whole chunks wherever its rows begin; in shared memory a row is LANES lanes of a warp, at
-// most W of its 4-byte words each, whose powers stay in registers, and the gradient takes the logits'
-// place.
-template <typename T, int MODE, int LANES, int W>
+// most W of its 4-byte words and K of its slots each, whose powers stay in registers, and the gradient
+// takes the logits' place.  A class that several slots have shows by a byte a class: each slot writes
+// its number there and looks whether it still stands.
+template <typename T, int MODE, int LANES, int W, int K>
 __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const DistillParams p) {
     constexpr int E = RowView<T>::E, N = 4 / static_cast<int>(sizeof(T));
     constexpr int ROWS = TILE_THREADS / LANES;
@@ -793,19 +775,13 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
     const int tid = threadIdx.x, tr = tid / LANES, lane = tid % LANES;
     const long long row0 = static_cast<long long>(blockIdx.x) * ROWS, row = row0 + tr;
     const int rows = p.rows - row0 < ROWS ? static_cast<int>(p.rows - row0) : ROWS;
-    const int pitch = static_cast<int>(p.pitch), top4 = (p.top + 3) & ~3;
+    const int pitch = static_cast<int>(p.pitch);
     const RowView<T> view(static_cast<const T*>(p.z), p.rows * p.pitch, row0 * p.pitch,
                           rows * pitch);
     const int chunks = view.chunks();
     int4* tile = dynamic;
-    Slots s;
-    s.top = p.top;
-    s.top4 = top4;
-    s.id = reinterpret_cast<int*>(tile + (ROWS * pitch + E - 1) / E + 1) + tr * 4 * top4;
-    s.p = reinterpret_cast<float*>(s.id + top4);
-    s.z = s.p + top4;
-    float* share = s.z + top4;
-    // the logits and the slots
+    uint8_t* owner =
+        reinterpret_cast<uint8_t*>(tile + (ROWS * pitch + E - 1) / E + 1) + tr * pitch;
     for (int i = tid; i < chunks; i += TILE_THREADS) {
         if (!view.outside(i)) {
             copy_async(tile + i, view.base + i * E);
@@ -816,23 +792,90 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         }
     }
     copies_commit();
+    // the teacher's side: p, and the sum of p ln p
     const bool active = tr < rows;
-    for (int k = lane; k < top4; k += LANES) {
-        float t = 0.0f;
-        s.id[k] = active && k < p.top ? slot(p, row, k, t) : -1;
-        s.p[k] = t;
+    long long raw[K];
+    float t[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const long long at = row * p.top + lane + k * LANES;
+        raw[k] = -1;
+        t[k] = 0.0f;
+        if (active && lane + k * LANES < p.top) {
+            raw[k] = slot_class(p, at);
+            t[k] = slot_logit(p, at);
+        }
     }
     float g = MODE & GRAD && p.dloss && active ? p.dloss[row] : 1.0f;
     float lse = MODE == GRAD && active ? p.lse_in[row] : 0.0f;
-    __syncwarp();  // (a row's slots are its warp's own)
-    bool some;
-    const float entropy = teacher_side(s, p, lane, LANES, some);
+    int id[K];
+    float tm = -INFINITY;
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        id[k] = slot_id(p, raw[k], t[k]);
+        if (id[k] >= 0) {
+            tm = fmaxf(tm, t[k]);
+            any = true;
+        }
+    }
+    tm = lanes_max(tm, LANES);
+    const unsigned votes = __ballot_sync(0xffffffffu, any);
+    const unsigned of_row = (0xffffffffu >> (32 - LANES)) << ((tid & 31) - lane);
+    const bool some = (votes & of_row) != 0;
+    float ts = 0.0f, h = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const float x = t[k] - tm;
+        t[k] = id[k] >= 0 ? ex2_approx_ftz(x * p.c) : 0.0f;
+        ts += t[k];
+        // (a slot whose share has vanished has no part)
+        if (t[k] > 0.0f || t[k] != t[k]) h = fmaf(t[k], x, h);
+    }
+    ts = lanes_sum(ts, LANES);
+    h = lanes_sum(h, LANES);
+    const float inv_ts = 1.0f / ts;
+    float loss = 0.0f;
+    const float entropy = fmaf(h * inv_ts, p.inv_t, -logf(ts));
+    // the share of each class, -1 in all its slots but the first
+    bool lost = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        t[k] *= inv_ts;
+        if (id[k] >= 0) owner[id[k]] = static_cast<uint8_t>(lane + k * LANES);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (id[k] >= 0) lost = lost || owner[id[k]] != lane + k * LANES;
+    if (__any_sync(0xffffffffu, lost)) {
+        float share[K];
+        bool first[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) share[k] = 0.0f, first[k] = true;
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll 1
+            for (int l = 0; l < LANES; ++l) {
+                const int other = __shfl_sync(0xffffffffu, id[j], (tid & 31) - lane + l);
+                const float part = __shfl_sync(0xffffffffu, t[j], (tid & 31) - lane + l);
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+                    if (other == id[k]) {
+                        share[k] += part;
+                        if (l + j * LANES < lane + k * LANES) first[k] = false;
+                    }
+            }
+#pragma unroll
+        for (int k = 0; k < K; ++k) t[k] = first[k] ? share[k] : -1.0f;
+    }
     copies_wait<0>();
     __syncthreads();
     // the row's words: `odd` elements of the row before it stand in the first one
     T* mine = reinterpret_cast<T*>(tile) + view.head + tr * pitch;
     const int odd = N == 2 ? (view.head + tr * pitch) & 1 : 0;
     T* words = mine - odd;
+    const int classes = active ? p.classes : 0;
     float v[W][N];
     Largest<T, N> largest;
 #pragma unroll
@@ -840,13 +883,9 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         const int e0 = N * (lane + j * LANES) - odd;  // element of the word's first
         Raw<T, N> r;
         r.w[0] = N == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
-        if (active && e0 < p.classes) {
-            r.load(words + N * (lane + j * LANES));
-            if (N == 2) {
-                if (e0 < 0) r.w[0] = (r.w[0] & 0xFFFF0000u) | 0xFF80u;
-                if (e0 + 1 >= p.classes) r.w[0] = (r.w[0] & 0xFFFFu) | 0xFF800000u;
-            }
-        }
+        if (e0 < classes) r.load(words + N * (lane + j * LANES));
+        if (N == 2 && j == 0 && e0 < 0) r.w[0] = (r.w[0] & 0xFFFF0000u) | 0xFF80u;
+        if (N == 2 && e0 + 1 >= classes) r.w[0] = (r.w[0] & 0xFFFFu) | 0xFF800000u;
         if (MODE & LOSS) largest.add(r);
         r.values(v[j]);
     }
@@ -862,20 +901,20 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         ln_s = logf(sum);
         lse = fmaf(m, p.inv_t, ln_s);
     }
-    __syncwarp();  // (p of every slot)
     g = some ? g * p.scale : 0.0f;
     auto q_of = [&](float x) {
         return MODE & LOSS ? ex2_approx_ftz((x - m) * p.c) * inv_s
                            : ex2_approx_ftz(fmaf(x, p.inv_t, -lse) * LOG2E);
     };
-    float loss = 0.0f;
-    for (int k = lane; k < p.top; k += LANES) {
-        share[k] = -1.0f;
-        if (s.id[k] < 0) continue;
-        const float f = class_share(s, k), zk = element(mine + s.id[k]);
-        share[k] = f;
-        s.z[k] = zk;
-        if (f > 0.0f || f != f) loss = fmaf(-f, (zk - m) * p.inv_t - ln_s, loss);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (t[k] == -1.0f) id[k] = -1;
+        if (id[k] < 0) continue;
+        const float z = element(mine + id[k]), share = t[k];
+        if (MODE & LOSS)
+            if (share > 0.0f || share != share)
+                loss = fmaf(-share, (z - m) * p.inv_t - ln_s, loss);
+        if (MODE & GRAD) t[k] = g * (q_of(z) - share);  // the gradient there
     }
     if (MODE & LOSS) {
         loss = lanes_sum(loss, LANES) + entropy;
@@ -887,29 +926,33 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
     if (MODE & GRAD) {
         __syncwarp();  // every slot's logit is read
         const float gs = g * inv_s;
+        const uint32_t keep = g == 0.0f ? 0u : ~0u;  // (0 whatever the logits are)
+        const int end = active ? pitch : -1;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
             const int e0 = N * (lane + j * LANES) - odd;
-            if (!active || e0 >= pitch) break;
+            if (!(MODE & LOSS)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (!(MODE & LOSS)) v[j][i] = q_of(v[j][i]);
-                v[j][i] = g == 0.0f || e0 + i >= p.classes ? 0.0f : v[j][i] * gs;
+                for (int i = 0; i < N; ++i) v[j][i] = q_of(v[j][i]);
             }
+            times(v[j], gs);
+            Raw<T, N> r;
+            r.set(v[j]);
+            r.w[0] &= keep;
+            if (e0 + N > p.classes) r.w[0] &= e0 + 1 == p.classes ? 0xFFFFu : 0u;  // padding
             T* at = words + N * (lane + j * LANES);
-            if (N == 1 || (e0 >= 0 && e0 + 1 < pitch)) {
-                Raw<T, N> r;
-                r.set(v[j]);
+            if (N == 1 ? e0 < end : (j > 0 || e0 >= 0) && e0 + 1 < end) {
                 r.store(at);
-            } else {  // a word that two rows share
-                if (e0 >= 0) put(at, v[j][0]);
-                else put(at + 1, v[j][N - 1]);
+            } else if (N == 2 && e0 < end) {  // a word that two rows share
+                const bool high = j == 0 && e0 < 0;
+                *reinterpret_cast<unsigned short*>(high ? at + 1 : at) =
+                    static_cast<unsigned short>(high ? r.w[0] >> 16 : r.w[0]);
             }
         }
         __syncwarp();
-        for (int k = lane; k < p.top && g != 0.0f; k += LANES)
-            if (s.id[k] >= 0 && share[k] != -1.0f)
-                put(mine + s.id[k], g * (q_of(s.z[k]) - share[k]));
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (id[k] >= 0 && g != 0.0f) put(mine + id[k], t[k]);
         __syncthreads();
         T* out = static_cast<T*>(p.dz) + row0 * p.pitch;
         const bool aligned = (reinterpret_cast<uintptr_t>(out - view.head) & 15u) == 0;
@@ -925,14 +968,14 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
 }
 
 size_t tile_bytes(const DistillParams& p, int size, int lanes) {
-    const size_t rows = TILE_THREADS / lanes, top4 = (p.top + 3) & ~3;
-    return ((rows * p.pitch * size + 15) / 16 + 1) * 16 + rows * top4 * 16;
+    const size_t rows = TILE_THREADS / lanes;
+    return ((rows * p.pitch * size + 15) / 16 + 1) * 16 + rows * p.pitch;
 }
 
-template <typename T, int MODE, int LANES, int W>
+template <typename T, int MODE, int LANES, int W, int K>
 cudaError_t launch_distill_tile(const DistillParams& p, cudaStream_t stream) {
     constexpr int ROWS = TILE_THREADS / LANES;
-    return launch_pdl(distill_tile_kernel<T, MODE, LANES, W>,
+    return launch_pdl(distill_tile_kernel<T, MODE, LANES, W, K>,
                       dim3(static_cast<unsigned>((p.rows + ROWS - 1) / ROWS)), dim3(TILE_THREADS),
                       tile_bytes(p, sizeof(T), LANES), stream, p);
 }
@@ -941,23 +984,23 @@ template <typename T, int MODE>
 cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_t stream) {
     constexpr int size = static_cast<int>(sizeof(T));
     constexpr size_t SMEM = 46 << 10;
-    // a row's words, with one that it may share: eight a lane, up to 32 of a whole warp
+    // a row's words, with one that it may share: 16 and four slots a lane, up to 32 and eight of a
+    // whole warp
     const bool even = (static_cast<uintptr_t>(p.pitch * size) | reinterpret_cast<uintptr_t>(p.z)) % 4 == 0;
     const long long words = p.pitch * size / 4 + (even ? 0 : 1);
     if (words <= 32 * 32) {
         int lanes = 4;
-        while (lanes < 32 && (8 * lanes < words || 8 * lanes < p.top ||
+        while (lanes < 32 && (16 * lanes < words || 4 * lanes < p.top ||
                               tile_bytes(p, size, lanes) > SMEM))
             lanes *= 2;
-        if (tile_bytes(p, size, lanes) <= SMEM) {
-            switch (lanes) {
-                case 4: return launch_distill_tile<T, MODE, 4, 8>(p, stream);
-                case 8: return launch_distill_tile<T, MODE, 8, 8>(p, stream);
-                case 16: return launch_distill_tile<T, MODE, 16, 8>(p, stream);
-                default:
-                    return words <= 32 * 8 ? launch_distill_tile<T, MODE, 32, 8>(p, stream)
-                                           : launch_distill_tile<T, MODE, 32, 32>(p, stream);
-            }
+        switch (lanes) {
+            case 4: return launch_distill_tile<T, MODE, 4, 16, 4>(p, stream);
+            case 8: return launch_distill_tile<T, MODE, 8, 16, 4>(p, stream);
+            case 16: return launch_distill_tile<T, MODE, 16, 16, 4>(p, stream);
+            default:
+                return words <= 32 * 16 && p.top <= 32 * 4
+                           ? launch_distill_tile<T, MODE, 32, 16, 4>(p, stream)
+                           : launch_distill_tile<T, MODE, 32, 32, 8>(p, stream);
         }
     }
     // blocks of a row: as many as its chunks need to stay in registers, more while there are

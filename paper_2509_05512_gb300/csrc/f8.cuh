@@ -59,6 +59,12 @@ __device__ __forceinline__ void f8x4_to_f32(uint32_t w, float (&v)[4]) {
     }
 }
 
+__device__ __forceinline__ float f8_to_f32(uint8_t b) {
+    float v[4];
+    f8x4_to_f32(b, v);
+    return v[0];
+}
+
 // ------------------------------------------------------------------ activations
 
 // SiLU z / (1 + e^-z), e^-z = 2^(-z log2 e), with the hardware's approximate 2^x and reciprocal,

@@ -401,8 +401,9 @@ cudaError_t launch_f8_rows(F8Rows r, cudaStream_t stream) {
     }
 }
 
-// Rows read back: a thread takes 16 channels of a component (a 16-byte load, LV channels a store) of
-// F8_ROWS_UNROLL rows, as above.  Bound by HBM: 1 byte read, 2 written a channel.
+// Rows read back: a thread takes eight channels of a component of F8_DEQUANT_UNROLL rows, as above, all
+// loads first.  The last rows go first: their writer has just left them in L2.  Bound by HBM: 1 byte
+// read, 2 written a channel.
 struct F8Dequant {
     const uint8_t* q;    // [rows][4][Kp]
     const float* scale;  // [4][kblk][pitch]
@@ -412,48 +413,88 @@ struct F8Dequant {
     int group;  // rows side by side in a block of threads
 };
 
-template <int LV>
+constexpr int F8_DEQUANT_UNROLL = 8;
+
 __global__ void __launch_bounds__(256) f8_dequant_kernel(const F8Dequant p) {
     griddep_launch_dependents();
     griddep_wait();
-    const unsigned units = p.Kp / 16, per_row = 4u * units;
+    const unsigned units = p.Kq / 8, per_row = 4u * units;
     const unsigned unit = blockIdx.y * 256u + threadIdx.x;
     const unsigned r0 = unit / per_row, rest = unit - r0 * per_row;
-    const unsigned ci = rest / units, k = (rest - ci * units) * 16;
+    const unsigned ci = rest / units, k = (rest - ci * units) * 8;
     if (r0 >= static_cast<unsigned>(p.group)) return;
-    const long long row0 = static_cast<long long>(blockIdx.x) * (p.group * F8_ROWS_UNROLL) + r0;
-    uint4 w[F8_ROWS_UNROLL];
-    float s[F8_ROWS_UNROLL];
+    const long long row0 = static_cast<long long>(gridDim.x - 1 - blockIdx.x) *
+                               (p.group * F8_DEQUANT_UNROLL) + r0;
+    const uint8_t* q = p.q + (row0 * 4 + ci) * p.Kp + k;
+    const float* scale =
+        p.scale + (static_cast<long long>(ci) * p.kblk + k / F8_BLOCK) * p.pitch + row0;
+    __nv_bfloat16* out = p.out + row0 * (4LL * p.Kq) + static_cast<long long>(ci) * p.Kq + k;
+    const int left = p.rows - row0 < p.group * F8_DEQUANT_UNROLL
+                         ? static_cast<int>(p.rows - row0)
+                         : p.group * F8_DEQUANT_UNROLL;
+    uint2 w[F8_DEQUANT_UNROLL];
+    float s[F8_DEQUANT_UNROLL];
 #pragma unroll
-    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
-        const long long row = row0 + i * p.group;
-        if (row >= p.rows) break;
-        w[i] = *reinterpret_cast<const uint4*>(p.q + (row * 4 + ci) * p.Kp + k);
-        s[i] = p.scale[(static_cast<long long>(ci) * p.kblk + k / F8_BLOCK) * p.pitch + row];
-    }
-#pragma unroll
-    for (int i = 0; i < F8_ROWS_UNROLL; ++i) {
-        const long long row = row0 + i * p.group;
-        if (row >= p.rows) break;
-        __nv_bfloat16* out = p.out + row * (4LL * p.Kq) + static_cast<long long>(ci) * p.Kq + k;
-        const uint32_t word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-        float v[16];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float d[4];
-            f8x4_to_f32(word[j], d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * j + e] = d[e] * s[i];
+    for (int i = 0; i < F8_DEQUANT_UNROLL; ++i)
+        if (i * p.group < left) {
+            w[i] = *reinterpret_cast<const uint2*>(q + static_cast<long long>(i * p.group) *
+                                                           (4LL * p.Kp));
+            s[i] = scale[i * p.group];
         }
 #pragma unroll
-        for (int j = 0; j < 16; j += LV) {
-            if (static_cast<int>(k) + j >= p.Kq) break;
-            float part[LV];
+    for (int i = 0; i < F8_DEQUANT_UNROLL; ++i)
+        if (i * p.group < left) {
+            float v[8], d[4];
+            f8x4_to_f32(w[i].x, d);
 #pragma unroll
-            for (int e = 0; e < LV; ++e) part[e] = v[j + e];
-            Raw<__nv_bfloat16, LV> o;
-            o.set(part);
-            o.store(out + j);
+            for (int j = 0; j < 4; ++j) v[j] = d[j] * s[i];
+            f8x4_to_f32(w[i].y, d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 + j] = d[j] * s[i];
+            Raw<__nv_bfloat16, 8> o;
+            o.set(v);
+            o.store(out + static_cast<long long>(i * p.group) * (4LL * p.Kq));
+        }
+}
+
+// The same of components that are not whole chunks of eight: eight elements of the output a thread,
+// wherever rows and components begin, eight rows a block (a multiple of eight elements).
+__global__ void __launch_bounds__(256) f8_dequant_any_kernel(const F8Dequant p) {
+    griddep_launch_dependents();
+    griddep_wait();
+    const long long row0 = static_cast<long long>(gridDim.x - 1 - blockIdx.x) * 8;
+    const int rows = p.rows - row0 < 8 ? static_cast<int>(p.rows - row0) : 8;
+    const unsigned C = 4u * p.Kq, n = rows * C;
+    __nv_bfloat16* out = p.out + row0 * C;
+    const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+    for (unsigned f = 8u * threadIdx.x; f < n; f += 8u * 256u) {
+        unsigned r = f / C, k = f - r * C, ci = k / p.Kq;
+        k -= ci * p.Kq;
+        const uint8_t* q = p.q + ((row0 + r) * 4 + ci) * p.Kp;
+        float s = 0.0f, v[8];
+        bool fresh = true;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = 0.0f;
+            if (f + j >= n) continue;
+            if (fresh || k % F8_BLOCK == 0)
+                s = p.scale[(static_cast<long long>(ci) * p.kblk + k / F8_BLOCK) * p.pitch + row0 + r];
+            v[j] = f8_to_f32(q[k]) * s;
+            fresh = ++k == static_cast<unsigned>(p.Kq);
+            if (fresh) {
+                k = 0;
+                q += p.Kp;
+                if (++ci == 4) ci = 0, ++r;
+            }
+        }
+        if (aligned && f + 8 <= n) {
+            Raw<__nv_bfloat16, 8> o;
+            o.set(v);
+            o.store(out + f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (f + j < n) out[f + j] = __float2bfloat16_rn(v[j]);
         }
     }
 }
@@ -474,16 +515,16 @@ cudaError_t launch_f8_dequant(const void* q, const float* scale, long long rows,
                               cudaStream_t stream) {
     F8Dequant p = {static_cast<const uint8_t*>(q), scale, static_cast<__nv_bfloat16*>(out), rows,
                    f8_scale_pitch(rows), Kq, f8_pitch(Kq), blocks_of(Kq), 0};
-    const int per_row = p.Kp / 4;
+    if (Kq % 8 != 0 || reinterpret_cast<uintptr_t>(out) % 16 != 0)
+        return launch_pdl(f8_dequant_any_kernel, dim3(static_cast<unsigned>((rows + 7) / 8)),
+                          dim3(256), 0, stream, p);
+    const int per_row = Kq / 2;
     p.group = per_row < 256 ? 256 / per_row : 1;
-    const dim3 g(static_cast<unsigned>((rows + p.group * F8_ROWS_UNROLL - 1) /
-                                       (p.group * F8_ROWS_UNROLL)),
-                 static_cast<unsigned>((per_row + 255) / 256));
-    switch (load_channels(Kq, reinterpret_cast<uintptr_t>(out))) {
-        case 8: return launch_pdl(f8_dequant_kernel<8>, g, dim3(256), 0, stream, p);
-        case 2: return launch_pdl(f8_dequant_kernel<2>, g, dim3(256), 0, stream, p);
-        default: return launch_pdl(f8_dequant_kernel<1>, g, dim3(256), 0, stream, p);
-    }
+    return launch_pdl(f8_dequant_kernel,
+                      dim3(static_cast<unsigned>((rows + p.group * F8_DEQUANT_UNROLL - 1) /
+                                                 (p.group * F8_DEQUANT_UNROLL)),
+                           static_cast<unsigned>((per_row + 255) / 256)),
+                      dim3(256), 0, stream, p);
 }
 
 cudaError_t launch_f8_letters(const void* const w[4], int Qout, int Qin, bool transpose, void* q,
