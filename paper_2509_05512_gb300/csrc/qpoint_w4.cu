@@ -23,6 +23,8 @@
 // Inputs are read with plain loads only, behind the wait for the grid before this one.
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "f8.cuh"
 #include "internal.h"
 #include "ptx.cuh"
@@ -159,89 +161,13 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t (&a)[4]) {
 
 constexpr int W4_WARPS = 8;
 
-// 16 output channels and 2 NT pixels a block, or a cluster that splits the inputs.  A warp takes a
-// letter's block of 64 inputs at a time.
-template <int NT, int LV, bool G32>
-__global__ void __launch_bounds__(32 * W4_WARPS) qpoint_w4_kernel(const W4Params p) {
-    __shared__ float part[W4_WARPS][NT * 128];
-    griddep_launch_dependents();
-    griddep_wait();
+// The warps' sums, and the cluster's, in a fixed order, and the output.  `part`: a row of NT x 128 values
+// a warp, element e of a tile's 16 x 8 being channel e mod 16 of column e / 16.
+template <int NT>
+__device__ __forceinline__ void w4_finish(const W4Params& p, float (&acc)[NT][4],
+                                          float (*part)[NT * 128], int rank, int nt,
+                                          long long row0) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const unsigned tile = blockIdx.x / static_cast<unsigned>(p.split);
-    const int rank = static_cast<int>(blockIdx.x - tile * p.split), nt = blockIdx.y;
-    const long long row0 = static_cast<long long>(tile) * (2 * NT);
-    // this lane's column of an MMA: pixel and output component
-    const int co = g & 3;
-    float acc[NT][4] = {};
-    const int items = 4 * p.ktiles, per = (items + p.split - 1) / p.split;
-    const int end = (rank + 1) * per < items ? (rank + 1) * per : items;
-    constexpr int U = NT == 1 ? 4 : 2;  // blocks whose loads go out together
-    for (int i0 = rank * per + warp; i0 < end; i0 += U * W4_WARPS) {
-        uint4 q[U];
-        uint32_t s[U][2], x[U][NT > 2 ? 1 : NT][8];
-        auto load_x = [&](int i, int j, uint32_t (&w)[8]) {
-            const int L = i & 3, k = (i >> 2) * W4_TILE_K + 8 * t, ci = co ^ L;
-            const long long row = row0 + 2 * j + (g >> 2);
-            const uint32_t neg = (tc::NEG_MASK >> (4 * co + ci)) & 1u ? 0x80008000u : 0u;
-            const __nv_bfloat16* src =
-                p.x + row * (4LL * p.Qi) + static_cast<long long>(ci) * p.Qi + k;
-            const int left = row < p.rows ? p.Qi - k : 0;
-            load_words8<LV>(src, left, w);
-            load_words8<LV>(src + 32, left - 32, w + 4);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] ^= neg;
-        };
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * W4_WARPS;
-            if (i >= end) break;
-            const int L = i & 3, kt = i >> 2;
-            const long long block = (static_cast<long long>(L) * p.ntiles + nt) * p.ktiles + kt;
-            q[u] = p.q[block * 32 + lane];
-            const uint32_t* sc = p.scale + (static_cast<long long>(L) * p.ntiles + nt) * p.groups * 8;
-            // (64 inputs are two groups of 32, one of 64 or half of one of 128)
-            if constexpr (G32) {
-                s[u][0] = sc[2 * kt * 8 + g];
-                s[u][1] = 2 * kt + 1 < p.groups ? sc[(2 * kt + 1) * 8 + g] : 0u;
-            } else {
-                s[u][0] = sc[(kt >> p.wide) * 8 + g];
-            }
-            if constexpr (NT <= 2) {
-#pragma unroll
-                for (int j = 0; j < NT; ++j) load_x(i, j, x[u][j]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * W4_WARPS;
-            if (i >= end) break;
-            uint32_t a[4][4];
-            widen(q[u].x, a[0]);
-            widen(q[u].y, a[1]);
-            widen(q[u].z, a[2]);
-            widen(q[u].w, a[3]);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if constexpr (NT > 2) load_x(i, j, x[u][0]);
-                const uint32_t(&b)[8] = x[u][NT > 2 ? 0 : j];
-#pragma unroll
-                for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-                    float c[4] = {};
-#pragma unroll
-                    for (int e = 0; e < (G32 ? 2 : 4); ++e)
-                        mma_bf16(c, a[2 * h + e], b[4 * h + 2 * e], b[4 * h + 2 * e + 1]);
-                    float lo, hi;
-                    bf16x2_to_f32(s[u][h], lo, hi);
-                    acc[j][0] = fmaf(lo, c[0], acc[j][0]);
-                    acc[j][1] = fmaf(lo, c[1], acc[j][1]);
-                    acc[j][2] = fmaf(hi, c[2], acc[j][2]);
-                    acc[j][3] = fmaf(hi, c[3], acc[j][3]);
-                }
-            }
-        }
-    }
-    // the warps' sums, and the cluster's, in a fixed order; element e of a tile's 16 x 8 values is
-    // channel e mod 16 of column e / 16
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -293,28 +219,233 @@ __global__ void __launch_bounds__(32 * W4_WARPS) qpoint_w4_kernel(const W4Params
     }
 }
 
-template <int NT, int LV>
-cudaError_t launch_w4_lv(W4Params p, bool g32, int num_sms, cudaStream_t stream) {
+// 16 output channels and 2 NT pixels a block, or a cluster that splits the inputs.  A warp takes a
+// letter's block of 64 inputs at a time.
+template <int NT, bool G32>
+__global__ void __launch_bounds__(32 * W4_WARPS) qpoint_w4_kernel(const W4Params p) {
+    __shared__ float part[W4_WARPS][NT * 128];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const unsigned tile = blockIdx.x / static_cast<unsigned>(p.split);
+    const int rank = static_cast<int>(blockIdx.x - tile * p.split), nt = blockIdx.y;
+    const long long row0 = static_cast<long long>(tile) * (2 * NT);
+    // this lane's column of an MMA: pixel and output component
+    const int co = g & 3;
+    float acc[NT][4] = {};
+    const int items = 4 * p.ktiles, per = (items + p.split - 1) / p.split;
+    const int end = (rank + 1) * per < items ? (rank + 1) * per : items;
+    constexpr int U = NT == 1 ? 4 : 2;  // blocks whose loads go out together
+    for (int i0 = rank * per + warp; i0 < end; i0 += U * W4_WARPS) {
+        uint4 q[U];
+        uint32_t s[U][2], x[U][NT][8];
+        auto load_x = [&](int i, int j, uint32_t (&w)[8]) {
+            const int L = i & 3, k = (i >> 2) * W4_TILE_K + 8 * t, ci = co ^ L;
+            const long long row = row0 + 2 * j + (g >> 2);
+            const uint32_t neg = (tc::NEG_MASK >> (4 * co + ci)) & 1u ? 0x80008000u : 0u;
+            const __nv_bfloat16* src =
+                p.x + row * (4LL * p.Qi) + static_cast<long long>(ci) * p.Qi + k;
+            const int left = row < p.rows ? p.Qi - k : 0;
+            load_words8<8>(src, left, w);
+            load_words8<8>(src + 32, left - 32, w + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] ^= neg;
+        };
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * W4_WARPS;
+            if (i >= end) break;
+            const int L = i & 3, kt = i >> 2;
+            const long long block = (static_cast<long long>(L) * p.ntiles + nt) * p.ktiles + kt;
+            q[u] = p.q[block * 32 + lane];
+            const uint32_t* sc = p.scale + (static_cast<long long>(L) * p.ntiles + nt) * p.groups * 8;
+            // (64 inputs are two groups of 32, one of 64 or half of one of 128)
+            if constexpr (G32) {
+                s[u][0] = sc[2 * kt * 8 + g];
+                s[u][1] = 2 * kt + 1 < p.groups ? sc[(2 * kt + 1) * 8 + g] : 0u;
+            } else {
+                s[u][0] = sc[(kt >> p.wide) * 8 + g];
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) load_x(i, j, x[u][j]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * W4_WARPS;
+            if (i >= end) break;
+            uint32_t a[4][4];
+            widen(q[u].x, a[0]);
+            widen(q[u].y, a[1]);
+            widen(q[u].z, a[2]);
+            widen(q[u].w, a[3]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const uint32_t(&b)[8] = x[u][j];
+#pragma unroll
+                for (int h = 0; h < (G32 ? 2 : 1); ++h) {
+                    float c[4] = {};
+#pragma unroll
+                    for (int e = 0; e < (G32 ? 2 : 4); ++e)
+                        mma_bf16(c, a[2 * h + e], b[4 * h + 2 * e], b[4 * h + 2 * e + 1]);
+                    float lo, hi;
+                    bf16x2_to_f32(s[u][h], lo, hi);
+                    acc[j][0] = fmaf(lo, c[0], acc[j][0]);
+                    acc[j][1] = fmaf(lo, c[1], acc[j][1]);
+                    acc[j][2] = fmaf(hi, c[2], acc[j][2]);
+                    acc[j][3] = fmaf(hi, c[3], acc[j][3]);
+                }
+            }
+        }
+    }
+    w4_finish<NT>(p, acc, part, rank, nt, row0);
+}
+
+// The same with the pixels' channels staged in shared memory, KT blocks of 64 inputs at a time: for
+// more pixels than fit a lane's registers, and where their channels cannot be loaded eight at a time.
+// Components of pixels stand 64 bytes past a multiple of 128 apart, so that the two that a quarter of a
+// warp reads lie in different banks.  49 rows 2048 -> 2048: 12.4 us with loads of their own for every
+// MMA, whose trips to L2 added up.
+template <int NT>
+struct W4Stage {
+    static constexpr int KT = NT >= 8 ? 8 : NT == 4 ? 16 : 32;
+    static constexpr int PITCH = KT * W4_TILE_K * 2 + 64;  // bytes of a component
+    static constexpr int BYTES = 2 * NT * 4 * PITCH;
+};
+
+template <int NT, int LV, bool G32>
+__global__ void __launch_bounds__(32 * W4_WARPS) qpoint_w4_staged_kernel(const W4Params p) {
+    using S = W4Stage<NT>;
+    static_assert(S::BYTES >= W4_WARPS * NT * 128 * 4, "the warps' sums take the stage's place");
+    extern __shared__ int4 stage[];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const unsigned tile = blockIdx.x / static_cast<unsigned>(p.split);
+    const int rank = static_cast<int>(blockIdx.x - tile * p.split), nt = blockIdx.y;
+    const long long row0 = static_cast<long long>(tile) * (2 * NT);
+    const int co = g & 3, per = (p.ktiles + p.split - 1) / p.split;
+    const int last = (rank + 1) * per < p.ktiles ? (rank + 1) * per : p.ktiles;
+    char* xs = reinterpret_cast<char*>(stage);
+    float acc[NT][4] = {};
+    constexpr int U = 4;  // blocks of letters whose loads go out together
+    for (int k0 = rank * per; k0 < last; k0 += S::KT) {
+        const int kts = last - k0 < S::KT ? last - k0 : S::KT, items = 4 * kts;
+        uint4 q[U];
+        uint32_t s[U][2];
+        auto letters = [&](int first) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = first + u * W4_WARPS;
+                if (i >= items) break;
+                const int L = i & 3, kt = k0 + (i >> 2);
+                const long long block = (static_cast<long long>(L) * p.ntiles + nt) * p.ktiles + kt;
+                q[u] = p.q[block * 32 + lane];
+                const uint32_t* sc =
+                    p.scale + (static_cast<long long>(L) * p.ntiles + nt) * p.groups * 8;
+                if constexpr (G32) {
+                    s[u][0] = sc[2 * kt * 8 + g];
+                    s[u][1] = 2 * kt + 1 < p.groups ? sc[(2 * kt + 1) * 8 + g] : 0u;
+                } else {
+                    s[u][0] = sc[(kt >> p.wide) * 8 + g];
+                }
+            }
+        };
+        letters(warp);
+        // the pixels' channels of these blocks, eight a thread, 0 past the last
+        for (int i = threadIdx.x; i < 2 * NT * 4 * 8 * kts; i += 32 * W4_WARPS) {
+            const int c = i / (8 * kts), k = (i - c * 8 * kts) * 8;  // component of a pixel
+            const long long row = row0 + (c >> 2);
+            const int at = k0 * W4_TILE_K + k, left = row < p.rows ? p.Qi - at : 0;
+            const __nv_bfloat16* src =
+                p.x + row * (4LL * p.Qi) + static_cast<long long>(c & 3) * p.Qi + at;
+            uint32_t w[4];
+            load_words8<LV>(src, left, w);
+            *reinterpret_cast<uint4*>(xs + c * S::PITCH + k * 2) =
+                make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        __syncthreads();
+        for (int i0 = warp; i0 < items; i0 += U * W4_WARPS) {
+            if (i0 != warp) letters(i0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * W4_WARPS;
+                if (i >= items) break;
+                const int L = i & 3, ci = co ^ L;
+                const uint32_t neg = (tc::NEG_MASK >> (4 * co + ci)) & 1u ? 0x80008000u : 0u;
+                const char* at = xs + ((g >> 2) * 4 + ci) * S::PITCH + (i >> 2) * 128 + 16 * t;
+                uint32_t a[4][4];
+                widen(q[u].x, a[0]);
+                widen(q[u].y, a[1]);
+                widen(q[u].z, a[2]);
+                widen(q[u].w, a[3]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const uint4 b0 = *reinterpret_cast<const uint4*>(at + j * 8 * S::PITCH);
+                    const uint4 b1 = *reinterpret_cast<const uint4*>(at + j * 8 * S::PITCH + 64);
+                    const uint32_t b[8] = {b0.x ^ neg, b0.y ^ neg, b0.z ^ neg, b0.w ^ neg,
+                                           b1.x ^ neg, b1.y ^ neg, b1.z ^ neg, b1.w ^ neg};
+#pragma unroll
+                    for (int h = 0; h < (G32 ? 2 : 1); ++h) {
+                        float c[4] = {};
+#pragma unroll
+                        for (int e = 0; e < (G32 ? 2 : 4); ++e)
+                            mma_bf16(c, a[2 * h + e], b[4 * h + 2 * e], b[4 * h + 2 * e + 1]);
+                        float lo, hi;
+                        bf16x2_to_f32(s[u][h], lo, hi);
+                        acc[j][0] = fmaf(lo, c[0], acc[j][0]);
+                        acc[j][1] = fmaf(lo, c[1], acc[j][1]);
+                        acc[j][2] = fmaf(hi, c[2], acc[j][2]);
+                        acc[j][3] = fmaf(hi, c[3], acc[j][3]);
+                    }
+                }
+            }
+        }
+        __syncthreads();  // before the stage is filled again
+    }
+    w4_finish<NT>(p, acc, reinterpret_cast<float(*)[NT * 128]>(stage), rank, nt, row0);
+}
+
+template <int NT, int LV, bool G32>
+cudaError_t launch_w4_form(W4Params p, int num_sms, cudaStream_t stream) {
+    // staged for more than four pixels, or channels that are not loaded eight at a time
+    constexpr bool STAGED = NT > 2 || LV != 8;
     const long long tiles = (p.rows + 2 * NT - 1) / (2 * NT);
     // the inputs are split while the blocks are fewer than the SMs' and a warp keeps two blocks
+    // of letters
     p.split = 1;
-    while (p.split < 8 && tiles * p.ntiles * p.split < 2 * num_sms &&
+    while (p.split < 8 && tiles * p.ntiles * p.split < (STAGED ? 1 : 2) * num_sms &&
            4 * p.ktiles >= 4 * W4_WARPS * p.split)
         p.split *= 2;
     const dim3 g(static_cast<unsigned>(tiles * p.split), static_cast<unsigned>(p.ntiles));
     const unsigned cluster = static_cast<unsigned>(p.split);
-    return g32 ? launch_pdl_cluster(qpoint_w4_kernel<NT, LV, true>, g, dim3(32 * W4_WARPS), cluster,
-                                    0, stream, p)
-               : launch_pdl_cluster(qpoint_w4_kernel<NT, LV, false>, g, dim3(32 * W4_WARPS),
-                                    cluster, 0, stream, p);
+    if constexpr (STAGED) {
+        constexpr int BYTES = W4Stage<NT>::BYTES;
+        auto* kern = qpoint_w4_staged_kernel<NT, LV, G32>;
+        static std::atomic<unsigned long long> ready{0};  // once a device: the shared memory
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev >= 64 || !((ready.load(std::memory_order_acquire) >> dev) & 1ull)) {
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES);
+            if (e != cudaSuccess) return e;
+            if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+        }
+        return launch_pdl_cluster(kern, g, dim3(32 * W4_WARPS), cluster, BYTES, stream, p);
+    } else {
+        return launch_pdl_cluster(qpoint_w4_kernel<NT, G32>, g, dim3(32 * W4_WARPS), cluster, 0,
+                                  stream, p);
+    }
 }
 
 template <int NT>
 cudaError_t launch_w4_nt(const W4Params& p, bool g32, int num_sms, cudaStream_t stream) {
     switch (load_channels(p.Qi, reinterpret_cast<uintptr_t>(p.x))) {
-        case 8: return launch_w4_lv<NT, 8>(p, g32, num_sms, stream);
-        case 2: return launch_w4_lv<NT, 2>(p, g32, num_sms, stream);
-        default: return launch_w4_lv<NT, 1>(p, g32, num_sms, stream);
+        case 8: return g32 ? launch_w4_form<NT, 8, true>(p, num_sms, stream)
+                           : launch_w4_form<NT, 8, false>(p, num_sms, stream);
+        case 2: return g32 ? launch_w4_form<NT, 2, true>(p, num_sms, stream)
+                           : launch_w4_form<NT, 2, false>(p, num_sms, stream);
+        default: return g32 ? launch_w4_form<NT, 1, true>(p, num_sms, stream)
+                            : launch_w4_form<NT, 1, false>(p, num_sms, stream);
     }
 }
 
