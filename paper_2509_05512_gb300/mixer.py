@@ -13,7 +13,9 @@ draws new masks at each replay.
 
     python -m paper_2509_05512_gb300.mixer --steps 30
 
-trains such a stack on synthetic maps and prints the loss.
+trains such a stack on synthetic maps and prints the loss; with --top 10, by distillation from the
+largest logits of a teacher, its channels taken for classes.  `Mixer.serve` runs a few pixels with
+4-bit letters.
 """
 from __future__ import annotations
 
@@ -122,19 +124,39 @@ class Mixer:
         self.quantize()
 
 
+def distillation(model, x, index, teacher, *, temperature=1.0, training=True):
+    """A stack whose channels are classes against a teacher's top logits (index, teacher
+    [N, H, W, top], as torch.topk gives them): the mean loss over the pixels that have any (a device
+    scalar) and the gradient of model.forward's result, for model.backward."""
+    out = model.forward(x, training=training)
+    pixels = (index >= 0).any(dim=-1)
+    weight = pixels.float() / pixels.sum().clamp(min=1)
+    loss, dn = quan.distill_loss_and_gradient(out, index, teacher, weight,
+                                              temperature=temperature)
+    return (loss * weight).sum(), dn
+
+
 def train(steps: int = 30, N: int = 8, H: int = 16, channels: int = 256, depth: int = 3,
-          lr: float = 0.2, p: float = 0.1, seed: int = 0, report=print) -> list:
-    """Fits a stack to the output of another one on fixed synthetic maps; the losses."""
+          lr: float = 0.2, p: float = 0.1, seed: int = 0, top: int = 0, temperature: float = 1.0,
+          report=print) -> list:
+    """Fits a stack on fixed synthetic maps to the output of another one, or with top > 0, its
+    channels taken for classes, to that many largest logits of the other's; the losses."""
     import torch
     gen = torch.Generator(device="cuda").manual_seed(seed + 1)
     x = torch.randn((N, H, H, channels), generator=gen, device="cuda").to(torch.bfloat16)
     target = Mixer(channels, depth, seed=seed + 2).forward(x, training=False).float()
     model = Mixer(channels, depth, p=p, seed=seed)
+    if top:
+        teacher, index = torch.topk(target, top, dim=-1)
     losses = []
     for step in range(steps):
-        diff = model.forward(x).float() - target
-        losses.append(float(diff.square().mean()))
-        grads = model.backward((2.0 / (N * H * H) * diff).to(torch.bfloat16))
+        if top:
+            loss, dn = distillation(model, x, index, teacher, temperature=temperature)
+        else:
+            diff = model.forward(x).float() - target
+            loss, dn = diff.square().mean(), (2.0 / (N * H * H) * diff).to(torch.bfloat16)
+        losses.append(float(loss))
+        grads = model.backward(dn)
         model.update(grads, lr)
         model.advance()
         if report:
@@ -150,8 +172,12 @@ def main(argv=None) -> None:
     ap.add_argument("--channels", type=int, default=256)
     ap.add_argument("--depth", type=int, default=3)
     ap.add_argument("--dropout", type=float, default=0.1)
+    ap.add_argument("--top", type=int, default=0,
+                    help="distil that many of a teacher's largest logits a pixel")
+    ap.add_argument("--temperature", type=float, default=1.0)
     a = ap.parse_args(argv)
-    train(a.steps, a.images, a.size, channels=a.channels, depth=a.depth, p=a.dropout)
+    train(a.steps, a.images, a.size, channels=a.channels, depth=a.depth, p=a.dropout, top=a.top,
+          temperature=a.temperature)
 
 
 if __name__ == "__main__":
