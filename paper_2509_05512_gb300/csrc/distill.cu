@@ -630,7 +630,9 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
                         for (int j = 0; j < 4; ++j) o.w[j] &= keep;
                         if (k < n && !(k == 0 && part0))
                             o.store(place + k * CT * E);
-                        else  // back to its place in the ring, which nothing overwrites yet
+                        else if (tid + k * CT < view.chunks())
+                            // back to its place in the ring, until the next row is fetched there
+                            // (what no row has keeps its -inf)
                             o.store(mine + k * CT * E);
                     }
                 const int chunks = view.chunks();
@@ -983,7 +985,7 @@ cudaError_t launch_distill_tile(const DistillParams& p, cudaStream_t stream) {
 template <typename T, int MODE>
 cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_t stream) {
     constexpr int size = static_cast<int>(sizeof(T));
-    constexpr size_t SMEM = 46 << 10;
+    constexpr size_t SMEM = 48 << 10;
     // a row's words, with one that it may share: 16 and four slots a lane, up to 32 and eight of a
     // whole warp
     const bool even = (static_cast<uintptr_t>(p.pitch * size) | reinterpret_cast<uintptr_t>(p.z)) % 4 == 0;
@@ -993,7 +995,7 @@ cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_
         while (lanes < 32 && (16 * lanes < words || 4 * lanes < p.top ||
                               tile_bytes(p, size, lanes) > SMEM))
             lanes *= 2;
-        switch (lanes) {
+        if (tile_bytes(p, size, lanes) <= SMEM) switch (lanes) {
             case 4: return launch_distill_tile<T, MODE, 4, 16, 4>(p, stream);
             case 8: return launch_distill_tile<T, MODE, 8, 16, 4>(p, stream);
             case 16: return launch_distill_tile<T, MODE, 16, 16, 4>(p, stream);

@@ -334,3 +334,58 @@ def test_refuses_on_the_device():
         quan.distill_loss(z, i, t, temperature=0.0)
     with pytest.raises(quan.QuanError):
         quan.distill_loss_and_gradient(z, i, t, out=z, loss=z.view(-1)[:4])
+
+
+def reference(d, T):
+    """The oracle's arithmetic for many rows at once, in fp64 on the device."""
+    V, index = d["V"], d["index"].long()
+    z, t = d["z"][:, :V].double() / T, d["teacher"].double() / T
+    valid = (index >= 0) & (index < V) & (t > -float("inf"))
+    some = valid.any(dim=1, keepdim=True)
+    lse = torch.logsumexp(z, dim=1, keepdim=True)
+    logp = torch.log_softmax(torch.where(valid | ~some, t.clamp(min=-1e300), -1e300), dim=1)
+    p = torch.where(valid, logp.exp(), 0.0)
+    at = torch.where(valid, index, 0)
+    loss = T * T * torch.where(p > 0, p * (logp - (z.gather(1, at) - lse)), 0.0).sum(dim=1)
+    share = torch.zeros_like(z).scatter_add_(1, at, p)
+    q = (z - lse).exp()
+    return loss, lse[:, 0], torch.where(some, T * d["g"].double()[:, None] * (q - share), 0.0), q, share
+
+
+MANY = [(3000, 5, 0, 2), (3000, 100, 1, 10), (2500, 513, 0, 40), (2500, 1023, 3, 100),
+        (2000, 2046, 2, 64), (2000, 2048, 0, 256), (2000, 2049, 0, 5), (3000, 2549, 2, 123),
+        (3000, 4246, 3, 20), (2600, 6633, 0, 11), (1300, 8192, 0, 30), (1300, 11321, 0, 4),
+        (700, 16384, 1, 8), (700, 20000, 0, 33), (500, 27855, 2, 27), (500, 32768, 0, 64),
+        (400, 32767, 1, 64), (200, 70003, 0, 9)]
+
+
+@pytest.mark.parametrize("rows, V, pad, top", MANY)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows(rows, V, pad, top, dtype):
+    # more rows than a block of any kind takes at once, of every length that picks another kernel
+    T = 2.0
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.full((rows, V + pad), 9.0, device="cuda", dtype=DT[dtype])
+    z[:, :V] = 3.0 * torch.randn(rows, V, generator=g, device="cuda")
+    # rows of different magnitudes and offsets: what one leaves behind would show in another
+    z[:, :V] *= torch.rand(rows, 1, generator=g, device="cuda") * 2
+    z[:, :V] += 40.0 * torch.randn(rows, 1, generator=g, device="cuda")
+    index = torch.randint(0, V, (rows, top), generator=g, device="cuda")
+    index[torch.rand(rows, generator=g, device="cuda") < 0.1] = -1
+    t = torch.randn(rows, top, generator=g, device="cuda").to(DT[dtype])
+    d = dict(z=z, index=index, teacher=t, V=V, dtype=dtype,
+             g=torch.rand(rows, generator=g, device="cuda") + 0.5)
+    loss, lse, dz, q, share = reference(d, T)
+    args = dict(classes=V, temperature=T)
+    l1, e1 = quan.distill_loss(z, index, t, **args)
+    g1 = quan.distill_loss_backward(d["g"], z, e1, index, t, **args)
+    l2, g2 = quan.distill_loss_and_gradient(z, index, t, d["g"], **args)
+    R = 5e-6 + (V / 128 + 32) * U
+    x = (z[:, :V].double().amax(dim=1) / T).abs() + lse.abs() + 30.0  # |x| of what counts
+    for got in (l1, l2):
+        assert ((got.double() - loss).abs() <= T * T * 2 * (R + 16 * U * x) * (1 + loss / T / T)).all()
+    assert ((e1.double() - lse).abs() <= R + 4 * U * x).all()
+    for got in (g1, g2):
+        assert not got[:, V:].any()
+        tol = T * d["g"].double()[:, None] * (q + share) * (R + 8 * U * (x + 60.0))[:, None]
+        assert ((got[:, :V].double() - dz).abs() <= tol + HALF[dtype] * dz.abs() + 1e-30).all()
