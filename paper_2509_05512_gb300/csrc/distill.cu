@@ -55,21 +55,14 @@ struct RowView {
         n = len;
     }
     __device__ __forceinline__ int chunks() const { return (head + n + E - 1) / E; }
-    // All of a chunk is in the row's first `len` elements; some of it is past the tensor's ends.
+    // All of a chunk is in the row's first `len` elements.
     __device__ __forceinline__ bool whole(int chunk, int len) const {
         return chunk * E >= head && (chunk + 1) * E <= head + len;
     }
+    // Some of it is past the tensor's ends.
     __device__ __forceinline__ bool outside(int chunk) const {
         const T* p = base + chunk * E;
         return p < first || p + E > last;
-    }
-    // A chunk as it is in memory, element by element where it reaches past the tensor's ends.
-    __device__ __forceinline__ void load(int chunk, Raw<T, E>& r) const {
-        if (!outside(chunk)) {
-            r.load(base + chunk * E);
-        } else {
-            load_masked(chunk, n, r);
-        }
     }
     // A chunk of which not all is in the row's first `len` elements, the others -inf.
     __device__ __forceinline__ void load_masked(int chunk, int len, Raw<T, E>& r) const {
@@ -227,6 +220,7 @@ template <int N>
 __device__ __forceinline__ void copies_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+
 // v becomes 2^((v - at) c); `sum` takes its elements by twos.
 template <int N>
 __device__ __forceinline__ void powers(float (&v)[N], float at, float c, float2& sum) {
@@ -530,8 +524,8 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
     };
     if (tid < CT) {
         int4* ring = dynamic + tid;
-        auto view_of = [&](long long row) {
-            return RowView<T>(z, p.rows * p.pitch, row * p.pitch, len);
+        auto view_of = [&](long long row) {  // (its loads stay in the row: no look at the tensor's ends)
+            return RowView<T>(z, 0, row * p.pitch, len);
         };
         // Of a thread's chunks, the first `wholes` are all classes (but for chunk 0 of a row that does
         // not begin on a chunk).
@@ -585,7 +579,7 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             Largest<T, E> largest;
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
-                if (k * CT < most) {
+                if ((k & ~1) * CT < most) {
                     Raw<T, E> r;
                     r.load(mine + k * CT * E);
                     largest.add(r);
@@ -594,7 +588,7 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             float2 sums = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
-                if (k * CT < most) {
+                if ((k & ~1) * CT < most) {
                     Raw<T, E> r;
                     r.load(mine + k * CT * E);
                     r.values(e[k]);
@@ -620,30 +614,40 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
                 const bool part0 = tid == 0 && view.head != 0;
                 const int n = (reinterpret_cast<uintptr_t>(place) & 15u) == 0 ? wholes(view) : 0;
                 const uint32_t keep = g == 0.0f ? 0u : ~0u;  // (0 whatever the logits are)
+                const int chunks = view.chunks();
+                // chunks that are not all classes, or not on 16 bytes: back to their place in the
+                // ring until the next row is fetched there, and from there element by element
+                // (what no row has keeps its -inf)
+                const bool parts = part0 || tid + n * CT < chunks;
 #pragma unroll
                 for (int k = 0; k < NCH; ++k)
-                    if (k * CT < most) {
+                    if ((k & ~1) * CT < most) {
                         Raw<T, E> o;
                         times(e[k], f);
                         o.set(e[k]);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) o.w[j] &= keep;
-                        if (k < n && !(k == 0 && part0))
-                            o.store(place + k * CT * E);
-                        else if (tid + k * CT < view.chunks())
-                            // back to its place in the ring, until the next row is fetched there
-                            // (what no row has keeps its -inf)
-                            o.store(mine + k * CT * E);
+                        if (k < n && (k > 0 || !part0)) o.store(place + k * CT * E);
                     }
-                const int chunks = view.chunks();
-                auto part = [&](int i) {
-                    Raw<T, E> o;
-                    o.load(mine + (i - tid) * E);
-                    view.store_part(i, o, p.classes, out);
-                };
-                if (part0 && n > 0) part(0);
+                if (parts) {
+#pragma unroll
+                    for (int k = 0; k < NCH; ++k)
+                        if (((k == 0 && part0) || k >= n) && tid + k * CT < chunks) {
+                            Raw<T, E> o;
+                            o.set(e[k]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o.w[j] &= keep;
+                            o.store(mine + k * CT * E);
+                        }
+                    auto part = [&](int i) {
+                        Raw<T, E> o;
+                        o.load(mine + (i - tid) * E);
+                        view.store_part(i, o, p.classes, out);
+                    };
+                    if (part0 && n > 0) part(0);
 #pragma unroll 1
-                for (int i = tid + n * CT; i < chunks; i += CT) part(i);
+                    for (int i = tid + n * CT; i < chunks; i += CT) part(i);
+                }
                 named_bar_arrive(1 + H + h, CT + 32);
             }
             h = h == H - 1 ? 0 : h + 1;
@@ -878,10 +882,13 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
     const int odd = N == 2 ? (view.head + tr * pitch) & 1 : 0;
     T* words = mine - odd;
     const int classes = active ? p.classes : 0;
+    // (words are passed over by twos where no row reaches)
+    auto none = [&](int j) { return (j & ~1) * LANES * N > pitch; };
     float v[W][N];
     Largest<T, N> largest;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
+        if (none(j)) break;
         const int e0 = N * (lane + j * LANES) - odd;  // element of the word's first
         Raw<T, N> r;
         r.w[0] = N == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
@@ -897,7 +904,10 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         const float at = m == -INFINITY ? 0.0f : m;
         float2 sums = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int j = 0; j < W; ++j) powers(v[j], at, p.c, sums);
+        for (int j = 0; j < W; ++j) {
+            if (none(j)) break;
+            powers(v[j], at, p.c, sums);
+        }
         const float sum = lanes_sum(sums.x + sums.y, LANES);
         inv_s = 1.0f / sum;
         ln_s = logf(sum);
@@ -932,6 +942,7 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         const int end = active ? pitch : -1;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
+            if (none(j)) break;
             const int e0 = N * (lane + j * LANES) - odd;
             if (!(MODE & LOSS)) {
 #pragma unroll
