@@ -485,15 +485,15 @@ __device__ __forceinline__ void named_bar_arrive(int id, int count) {
 // them for the slots.  Two rows are on their way into shared memory while one is worked on: a thread
 // copies, and later reads, its own chunks, so no barrier stands between.  It takes its powers against
 // its own maximum and keeps them: one power an element, and a factor a thread,
-// 2^((own max - max) c) g / S, once the row's maximum and sum are known.  Helper warp h does the
-// slots of every H-th row ahead of time, the loss, and the classes' elements behind the others.
+// 2^((own max - max) c) g / S, once the row's maximum and sum are known.  Helper warp h joins the
+// warps' sums of every H-th row, while they take the next row's maximum, and does its slots ahead of
+// time, its loss, and its classes' elements behind the others.
 template <int CT_>
 struct RingCfg {
     static constexpr int CT = CT_, NCH = 8, H = CT == 512 ? 4 : 2;  // helper warps
     static constexpr int THREADS = CT + 32 * H;
     static constexpr int STAGES = 3;
     static constexpr int STAGE_CHUNKS = NCH * CT;
-    static constexpr int SUMS = H + 1;  // a row's sums are not overwritten before row + H's helper ran
     // Blocks an SM, by the powers that a thread keeps: 64 of them leave room for 113 registers.
     static constexpr int blocks(bool kept64) { return kept64 && CT == 128 ? 3 : 512 / CT; }
     static size_t smem(int top) {
@@ -509,19 +509,14 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
     using C = RingCfg<CT>;
     constexpr int E = RowView<T>::E, H = C::H, NCH = C::NCH, WARPS = CT / 32;
     extern __shared__ int4 dynamic[];
-    __shared__ float sum_m[C::SUMS][WARPS], sum_s[C::SUMS][WARPS], factor[H];
+    // the warps' maxima and sums of two rows in turn, and what a helper makes of them
+    __shared__ float sum_m[2][WARPS], sum_s[2][WARPS], row_m[H], row_f[H];
     griddep_launch_dependents();
     griddep_wait();
     const int tid = threadIdx.x, lane = tid & 31;
     const T* z = static_cast<const T*>(p.z);
     const long long step = gridDim.x;
     const int len = MODE & GRAD ? static_cast<int>(p.pitch) : p.classes;
-    // maximum and sum of a row, from its warps'
-    auto joined = [&](int buf, float& m, float& s) {
-        const float wm = lane < WARPS ? sum_m[buf][lane] : -INFINITY;
-        m = lanes_max(wm, 32);
-        s = lanes_sum(lane < WARPS ? shifted(sum_s[buf][lane], wm, m, p.c) : 0.0f, 32);
-    };
     if (tid < CT) {
         int4* ring = dynamic + tid;
         auto view_of = [&](long long row) {  // (its loads stay in the row: no look at the tensor's ends)
@@ -570,21 +565,27 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
         fetch(row, 0);
         fetch(row + step, 1);
         int stage = 0, h = 0, buf = 0;
-        for (; row < p.rows; row += step) {
-            copies_wait<1>();
-            // (the stage that this overwrites was read a row ago, by this thread)
-            fetch(row + 2 * step, stage == 0 ? 2 : stage - 1);
-            T* mine = reinterpret_cast<T*>(ring + stage * C::STAGE_CHUNKS);
-            float e[NCH][E];
+        // largest of this thread's elements of the row in a stage
+        auto largest_of = [&](int st) {
+            const T* from = reinterpret_cast<const T*>(ring + st * C::STAGE_CHUNKS);
             Largest<T, E> largest;
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
                 if ((k & ~1) * CT < most) {
                     Raw<T, E> r;
-                    r.load(mine + k * CT * E);
+                    r.load(from + k * CT * E);
                     largest.add(r);
                 }
-            const float m = largest.get(), at = m == -INFINITY ? 0.0f : m;
+            return largest.get();
+        };
+        copies_wait<1>();
+        float m = largest_of(0);
+        for (; row < p.rows; row += step) {
+            // (the stage that this overwrites was read a row ago, by this thread)
+            fetch(row + 2 * step, stage == 0 ? 2 : stage - 1);
+            T* mine = reinterpret_cast<T*>(ring + stage * C::STAGE_CHUNKS);
+            float e[NCH][E];
+            const float at = m == -INFINITY ? 0.0f : m;
             float2 sums = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
@@ -602,12 +603,13 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
                 sum_m[buf][tid >> 5] = top;
                 sum_s[buf][tid >> 5] = sum;
             }
-            named_bar_sync(1 + h, CT + 32);
+            named_bar_arrive(1 + h, CT + 32);
+            copies_wait<1>();  // (past the last row: nothing is under way, and what is read not used)
+            m = largest_of(stage);
+            named_bar_sync(1 + H + h, CT + 32);
             if (MODE & GRAD) {
-                float all, s;
-                joined(buf, all, s);
-                const float g = factor[h];
-                const float f = ex2_approx_ftz((at - all) * p.c) * (g * (1.0f / s));
+                const float g = row_f[h];
+                const float f = ex2_approx_ftz((at - row_m[h]) * p.c) * g;
                 const RowView<T> view = view_of(row);
                 T* out = static_cast<T*>(p.dz) + row * p.pitch;
                 T* place = out - view.head + tid * E;
@@ -648,10 +650,10 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
 #pragma unroll 1
                     for (int i = tid + n * CT; i < chunks; i += CT) part(i);
                 }
-                named_bar_arrive(1 + H + h, CT + 32);
+                named_bar_arrive(1 + 2 * H + h, CT + 32);
             }
             h = h == H - 1 ? 0 : h + 1;
-            buf = buf == C::SUMS - 1 ? 0 : buf + 1;
+            buf ^= 1;
         }
         return;
     }
@@ -663,7 +665,7 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
     s.p = reinterpret_cast<float*>(s.id + s.top4);
     s.z = s.p + s.top4;
     float* share = s.z + s.top4;
-    int buf = h;
+    int buf = h & 1;
     // A lane's first slot and the row's weight are loaded a turn ahead, the student's logit behind
     // the loss (a row's logits are overwritten only after its helper has come to its sums).
     long long row = blockIdx.x + h * step, raw = -1;
@@ -706,10 +708,17 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
         for (int k = lane; k < s.top; k += 32)
             share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
         const float g = some ? g_row * p.scale : 0.0f;
-        if (lane == 0) factor[h] = g;
         named_bar_sync(1 + h, CT + 32);
-        float m, sum, loss = 0.0f;
-        joined(buf, m, sum);
+        const float wm = lane < WARPS ? sum_m[buf][lane] : -INFINITY, m = lanes_max(wm, 32);
+        const float sum = lanes_sum(lane < WARPS ? shifted(sum_s[buf][lane], wm, m, p.c) : 0.0f, 32);
+        const float inv_s = 1.0f / sum;
+        if (lane == 0) {
+            row_m[h] = m;
+            row_f[h] = g == 0.0f ? 0.0f : g * inv_s;
+        }
+        __syncwarp();
+        named_bar_arrive(1 + H + h, CT + 32);
+        float loss = 0.0f;
         const float ln_s = logf(sum);
         for (int k = lane; k < s.top; k += 32)
             if (share[k] > 0.0f || share[k] != share[k])
@@ -721,17 +730,15 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
         }
         gather(row + H * step);
         if (MODE & GRAD) {
-            named_bar_sync(1 + H + h, CT + 32);
+            named_bar_sync(1 + 2 * H + h, CT + 32);
             T* out = static_cast<T*>(p.dz) + row * p.pitch;
-            const float inv_s = 1.0f / sum;
             for (int k = lane; k < s.top && g != 0.0f; k += 32)
                 if (s.id[k] >= 0 && share[k] != -1.0f)
                     put(out + s.id[k],
                         g * (ex2_approx_ftz((s.z[k] - m) * p.c) * inv_s - share[k]));
         }
         __syncwarp();
-        buf += H;
-        if (buf >= C::SUMS) buf -= C::SUMS;
+        if (H & 1) buf ^= 1;
     }
 }
 
@@ -882,13 +889,10 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
     const int odd = N == 2 ? (view.head + tr * pitch) & 1 : 0;
     T* words = mine - odd;
     const int classes = active ? p.classes : 0;
-    // (words are passed over by twos where no row reaches)
-    auto none = [&](int j) { return (j & ~1) * LANES * N > pitch; };
     float v[W][N];
     Largest<T, N> largest;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-        if (none(j)) break;
         const int e0 = N * (lane + j * LANES) - odd;  // element of the word's first
         Raw<T, N> r;
         r.w[0] = N == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
@@ -905,8 +909,7 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         float2 sums = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            if (none(j)) break;
-            powers(v[j], at, p.c, sums);
+                powers(v[j], at, p.c, sums);
         }
         const float sum = lanes_sum(sums.x + sums.y, LANES);
         inv_s = 1.0f / sum;
@@ -942,8 +945,7 @@ __global__ void __launch_bounds__(TILE_THREADS) distill_tile_kernel(const Distil
         const int end = active ? pitch : -1;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            if (none(j)) break;
-            const int e0 = N * (lane + j * LANES) - odd;
+                const int e0 = N * (lane + j * LANES) - odd;
             if (!(MODE & LOSS)) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) v[j][i] = q_of(v[j][i]);
@@ -993,12 +995,21 @@ cudaError_t launch_distill_tile(const DistillParams& p, cudaStream_t stream) {
                       tile_bytes(p, sizeof(T), LANES), stream, p);
 }
 
+// The least multiple of four words a lane that holds a row (100,000 rows of 300 bf16 with 32 slots, ten
+// words of 16: 69 us with 16, 55 with 12).
+template <typename T, int MODE, int LANES>
+cudaError_t launch_distill_lanes(const DistillParams& p, int words, cudaStream_t stream) {
+    return words <= 8    ? launch_distill_tile<T, MODE, LANES, 8, 4>(p, stream)
+           : words <= 12 ? launch_distill_tile<T, MODE, LANES, 12, 4>(p, stream)
+                         : launch_distill_tile<T, MODE, LANES, 16, 4>(p, stream);
+}
+
 template <typename T, int MODE>
 cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_t stream) {
     constexpr int size = static_cast<int>(sizeof(T));
     constexpr size_t SMEM = 48 << 10;
-    // a row's words, with one that it may share: 16 and four slots a lane, up to 32 and eight of a
-    // whole warp
+    // a row's words, with one that it may share: up to 16 and four slots a lane, up to 32 and eight
+    // of a whole warp
     const bool even = (static_cast<uintptr_t>(p.pitch * size) | reinterpret_cast<uintptr_t>(p.z)) % 4 == 0;
     const long long words = p.pitch * size / 4 + (even ? 0 : 1);
     if (words <= 32 * 32) {
@@ -1006,14 +1017,16 @@ cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_
         while (lanes < 32 && (16 * lanes < words || 4 * lanes < p.top ||
                               tile_bytes(p, size, lanes) > SMEM))
             lanes *= 2;
-        if (tile_bytes(p, size, lanes) <= SMEM) switch (lanes) {
-            case 4: return launch_distill_tile<T, MODE, 4, 16, 4>(p, stream);
-            case 8: return launch_distill_tile<T, MODE, 8, 16, 4>(p, stream);
-            case 16: return launch_distill_tile<T, MODE, 16, 16, 4>(p, stream);
-            default:
-                return words <= 32 * 16 && p.top <= 32 * 4
-                           ? launch_distill_tile<T, MODE, 32, 16, 4>(p, stream)
-                           : launch_distill_tile<T, MODE, 32, 32, 8>(p, stream);
+        if (tile_bytes(p, size, lanes) <= SMEM) {
+            const int each = static_cast<int>((words + lanes - 1) / lanes);  // words a lane
+            if (each > 16 || p.top > 4 * lanes)
+                return launch_distill_tile<T, MODE, 32, 32, 8>(p, stream);
+            switch (lanes) {
+                case 4: return launch_distill_lanes<T, MODE, 4>(p, each, stream);
+                case 8: return launch_distill_lanes<T, MODE, 8>(p, each, stream);
+                case 16: return launch_distill_lanes<T, MODE, 16>(p, each, stream);
+                default: return launch_distill_lanes<T, MODE, 32>(p, each, stream);
+            }
         }
     }
     // blocks of a row: as many as its chunks need to stay in registers, more while there are

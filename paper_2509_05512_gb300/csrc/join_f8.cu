@@ -26,7 +26,6 @@ struct JoinF8Cfg {
     static constexpr int RED = WHOLE ? LANES : TPS;
     static constexpr int THREADS = LANES > 256 ? LANES : 256;
     static constexpr int SLOTS = THREADS / LANES;
-    static constexpr int WPS = RED / 32;  // warps of a statistic past 32 lanes
 };
 
 // Sums over the RED lanes of a statistic, as group_sum orders them.
@@ -39,6 +38,7 @@ __device__ __forceinline__ void statistic(float (&v)[R], float (*both)[R][32], i
 #pragma unroll
         for (int i = 0; i < R; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     if constexpr (C::RED > 32) {
+        constexpr int WPS = C::RED / 32;  // warps of a statistic
         float(*sm)[32] = both[turn];
         turn ^= 1;
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -47,11 +47,11 @@ __device__ __forceinline__ void statistic(float (&v)[R], float (*both)[R][32], i
             for (int i = 0; i < R; ++i) sm[i][warp] = v[i];
         }
         __syncthreads();
-        const int at = (warp & ~(C::WPS - 1)) + (lane & (C::WPS - 1));
+        const int at = (warp & ~(WPS - 1)) + (lane & (WPS - 1));
 #pragma unroll
         for (int i = 0; i < R; ++i) v[i] = sm[i][at];
 #pragma unroll
-        for (int o = C::WPS / 2; o > 0; o >>= 1)
+        for (int o = WPS / 2; o > 0; o >>= 1)
 #pragma unroll
             for (int i = 0; i < R; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     }
