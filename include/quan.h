@@ -624,7 +624,8 @@ quan_status_t quan_qpoint_w4_fwd(const void* x, const void* wq, const void* wsca
  * A slot whose class is outside [0, classes) or whose t is -infinity is empty; a row of empty slots
  * has loss 0 and gradient 0, and a row with g = 0 gradient 0, whatever their logits are.  A class may
  * stand in several slots.  A logit of -infinity is a class that cannot be (q = 0; a slot with p > 0 of
- * it makes the loss infinite).  +infinity, NaN, or no finite logit in a row that counts give NaN.
+ * it makes the loss infinite).  +infinity, NaN, or no finite logit in a row that counts give NaN (a
+ * teacher's in the loss and the slots' classes).  z / T and t / T have to stay within fp32.
  * Arithmetic is fp32; the gradient is rounded once.  Repeated calls give the same bits.
  *   z, dz     [rows][pitch] of dtype (quan_dtype_t), the row's first `classes` elements its logits;
  *             dz's others become 0.  dz may be z itself (in place), no other overlap

@@ -11,6 +11,14 @@
 //
 // Everything is fp32; a gradient is rounded once.  A slot's class may come twice: the first of its slots
 // adds the others' p in their order, so that no sum depends on which thread comes first.
+//
+// A row is read once and its gradient written once, with what a row needs in between on the chip: rows
+// of up to 4 KB as tiles of many rows (distill_tile_kernel), longer ones whole in a ring of shared
+// memory (distill_ring_kernel), single ones, those of more than 64 KB and the gradient alone by blocks
+// that keep their part in registers (distill_row_kernel).  Bound: HBM for long rows; for short ones the
+// instructions of their slots and reductions.  Loss and gradient, device time: 4096 x 32768 bf16 90 us,
+// 6.0 TB/s (149 by a block a row that reads it twice); 100,352 x 100 bf16, ten slots, 17.6 us, 2.9 TB/s
+// (403); gradient of 333 x 10007 bf16 6.5 us; loss of one row of 65,536 fp32 4.1 us.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -155,38 +163,56 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
 }
 
 // A row's slots, `top4` (top rounded up to 4) each: the class or -1, the teacher's logit and then p,
-// the student's logit of the class.
+// ln p, the student's logit of the class, and what all slots of the class put on it, -1 but in the
+// first of them.
+constexpr int SLOT_BYTES = 20;
 struct Slots {
     int* id;
-    float *p, *z;
+    float *p, *lnp, *z, *share;
     int top, top4;
+    __device__ __forceinline__ Slots(void* at, int slots) {
+        top = slots;
+        top4 = (slots + 3) & ~3;
+        id = static_cast<int*>(at);
+        p = reinterpret_cast<float*>(id + top4);
+        lnp = p + top4;
+        z = lnp + top4;
+        share = z + top4;
+    }
 };
 
-// The teacher's side of a row by `lanes` lanes of a warp: p of each slot, and the sum of p ln p.
-__device__ __forceinline__ float teacher_side(const Slots& s, const DistillParams& p, int lane,
-                                              int lanes, bool& some) {
-    float m = -INFINITY, sum = 0.0f, h = 0.0f;
+// The teacher's side of a row by a warp: p and ln p of each slot; whether there is one.
+__device__ __forceinline__ bool teacher_side(const Slots& s, const DistillParams& p, int lane) {
+    float m = -INFINITY, sum = 0.0f;
     bool any = false;
-    for (int k = lane; k < s.top; k += lanes)
+    for (int k = lane; k < s.top; k += 32)
         if (s.id[k] >= 0) {
             m = fmaxf(m, s.p[k]);
             any = true;
         }
-    m = lanes_max(m, lanes);
-    const unsigned votes = __ballot_sync(0xffffffffu, any);
-    some = ((votes >> ((threadIdx.x & 31) - lane)) & (0xffffffffu >> (32 - lanes))) != 0;
-    for (int k = lane; k < s.top; k += lanes)
+    m = lanes_max(m, 32);
+    for (int k = lane; k < s.top; k += 32)
         if (s.id[k] >= 0) sum += ex2_approx_ftz((s.p[k] - m) * p.c);
-    sum = lanes_sum(sum, lanes);
+    sum = lanes_sum(sum, 32);
     const float ln_sum = logf(sum), inv = 1.0f / sum;
-    for (int k = lane; k < s.top; k += lanes)
+    for (int k = lane; k < s.top; k += 32)
         if (s.id[k] >= 0) {
-            const float x = s.p[k] - m, pk = ex2_approx_ftz(x * p.c) * inv;
-            s.p[k] = pk;
-            // (a slot whose share has vanished has no part, be its class impossible)
-            if (!(pk == 0.0f)) h = fmaf(pk, fmaf(x, p.inv_t, -ln_sum), h);
+            const float x = s.p[k] - m;
+            s.p[k] = ex2_approx_ftz(x * p.c) * inv;
+            s.lnp[k] = fmaf(x, p.inv_t, -ln_sum);
         }
-    return lanes_sum(h, lanes);
+    return __any_sync(0xffffffffu, any);
+}
+
+// A row's loss over T^2 by a warp: slot by slot, so that a student near its teacher loses nothing to
+// sums that cancel.  (A slot whose share has vanished has no part, be its class impossible.)
+__device__ __forceinline__ float slots_loss(const Slots& s, const DistillParams& p, int lane, float m,
+                                            float ln_s) {
+    float loss = 0.0f;
+    for (int k = lane; k < s.top; k += 32)
+        if (s.id[k] >= 0 && !(s.p[k] == 0.0f))
+            loss = fmaf(s.p[k], s.lnp[k] - ((s.z[k] - m) * p.inv_t - ln_s), loss);
+    return lanes_sum(loss, 32);
 }
 
 // What all slots of slot k's class put on it, or -1 where an earlier slot has that class.
@@ -290,14 +316,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const Disti
     constexpr int E = RowView<T>::E;
     extern __shared__ int4 dynamic[];
     __shared__ float warp_m[ROW_WARPS], warp_s[ROW_WARPS], part_m[ROW_CLUSTER], part_s[ROW_CLUSTER];
-    __shared__ float entropy, counts;
-    Slots s;
-    s.top = p.top;
-    s.top4 = (p.top + 3) & ~3;
-    s.id = reinterpret_cast<int*>(dynamic);
-    s.p = reinterpret_cast<float*>(s.id + s.top4);
-    s.z = s.p + s.top4;
-    float* share = s.z + s.top4;
+    __shared__ int counts;
+    const Slots s(dynamic, p.top);
     griddep_launch_dependents();
     griddep_wait();
     const long long row = blockIdx.x / static_cast<unsigned>(parts);
@@ -339,12 +359,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const Disti
             if (id >= 0 && (((MODE & LOSS) && part == 0) || here(id))) s.z[k] = element(zrow + id);
         }
         __syncwarp();
-        bool some;
-        const float h = teacher_side(s, p, lane, 32, some);
-        if (lane == 0) {
-            entropy = h;
-            counts = some ? 1.0f : 0.0f;
-        }
+        const bool some = teacher_side(s, p, lane);
+        if (lane == 0) counts = some;
     }
     float m = -INFINITY, sum = 0.0f;
     if (MODE & LOSS) {
@@ -385,10 +401,10 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const Disti
         }
     }
     __syncthreads();
-    const bool some = counts > 0.0f;
-    // the shares of classes, for the loss and the gradient (their slots' first ones')
-    for (int k = tid; k < s.top; k += blockDim.x)
-        share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
+    const bool some = counts != 0;
+    if (MODE & GRAD)
+        for (int k = tid; k < s.top; k += blockDim.x)
+            s.share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
     float inv_s = 1.0f, lse = 0.0f;
     if (MODE & LOSS) {
         const float wm = lane < warps ? warp_m[lane] : -INFINITY;
@@ -408,18 +424,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const Disti
         inv_s = 1.0f / sum;
         const float ln_s = logf(sum);
         lse = fmaf(m, p.inv_t, ln_s);
-        if (part == 0) {
-            __syncthreads();  // (share)
-            if (tid < 32) {
-                float loss = 0.0f;
-                for (int k = lane; k < s.top; k += 32)
-                    if (share[k] > 0.0f || share[k] != share[k])
-                        loss = fmaf(-share[k], (s.z[k] - m) * p.inv_t - ln_s, loss);
-                loss = lanes_sum(loss, 32) + entropy;
-                if (lane == 0) {
-                    p.loss[row] = some ? p.t2 * loss : 0.0f;
-                    if (p.lse) p.lse[row] = lse;
-                }
+        if (part == 0 && tid < 32) {
+            const float loss = slots_loss(s, p, lane, m, ln_s);
+            if (lane == 0) {
+                p.loss[row] = some ? p.t2 * loss : 0.0f;
+                if (p.lse) p.lse[row] = lse;
             }
         }
     } else {
@@ -469,8 +478,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const Disti
         __syncthreads();  // the slots' classes, over what was just written
         for (int k = tid; k < s.top && g != 0.0f; k += blockDim.x) {
             const int id = s.id[k];
-            if (id >= 0 && share[k] != -1.0f && here(id))
-                put(out + id, g * (q_of(s.z[k]) - share[k]));
+            if (id >= 0 && s.share[k] != -1.0f && here(id))
+                put(out + id, g * (q_of(s.z[k]) - s.share[k]));
         }
     }
 }
@@ -488,6 +497,11 @@ __device__ __forceinline__ void named_bar_arrive(int id, int count) {
 // 2^((own max - max) c) g / S, once the row's maximum and sum are known.  Helper warp h joins the
 // warps' sums of every H-th row, while they take the next row's maximum, and does its slots ahead of
 // time, its loss, and its classes' elements behind the others.
+//
+// 4096 x 32768 bf16, loss and gradient: 89.7 us, 89% of the bytes' floor (101 where the threads wait
+// for the joined sums with nothing else to do, 156 with two powers an element and bounds at every
+// chunk).  Rows that fill fewer threads take blocks of 256 or 128, two to four an SM; of those one
+// helper a block was the slower side (20,000 x 3000, loss: 90 us; 47 with two).
 template <int CT_>
 struct RingCfg {
     static constexpr int CT = CT_, NCH = 8, H = CT == 512 ? 4 : 2;  // helper warps
@@ -497,7 +511,7 @@ struct RingCfg {
     // Blocks an SM, by the powers that a thread keeps: 64 of them leave room for 113 registers.
     static constexpr int blocks(bool kept64) { return kept64 && CT == 128 ? 3 : 512 / CT; }
     static size_t smem(int top) {
-        return size_t(16) * STAGES * STAGE_CHUNKS + size_t(16) * H * ((top + 3) & ~3);
+        return size_t(16) * STAGES * STAGE_CHUNKS + size_t(SLOT_BYTES) * H * ((top + 3) & ~3);
     }
 };
 
@@ -658,14 +672,9 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
         return;
     }
     const int h = (tid - CT) >> 5;
-    Slots s;
-    s.top = p.top;
-    s.top4 = (p.top + 3) & ~3;
-    s.id = reinterpret_cast<int*>(dynamic + C::STAGES * C::STAGE_CHUNKS) + h * s.top4 * 4;
-    s.p = reinterpret_cast<float*>(s.id + s.top4);
-    s.z = s.p + s.top4;
-    float* share = s.z + s.top4;
-    int buf = h & 1;
+    const Slots s(reinterpret_cast<char*>(dynamic + C::STAGES * C::STAGE_CHUNKS) +
+                      h * ((p.top + 3) & ~3) * SLOT_BYTES, p.top);
+    const int buf = h & 1;
     // A lane's first slot and the row's weight are loaded a turn ahead, the student's logit behind
     // the loss (a row's logits are overwritten only after its helper has come to its sums).
     long long row = blockIdx.x + h * step, raw = -1;
@@ -702,11 +711,12 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             if (id >= 0) s.z[k] = element(zrow + id);
         }
         __syncwarp();
-        bool some;
-        const float entropy = teacher_side(s, p, lane, 32, some);
-        __syncwarp();
-        for (int k = lane; k < s.top; k += 32)
-            share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
+        const bool some = teacher_side(s, p, lane);
+        if (MODE & GRAD) {
+            __syncwarp();
+            for (int k = lane; k < s.top; k += 32)
+                s.share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
+        }
         const float g = some ? g_row * p.scale : 0.0f;
         named_bar_sync(1 + h, CT + 32);
         const float wm = lane < WARPS ? sum_m[buf][lane] : -INFINITY, m = lanes_max(wm, 32);
@@ -718,12 +728,7 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
         }
         __syncwarp();
         named_bar_arrive(1 + H + h, CT + 32);
-        float loss = 0.0f;
-        const float ln_s = logf(sum);
-        for (int k = lane; k < s.top; k += 32)
-            if (share[k] > 0.0f || share[k] != share[k])
-                loss = fmaf(-share[k], (s.z[k] - m) * p.inv_t - ln_s, loss);
-        loss = lanes_sum(loss, 32) + entropy;
+        const float ln_s = logf(sum), loss = slots_loss(s, p, lane, m, ln_s);
         if (lane == 0) {
             p.loss[row] = some ? p.t2 * loss : 0.0f;
             if (p.lse) p.lse[row] = fmaf(m, p.inv_t, ln_s);
@@ -733,12 +738,12 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             named_bar_sync(1 + 2 * H + h, CT + 32);
             T* out = static_cast<T*>(p.dz) + row * p.pitch;
             for (int k = lane; k < s.top && g != 0.0f; k += 32)
-                if (s.id[k] >= 0 && share[k] != -1.0f)
+                if (s.id[k] >= 0 && s.share[k] != -1.0f)
                     put(out + s.id[k],
-                        g * (ex2_approx_ftz((s.z[k] - m) * p.c) * inv_s - share[k]));
+                        g * (ex2_approx_ftz((s.z[k] - m) * p.c) * inv_s - s.share[k]));
         }
         __syncwarp();
-        if (H & 1) buf ^= 1;
+        static_assert(H % 2 == 0, "a helper's rows have one buffer of sums");
     }
 }
 
@@ -777,13 +782,14 @@ constexpr int TILE_THREADS = 256;
 // gain from a block more than they would get (60,000 rows of 1000: 80 us without, 74 with four); for
 // the others it is left to choose (0).
 constexpr int tile_blocks(int size, int mode, int words) {
-    return size == 2 && mode == (LOSS | GRAD) && words <= 16 ? (words <= 12 ? 5 : 4) : 0;
+    return size == 2 && mode == (LOSS | GRAD) && words <= 16 ? (words <= 8 ? 5 : 4) : 0;
 }
 
 // A tile of 256 / LANES rows a block.  The rows lie one after the other, so the tile is read and
 // written in whole chunks wherever its rows begin; in shared memory a row is LANES lanes of a warp, at
 // most W of its 4-byte words and K of its slots each, whose powers stay in registers, and the gradient
-// takes the logits' place.  A class that several slots have shows by a byte a class: each slot writes
+// takes the logits' place: 100,352 x 100 bf16 with ten slots 17.6 us, bound by its instructions (31 with
+// the slots in shared memory and each compared with every other).  A class that several slots have shows by a byte a class: each slot writes
 // its number there and looks whether it still stands.
 template <typename T, int MODE, int LANES, int W, int K>
 __global__ void __launch_bounds__(TILE_THREADS, tile_blocks(sizeof(T), MODE, W))
@@ -844,24 +850,20 @@ __global__ void __launch_bounds__(TILE_THREADS, tile_blocks(sizeof(T), MODE, W))
     const unsigned votes = __ballot_sync(0xffffffffu, any);
     const unsigned of_row = (0xffffffffu >> (32 - LANES)) << ((tid & 31) - lane);
     const bool some = (votes & of_row) != 0;
-    float ts = 0.0f, h = 0.0f;
+    float ts = 0.0f, lnp[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const float x = t[k] - tm;
-        t[k] = id[k] >= 0 ? ex2_approx_ftz(x * p.c) : 0.0f;
+        lnp[k] = t[k] - tm;
+        t[k] = id[k] >= 0 ? ex2_approx_ftz(lnp[k] * p.c) : 0.0f;
         ts += t[k];
-        // (a slot whose share has vanished has no part)
-        if (t[k] > 0.0f || t[k] != t[k]) h = fmaf(t[k], x, h);
     }
     ts = lanes_sum(ts, LANES);
-    h = lanes_sum(h, LANES);
-    const float inv_ts = 1.0f / ts;
-    float loss = 0.0f;
-    const float entropy = fmaf(h * inv_ts, p.inv_t, -logf(ts));
-    // the share of each class, -1 in all its slots but the first
+    const float inv_ts = 1.0f / ts, ln_ts = logf(ts);
+    // the share of each class, in the first of its slots
     bool lost = false;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
+        lnp[k] = fmaf(lnp[k], p.inv_t, -ln_ts);
         t[k] *= inv_ts;
         if (id[k] >= 0) owner[id[k]] = static_cast<uint8_t>(lane + k * LANES);
     }
@@ -870,25 +872,34 @@ __global__ void __launch_bounds__(TILE_THREADS, tile_blocks(sizeof(T), MODE, W))
     for (int k = 0; k < K; ++k)
         if (id[k] >= 0) lost = lost || owner[id[k]] != lane + k * LANES;
     if (__any_sync(0xffffffffu, lost)) {
-        float share[K];
+        // (the first slot stands for all of its class, their p ln p included)
+        float share[K], sum[K];
         bool first[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) share[k] = 0.0f, first[k] = true;
+        for (int k = 0; k < K; ++k) share[k] = sum[k] = 0.0f, first[k] = true;
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll 1
             for (int l = 0; l < LANES; ++l) {
-                const int other = __shfl_sync(0xffffffffu, id[j], (tid & 31) - lane + l);
-                const float part = __shfl_sync(0xffffffffu, t[j], (tid & 31) - lane + l);
+                const int from = (tid & 31) - lane + l;
+                const int other = __shfl_sync(0xffffffffu, id[j], from);
+                const float part = __shfl_sync(0xffffffffu, t[j], from);
+                const float ln = __shfl_sync(0xffffffffu, lnp[j], from);
 #pragma unroll
                 for (int k = 0; k < K; ++k)
-                    if (other == id[k]) {
+                    if (other == id[k] && other >= 0) {
                         share[k] += part;
+                        if (!(part == 0.0f)) sum[k] = fmaf(part, ln, sum[k]);
                         if (l + j * LANES < lane + k * LANES) first[k] = false;
                     }
             }
 #pragma unroll
-        for (int k = 0; k < K; ++k) t[k] = first[k] ? share[k] : -1.0f;
+        for (int k = 0; k < K; ++k)
+            if (id[k] >= 0) {
+                if (share[k] != t[k]) lnp[k] = sum[k] / share[k];
+                t[k] = share[k];
+                if (!first[k]) id[k] = -1;
+            }
     }
     copies_wait<0>();
     __syncthreads();
@@ -929,18 +940,17 @@ __global__ void __launch_bounds__(TILE_THREADS, tile_blocks(sizeof(T), MODE, W))
         return MODE & LOSS ? ex2_approx_ftz((x - m) * p.c) * inv_s
                            : ex2_approx_ftz(fmaf(x, p.inv_t, -lse) * LOG2E);
     };
+    float loss = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        if (t[k] == -1.0f) id[k] = -1;
         if (id[k] < 0) continue;
-        const float z = element(mine + id[k]), share = t[k];
-        if (MODE & LOSS)
-            if (share > 0.0f || share != share)
-                loss = fmaf(-share, (z - m) * p.inv_t - ln_s, loss);
-        if (MODE & GRAD) t[k] = g * (q_of(z) - share);  // the gradient there
+        const float z = element(mine + id[k]);
+        if (MODE & LOSS)  // (slot by slot, as slots_loss)
+            if (!(t[k] == 0.0f)) loss = fmaf(t[k], lnp[k] - ((z - m) * p.inv_t - ln_s), loss);
+        if (MODE & GRAD) t[k] = g * (q_of(z) - t[k]);  // the gradient there
     }
     if (MODE & LOSS) {
-        loss = lanes_sum(loss, LANES) + entropy;
+        loss = lanes_sum(loss, LANES);
         if (active && lane == 0) {
             p.loss[row] = some ? p.t2 * loss : 0.0f;
             if (p.lse) p.lse[row] = lse;
@@ -1027,8 +1037,8 @@ cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_
             lanes *= 2;
         if (tile_bytes(p, size, lanes) <= SMEM) {
             const int each = static_cast<int>((words + lanes - 1) / lanes);  // words a lane
-            if (each > 16 || p.top > 4 * lanes)
-                return launch_distill_tile<T, MODE, 32, 32, 8>(p, stream);
+            if (p.top > 4 * lanes) return launch_distill_tile<T, MODE, 32, 32, 8>(p, stream);
+            if (each > 16) return launch_distill_tile<T, MODE, 32, 32, 4>(p, stream);
             switch (lanes) {
                 case 4: return launch_distill_lanes<T, MODE, 4>(p, each, stream);
                 case 8: return launch_distill_lanes<T, MODE, 8>(p, each, stream);
@@ -1055,7 +1065,7 @@ cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_
     const bool wide = per > 4 * ROW_THREADS;
     int threads = (per + (wide ? 8 : 4) - 1) / (wide ? 8 : 4);
     threads = threads < 128 ? 128 : threads > ROW_THREADS ? ROW_THREADS : (threads + 31) & ~31;
-    const size_t smem = static_cast<size_t>((p.top + 3) & ~3) * 16;
+    const size_t smem = static_cast<size_t>((p.top + 3) & ~3) * SLOT_BYTES;
     const dim3 g(static_cast<unsigned>(p.rows * parts)), b(static_cast<unsigned>(threads));
     const unsigned cluster = MODE & LOSS ? static_cast<unsigned>(parts) : 1u;
     return wide ? launch_pdl_cluster(distill_row_kernel<T, MODE, 8>, g, b, cluster, smem, stream, p,

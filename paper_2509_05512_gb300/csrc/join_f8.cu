@@ -6,6 +6,10 @@
 // taken in residual_join's order: the same bits.  With one for the row (WHOLE) it has 16, which halves
 // the exchange between lanes.  R rows a thread are under way together, the next R loaded ahead.
 // Everything elementwise goes by twos (f32x2), rounded as one by one.
+//
+// Bound by HBM beside the instructions of reductions and conversions.  32 x 56 x 56 x 256 bf16, a
+// statistic a component: 33 us, 5.4 TB/s (39 by residual.cu's form).  The norm of 25,600 rows of 4096,
+// a statistic a row: 58 us, 5.4 TB/s (138; 103 with eight channels a lane and 64-bit indexes).
 #include <cuda_bf16.h>
 
 #include <atomic>

@@ -403,7 +403,8 @@ cudaError_t launch_f8_rows(F8Rows r, cudaStream_t stream) {
 
 // Rows read back: a thread takes eight channels of a component of F8_DEQUANT_UNROLL rows, as above, all
 // loads first.  The last rows go first: their writer has just left them in L2.  Bound by HBM: 1 byte
-// read, 2 written a channel.
+// read, 2 written a channel.  25,600 rows of 4096: 48 us, 6.5 TB/s (60 with 16 channels a thread, from
+// the first rows on); 100,352 of 256: 14 us, 5.5 TB/s.
 struct F8Dequant {
     const uint8_t* q;    // [rows][4][Kp]
     const float* scale;  // [4][kblk][pitch]
@@ -458,7 +459,8 @@ __global__ void __launch_bounds__(256) f8_dequant_kernel(const F8Dequant p) {
 }
 
 // The same of components that are not whole chunks of eight: eight elements of the output a thread,
-// wherever rows and components begin, eight rows a block (a multiple of eight elements).
+// wherever rows and components begin, eight rows a block (a multiple of eight elements).  4805 rows
+// of 340: 5.0 us (13 by single elements).
 __global__ void __launch_bounds__(256) f8_dequant_any_kernel(const F8Dequant p) {
     griddep_launch_dependents();
     griddep_wait();

@@ -14,6 +14,11 @@
 // holding component co xor L of pixel m with Eq. 6's sign.  So an element of a letter is read and
 // widened once for all four components, and the quaternion product needs no other arithmetic.
 //
+// Device time: one pixel 512 -> 1024 1.7 us, 8192 -> 8192 7.0 us (8.9 MB of letters and scales: 1.3 us at
+// HBM's rate, which two rounds of loads, the join of the warps and a cluster's two barriers follow: with
+// the inputs over four blocks instead of two 11.2 us); 49 pixels 2048 -> 2048 8.5 us, 13 pixels
+// 1172 -> 2804 6.3 us.
+//
 // Layout of the letters: [L][16 output channels][64 input channels] blocks of 512 bytes, a lane's 16
 // bytes side by side: word s of lane 4 g + t has q + 8 of channels g and g + 8, inputs
 // k = 32 (s / 2) + 8 t + 4 (s mod 2) + 0 .. 3, so that a lane's inputs of a block are two runs of eight.

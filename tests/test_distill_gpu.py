@@ -389,3 +389,19 @@ def test_many_rows(rows, V, pad, top, dtype):
         assert not got[:, V:].any()
         tol = T * d["g"].double()[:, None] * (q + share) * (R + 8 * U * (x + 60.0))[:, None]
         assert ((got[:, :V].double() - dz).abs() <= tol + HALF[dtype] * dz.abs() + 1e-30).all()
+
+
+@pytest.mark.parametrize("rows, V", [(50, 8), (50, 64), (20, 256), (4000, 100)])
+@pytest.mark.parametrize("T", [1.0, 4.0])
+def test_a_student_like_its_teacher(rows, V, T):
+    # every class a slot, with the student's own logit: the loss is 0 and the gradient too.  Both sums
+    # have the same terms, at most (V / 4 + 8) roundings apart; ln p and ln q differ by four roundings
+    # of at most |x| + ln V, |x| < 20
+    z = torch.randn(rows, V, device="cuda") * 2
+    index = torch.argsort(torch.rand(rows, V, device="cuda"), dim=1)
+    t = z.gather(1, index)
+    loss, dz = quan.distill_loss_and_gradient(z, index, t, temperature=T)
+    tol = 2 * (V / 4 + 8) * U + 4 * U * (20 / T + np.log(V))
+    assert loss.abs().max() <= T * T * tol and dz.abs().max() <= T * 2 * tol
+    l2, lse = quan.distill_loss(z, index, t, temperature=T)
+    assert l2.abs().max() <= T * T * tol
