@@ -18,7 +18,7 @@
 // that keep their part in registers (distill_row_kernel).  Bound: HBM for long rows; for short ones the
 // instructions of their slots and reductions.  Loss and gradient, device time: 4096 x 32768 bf16 90 us,
 // 6.0 TB/s (149 by a block a row that reads it twice); 100,352 x 100 bf16, ten slots, 17.6 us, 2.9 TB/s
-// (403); gradient of 333 x 10007 bf16 6.5 us; loss of one row of 65,536 fp32 4.1 us.
+// (403); gradient of 333 x 10007 fp32 6.5 us; loss of one row of 65,536 fp32 4.1 us.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -623,7 +623,8 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             named_bar_sync(1 + H + h, CT + 32);
             if (MODE & GRAD) {
                 const float g = row_f[h];
-                const float f = ex2_approx_ftz((at - row_m[h]) * p.c) * g;
+                // (a thread with no finite logit has at = 0, which may be far above the row's maximum)
+                const float f = ex2_approx_ftz(fminf((at - row_m[h]) * p.c, 0.0f)) * g;
                 const RowView<T> view = view_of(row);
                 T* out = static_cast<T*>(p.dz) + row * p.pitch;
                 T* place = out - view.head + tid * E;

@@ -405,3 +405,39 @@ def test_a_student_like_its_teacher(rows, V, T):
     assert loss.abs().max() <= T * T * tol and dz.abs().max() <= T * 2 * tol
     l2, lse = quan.distill_loss(z, index, t, temperature=T)
     assert l2.abs().max() <= T * T * tol
+
+
+@pytest.mark.parametrize("V", [90, 2000, 5000, 12000, 32000, 70001])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masked_classes_of_rows_far_below_zero(V, dtype):
+    # all but 64 classes masked, so that most threads see no finite logit, and a largest logit whose
+    # distance from 0 no fp32 power spans; with a row of one class, and one that has none
+    rows, top, keep = 320, 6, 64
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.full((rows, V), -float("inf"), device="cuda")
+    z[:, :keep] = 3.0 * torch.randn(rows, keep, generator=g, device="cuda") - 400.0
+    z[5, 1:] = -float("inf")
+    z[6] = -float("inf")
+    z = z.to(DT[dtype])
+    index = torch.randint(0, keep, (rows, top), generator=g, device="cuda")
+    index[5], index[6] = 0, -1
+    d = dict(z=z, index=index, teacher=torch.randn(rows, top, generator=g, device="cuda"), V=V,
+             g=torch.rand(rows, generator=g, device="cuda") + 0.5)
+    loss, lse, dz, q, share = reference(d, 1.0)
+    loss[6], lse[6], dz[6], q[6] = 0.0, -float("inf"), 0.0, 0.0
+    l1, e1 = quan.distill_loss(z, index, d["teacher"])
+    g1 = quan.distill_loss_backward(d["g"], z, e1, index, d["teacher"])
+    l2, g2 = quan.distill_loss_and_gradient(z, index, d["teacher"], d["g"])
+    # (as above: roundings of logits and sums of up to 400 + 30)
+    R = 5e-6 + (V / 128 + 32) * U + 16 * U * 860.0
+    # (relative to its magnitude: a row whose slots all have its one possible class, as row 5, has
+    # ln q = 0 and the loss sum p ln p, at least -ln 6)
+    for got in (l1, l2):
+        assert ((got.double() - loss).abs() <= 2 * R * (1 + loss.abs())).all()
+    assert e1[6] == -float("inf")
+    others = torch.arange(rows, device="cuda") != 6
+    assert ((e1.double() - lse).abs()[others] <= R).all()
+    for got in (g1, g2):
+        tol = d["g"].double()[:, None] * (q + share) * R + HALF[dtype] * dz.abs() + 1e-30
+        assert ((got.double() - dz).abs() <= tol).all()
+        assert not got[:, keep:].any()
