@@ -126,10 +126,11 @@ class Mixer:
 
 def distillation(model, x, index, teacher, *, temperature=1.0, training=True):
     """A stack whose channels are classes against a teacher's top logits (index, teacher
-    [N, H, W, top], as torch.topk gives them): the mean loss over the pixels that have any (a device
+    [N, H, W, top], as torch.topk gives them): the mean loss over the pixels with a slot in use (a device
     scalar) and the gradient of model.forward's result, for model.backward."""
     out = model.forward(x, training=training)
-    pixels = (index >= 0).any(dim=-1)
+    slots = (index >= 0) & (index < out.shape[-1]) & (teacher != -float("inf"))
+    pixels = slots.any(dim=-1)
     weight = pixels.float() / pixels.sum().clamp(min=1)
     loss, dn = quan.distill_loss_and_gradient(out, index, teacher, weight,
                                               temperature=temperature)

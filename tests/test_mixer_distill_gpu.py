@@ -109,3 +109,25 @@ def test_captured_step():
     m.counter.zero_()
     loss, dn = distillation(m, x, index, teacher)
     assert float(loss) == seen[0][0] and torch.equal(dn, seen[0][1])
+
+
+def test_pixels_without_a_slot_in_use_have_no_part_in_the_mean():
+    # however a slot is left empty: no class, a class past the channels, a teacher that gives it nothing
+    m = Mixer(64, 1, seed=6)
+    x = torch.randn(1, 4, 4, 64, device="cuda").to(torch.bfloat16)
+    index = torch.randint(0, 64, (1, 4, 4, 3), device="cuda")
+    teacher = torch.randn(1, 4, 4, 3, device="cuda")
+    seen = []
+    for empty in range(3):
+        i, t = index.clone(), teacher.clone()
+        if empty == 0:
+            i[0, 1] = -1
+        elif empty == 1:
+            i[0, 1] = 64
+        else:
+            t[0, 1] = -float("inf")
+        loss, dn = distillation(m, x, i, t, training=False)
+        seen.append((float(loss), dn.clone()))
+    assert not seen[0][1][0, 1].any()
+    for loss, dn in seen[1:]:
+        assert loss == seen[0][0] and torch.equal(dn, seen[0][1])
