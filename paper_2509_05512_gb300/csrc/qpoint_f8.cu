@@ -459,34 +459,70 @@ __global__ void __launch_bounds__(256) f8_dequant_kernel(const F8Dequant p) {
 }
 
 // The same of components that are not whole chunks of eight: eight elements of the output a thread,
-// wherever rows and components begin, eight rows a block (a multiple of eight elements).  4805 rows
-// of 340: 5.0 us (13 by single elements).
+// wherever rows and components begin, `group` rows (a multiple of eight) a column of blocks.  PAIR,
+// components of eight channels or more: a thread's elements are a run of one component and perhaps the
+// start of the next, which follows it in memory whatever row it is of, so that two loads of eight bytes
+// hold the run and a third the start, shifted together; at most three scales.  100,352 rows of 244:
+// 22.5 us (39.7 by single bytes, eight rows a block); 4805 of 340: 3.0 (4.9); 401,408 of 20: 13.2 (51.9
+// with blocks of eight rows, 20 threads of 256).
+template <bool PAIR>
 __global__ void __launch_bounds__(256) f8_dequant_any_kernel(const F8Dequant p) {
     griddep_launch_dependents();
     griddep_wait();
-    const long long row0 = static_cast<long long>(gridDim.x - 1 - blockIdx.x) * 8;
-    const int rows = p.rows - row0 < 8 ? static_cast<int>(p.rows - row0) : 8;
+    const long long row0 = static_cast<long long>(gridDim.x - 1 - blockIdx.x) * p.group;
+    const int rows = p.rows - row0 < p.group ? static_cast<int>(p.rows - row0) : p.group;
     const unsigned C = 4u * p.Kq, n = rows * C;
     __nv_bfloat16* out = p.out + row0 * C;
     const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
-    for (unsigned f = 8u * threadIdx.x; f < n; f += 8u * 256u) {
+    for (unsigned f = 8u * (blockIdx.y * 256u + threadIdx.x); f < n; f += 8u * 256u * gridDim.y) {
         unsigned r = f / C, k = f - r * C, ci = k / p.Kq;
         k -= ci * p.Kq;
         const uint8_t* q = p.q + ((row0 + r) * 4 + ci) * p.Kp;
-        float s = 0.0f, v[8];
-        bool fresh = true;
+        float v[8];
+        if constexpr (PAIR) {
+            const float* scale = p.scale + row0 + r;
+            const int run = p.Kq - k < 8u ? static_cast<int>(p.Kq - k) : 8;  // of this component
+            const int block = F8_BLOCK - static_cast<int>(k % F8_BLOCK);     // of this scale
+            const unsigned from = k & ~7u, bits = 8u * (k & 7u);
+            using Eight = unsigned long long;
+            Eight w = *reinterpret_cast<const Eight*>(q + from);
+            Eight after = 0;
+            if (bits && from + 8u < static_cast<unsigned>(p.Kp))
+                after = *reinterpret_cast<const Eight*>(q + from + 8);
+            const long long at = (static_cast<long long>(ci) * p.kblk + k / F8_BLOCK) * p.pitch;
+            const float s0 = scale[at];
+            float s1 = 0.0f, s2 = 0.0f;
+            if (block < run) s1 = scale[at + p.pitch];
+            Eight next = 0;
+            if (f + run < n && run < 8) {
+                next = *reinterpret_cast<const Eight*>(q + p.Kp);
+                s2 = ci == 3 ? scale[1] : scale[static_cast<long long>(ci + 1) * p.kblk * p.pitch];
+            }
+            if (bits) w = (w >> bits) | (after << (64u - bits));
+            if (run < 8) w = (w & ((1ull << (8 * run)) - 1)) | (next << (8 * run));
+            float d[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = 0.0f;
-            if (f + j >= n) continue;
-            if (fresh || k % F8_BLOCK == 0)
-                s = p.scale[(static_cast<long long>(ci) * p.kblk + k / F8_BLOCK) * p.pitch + row0 + r];
-            v[j] = f8_to_f32(q[k]) * s;
-            fresh = ++k == static_cast<unsigned>(p.Kq);
-            if (fresh) {
-                k = 0;
-                q += p.Kp;
-                if (++ci == 4) ci = 0, ++r;
+            for (int i = 0; i < 2; ++i) {
+                f8x4_to_f32(static_cast<uint32_t>(w >> (32 * i)), d);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    v[4 * i + j] = d[j] * (4 * i + j >= run ? s2 : 4 * i + j >= block ? s1 : s0);
+            }
+        } else {
+            float s = 0.0f;
+            bool fresh = true;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = 0.0f;
+                if (f + j >= n) continue;
+                if (fresh) s = p.scale[static_cast<long long>(ci) * p.pitch + row0 + r];
+                v[j] = f8_to_f32(q[k]) * s;
+                fresh = ++k == static_cast<unsigned>(p.Kq);
+                if (fresh) {
+                    k = 0;
+                    q += p.Kp;
+                    if (++ci == 4) ci = 0, ++r;
+                }
             }
         }
         if (aligned && f + 8 <= n) {
@@ -517,9 +553,14 @@ cudaError_t launch_f8_dequant(const void* q, const float* scale, long long rows,
                               cudaStream_t stream) {
     F8Dequant p = {static_cast<const uint8_t*>(q), scale, static_cast<__nv_bfloat16*>(out), rows,
                    f8_scale_pitch(rows), Kq, f8_pitch(Kq), blocks_of(Kq), 0};
-    if (Kq % 8 != 0 || reinterpret_cast<uintptr_t>(out) % 16 != 0)
-        return launch_pdl(f8_dequant_any_kernel, dim3(static_cast<unsigned>((rows + 7) / 8)),
-                          dim3(256), 0, stream, p);
+    if (Kq % 8 != 0 || reinterpret_cast<uintptr_t>(out) % 16 != 0) {
+        // 4096 elements or eight rows a column, 4096 elements a block
+        p.group = Kq < 128 ? 8 * (128 / Kq) : 8;
+        const dim3 g(static_cast<unsigned>((rows + p.group - 1) / p.group),
+                     static_cast<unsigned>((static_cast<long long>(p.group) * 4 * Kq + 4095) / 4096));
+        return Kq < 8 ? launch_pdl(f8_dequant_any_kernel<false>, g, dim3(256), 0, stream, p)
+                      : launch_pdl(f8_dequant_any_kernel<true>, g, dim3(256), 0, stream, p);
+    }
     const int per_row = Kq / 2;
     p.group = per_row < 256 ? 256 / per_row : 1;
     return launch_pdl(f8_dequant_kernel,

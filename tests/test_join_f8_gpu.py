@@ -277,3 +277,27 @@ def test_refuses_on_the_device():
         quan.qpointwise_f8(n8, w)
     with pytest.raises(quan.QuanError):
         quan.residual_join_f8(x, h, n=x, **args)
+
+
+@pytest.mark.parametrize("C", [4, 20, 28, 32, 36, 60, 68, 244, 508, 512, 516, 524, 1028, 2060, 8188])
+@pytest.mark.parametrize("rows", [1, 2, 7, 33, 1000])
+def test_rows_of_any_width_read_back(C, rows):
+    # any bytes and scales (powers of two, so that a value is exact in bf16), padding that is not 0, a
+    # block without a scale: every element with its own block's scale, wherever components begin
+    Q, pitch, blocks = C // 4, (C + 63) // 64 * 16, (C + 511) // 512
+    g = torch.Generator(device="cuda").manual_seed(C + rows)
+    q = torch.randint(0, 127, (rows, 4, pitch), generator=g, device="cuda", dtype=torch.uint8)
+    q += 128 * torch.randint(0, 2, q.shape, generator=g, device="cuda", dtype=torch.uint8)
+    scale = torch.randint(-20, 20, (4, blocks, (rows + 127) // 128 * 128), generator=g, device="cuda")
+    scale = torch.exp2(scale.float())
+    scale[2, blocks - 1, rows - 1] = float("nan")
+    n8 = quan.F8Rows(q.view(torch.float8_e4m3fn), scale, C)
+    each = scale.repeat_interleave(128, dim=1)[:, :Q, :rows].permute(2, 0, 1)
+    want = (n8.q.float()[:, :, :Q] * each).to(torch.bfloat16).reshape(rows, C)
+    assert int(want.isnan().sum()) == Q - 128 * (blocks - 1)
+    for shift in (0, 1):
+        buf = torch.full((rows * C + 16,), 7.0, device="cuda", dtype=torch.bfloat16)
+        out = buf[shift:shift + rows * C].view(rows, C)
+        quan.dequantize_f8_rows(n8, out=out)
+        assert torch.equal(out.nan_to_num(12345.0), want.nan_to_num(12345.0))
+        assert (buf[:shift] == 7).all() and (buf[shift + rows * C:] == 7).all()
