@@ -307,7 +307,8 @@ struct Largest<__nv_bfloat16, N> {
 constexpr int ROW_THREADS = 512, ROW_WARPS = ROW_THREADS / 32, ROW_CLUSTER = 8;
 
 // A row by `parts` blocks of a cluster, NCH chunks of it a thread, which stay in registers between the
-// sums and the gradient (what a row has beyond that is read twice).  The first warp does the teacher's
+// sums and the gradient (what a row has beyond that is read twice, or for the loss alone once, NCH chunks
+// on their way together).  The first warp does the teacher's
 // side while the row's loads are under way; maximum and sum are joined over warps and, pushed into the
 // other blocks' shared memory, over the cluster.
 template <typename T, int MODE, int NCH>
@@ -379,17 +380,28 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const Disti
             powers(v, at, p.c, sums);
         }
         sum = sums.x + sums.y;
+        constexpr int U = MODE & GRAD ? 1 : NCH;  // (the gradient's chunks take the registers)
 #pragma unroll 1
-        for (int i = rest; i < end; i += blockDim.x) {
-            Raw<T, E> q;
+        for (int i0 = rest; i0 < end; i0 += U * static_cast<int>(blockDim.x)) {
+            Raw<T, E> q[U];
             Largest<T, E> other;
-            float v[E];
-            fetch(i, q);
-            other.add(q);
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + k * static_cast<int>(blockDim.x);
+                if (i < end) fetch(i, q[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+                if (i0 + k * static_cast<int>(blockDim.x) < end) other.add(q[k]);
             const float top = fmaxf(m, other.get()), now = top == -INFINITY ? 0.0f : top;
             sums = make_float2(shifted(sum, m, now, p.c), 0.0f);
-            q.values(v);
-            powers(v, now, p.c, sums);
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (i0 + k * static_cast<int>(blockDim.x) >= end) continue;
+                float v[E];
+                q[k].values(v);
+                powers(v, now, p.c, sums);
+            }
             sum = sums.x + sums.y;
             m = top;
         }
@@ -1049,14 +1061,17 @@ cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_
         }
     }
     // blocks of a row: as many as its chunks need to stay in registers, more while there are
-    // fewer blocks than SMs and a block keeps 256 chunks
+    // fewer blocks than SMs and a block keeps 256 chunks; the loss of longer rows keeps nothing, and
+    // takes two blocks an SM (1000 x 100,000 fp32: 80 us, 185 with eight blocks a row)
     const int n = row_chunks(p, size);
     int parts = 1;
+    const bool keeps = (MODE & GRAD) != 0 || n <= ROW_THREADS * 8;
     while (parts < ROW_CLUSTER &&
-           (n > parts * ROW_THREADS * 8 || (2 * parts * p.rows <= num_sms && n >= 512 * parts)))
+           (keeps ? n > parts * ROW_THREADS * 8 || (2 * parts * p.rows <= num_sms && n >= 512 * parts)
+                  : parts * p.rows < 2 * num_sms))
         parts *= 2;
     const int per = (n + parts - 1) / parts;
-    if ((MODE & LOSS) && parts == 1) {
+    if ((MODE & LOSS) && parts == 1 && n <= ROW_THREADS * 8) {
         if constexpr ((MODE & LOSS) != 0) {
             if (n <= 1024) return launch_distill_ring<T, MODE, 128>(p, num_sms, stream);
             if (n <= 2048) return launch_distill_ring<T, MODE, 256>(p, num_sms, stream);

@@ -441,3 +441,12 @@ def test_masked_classes_of_rows_far_below_zero(V, dtype):
         tol = d["g"].double()[:, None] * (q + share) * R + HALF[dtype] * dz.abs() + 1e-30
         assert ((got.double() - dz).abs() <= tol).all()
         assert not got[:, keep:].any()
+
+
+@pytest.mark.parametrize("rows, V, pad, top", [(320, 70001, 0, 5), (310, 33001, 3, 20),
+                                               (160, 40000, 8, 64), (1500, 2500, 1, 256),
+                                               (5000, 4100, 4, 3), (1300, 16390, 2, 40),
+                                               (700, 14001, 1, 50), (640, 30001, 0, 256)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_of_more_lengths(rows, V, pad, top, dtype):
+    test_many_rows(rows, V, pad, top, dtype)
