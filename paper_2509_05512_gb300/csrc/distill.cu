@@ -14,8 +14,8 @@
 //
 // A row is read once and its gradient written once, with what a row needs in between on the chip: rows
 // of up to 4 KB as tiles of many rows (distill_tile_kernel), longer ones whole in a ring of shared
-// memory (distill_ring_kernel), single ones, those of more than 64 KB and the gradient alone by blocks
-// that keep their part in registers (distill_row_kernel).  Bound: HBM for long rows; for short ones the
+// memory (distill_ring_kernel), single ones, those of more than 64 KB and the gradient alone of rows below
+// 48 KB or of few by blocks that keep their part in registers (distill_row_kernel).  Bound: HBM for long rows; for short ones the
 // instructions of their slots and reductions.  Loss and gradient, device time: 4096 x 32768 bf16 90 us,
 // 6.0 TB/s (149 by a block a row that reads it twice); 100,352 x 100 bf16, ten slots, 17.6 us, 2.9 TB/s
 // (403); gradient of 333 x 10007 fp32 6.5 us; loss of one row of 65,536 fp32 4.1 us.
@@ -508,20 +508,25 @@ __device__ __forceinline__ void named_bar_arrive(int id, int count) {
 // its own maximum and keeps them: one power an element, and a factor a thread,
 // 2^((own max - max) c) g / S, once the row's maximum and sum are known.  Helper warp h joins the
 // warps' sums of every H-th row, while they take the next row's maximum, and does its slots ahead of
-// time, its loss, and its classes' elements behind the others.
+// time, its loss, and its classes' elements behind the others.  (The gradient alone has its lse, and
+// nothing to join.)
 //
 // 4096 x 32768 bf16, loss and gradient: 89.7 us, 89% of the bytes' floor (101 where the threads wait
 // for the joined sums with nothing else to do, 156 with two powers an element and bounds at every
 // chunk).  Rows that fill fewer threads take blocks of 256 or 128, two to four an SM; of those one
 // helper a block was the slower side (20,000 x 3000, loss: 90 us; 47 with two).
-template <int CT_>
+template <typename T, int MODE, int CT_>
 struct RingCfg {
-    static constexpr int CT = CT_, NCH = 8, H = CT == 512 ? 4 : 2;  // helper warps
+    // Helper warps: fp32 keeps half the powers, which leaves four room beside fewer threads too
+    // (8000 x 4000, loss and gradient: 45 us, 57 with two; in bf16 they spill: 101 and 68 for
+    // 10,000 x 5001).
+    static constexpr bool GRADIENT = (MODE & GRAD) != 0;
+    static constexpr int CT = CT_, NCH = 8, H = CT == 512 || (GRADIENT && sizeof(T) == 4) ? 4 : 2;
     static constexpr int THREADS = CT + 32 * H;
     static constexpr int STAGES = 3;
     static constexpr int STAGE_CHUNKS = NCH * CT;
-    // Blocks an SM, by the powers that a thread keeps: 64 of them leave room for 113 registers.
-    static constexpr int blocks(bool kept64) { return kept64 && CT == 128 ? 3 : 512 / CT; }
+    // Blocks an SM: with powers kept, three of 128 threads, which have 113 or 85 registers.
+    static constexpr int BLOCKS = GRADIENT && CT == 128 ? 3 : 512 / CT;
     static size_t smem(int top) {
         return size_t(16) * STAGES * STAGE_CHUNKS + size_t(SLOT_BYTES) * H * ((top + 3) & ~3);
     }
@@ -529,10 +534,9 @@ struct RingCfg {
 
 // `most`: chunks of any row at most.
 template <typename T, int MODE, int CT>
-__global__ void __launch_bounds__(RingCfg<CT>::THREADS,
-                                  RingCfg<CT>::blocks((MODE & GRAD) && sizeof(T) == 2))
+__global__ void __launch_bounds__(RingCfg<T, MODE, CT>::THREADS, RingCfg<T, MODE, CT>::BLOCKS)
     distill_ring_kernel(const DistillParams p, int most) {
-    using C = RingCfg<CT>;
+    using C = RingCfg<T, MODE, CT>;
     constexpr int E = RowView<T>::E, H = C::H, NCH = C::NCH, WARPS = CT / 32;
     extern __shared__ int4 dynamic[];
     // the warps' maxima and sums of two rows in turn, and what a helper makes of them
@@ -605,7 +609,7 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             return largest.get();
         };
         copies_wait<1>();
-        float m = largest_of(0);
+        float m = MODE & LOSS ? largest_of(0) : 0.0f;
         for (; row < p.rows; row += step) {
             // (the stage that this overwrites was read a row ago, by this thread)
             fetch(row + 2 * step, stage == 0 ? 2 : stage - 1);
@@ -619,24 +623,35 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
                     Raw<T, E> r;
                     r.load(mine + k * CT * E);
                     r.values(e[k]);
-                    powers(e[k], at, p.c, sums);
+                    if (MODE & LOSS) powers(e[k], at, p.c, sums);
                 }
-            float sum = sums.x + sums.y;
             stage = stage == 2 ? 0 : stage + 1;
-            const float top = lanes_max(m, 32);
-            sum = lanes_sum(shifted(sum, m, top, p.c), 32);
-            if (lane == 0) {
-                sum_m[buf][tid >> 5] = top;
-                sum_s[buf][tid >> 5] = sum;
+            if (MODE & LOSS) {
+                const float top = lanes_max(m, 32);
+                const float sum = lanes_sum(shifted(sums.x + sums.y, m, top, p.c), 32);
+                if (lane == 0) {
+                    sum_m[buf][tid >> 5] = top;
+                    sum_s[buf][tid >> 5] = sum;
+                }
+                named_bar_arrive(1 + h, CT + 32);
             }
-            named_bar_arrive(1 + h, CT + 32);
             copies_wait<1>();  // (past the last row: nothing is under way, and what is read not used)
-            m = largest_of(stage);
+            if (MODE & LOSS) m = largest_of(stage);
             named_bar_sync(1 + H + h, CT + 32);
             if (MODE & GRAD) {
-                const float g = row_f[h];
+                const float g = row_f[h], of_row = row_m[h];
                 // (a thread with no finite logit has at = 0, which may be far above the row's maximum)
-                const float f = ex2_approx_ftz(fminf((at - row_m[h]) * p.c, 0.0f)) * g;
+                const float f =
+                    MODE & LOSS ? ex2_approx_ftz(fminf((at - of_row) * p.c, 0.0f)) * g : g;
+                if (!(MODE & LOSS)) {
+#pragma unroll
+                    for (int k = 0; k < NCH; ++k)
+                        if ((k & ~1) * CT < most) {
+#pragma unroll
+                            for (int j = 0; j < E; ++j)
+                                e[k][j] = ex2_approx_ftz(fmaf(e[k][j], p.inv_t, -of_row) * LOG2E);
+                        }
+                }
                 const RowView<T> view = view_of(row);
                 T* out = static_cast<T*>(p.dz) + row * p.pitch;
                 T* place = out - view.head + tid * E;
@@ -691,11 +706,12 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
     // A lane's first slot and the row's weight are loaded a turn ahead, the student's logit behind
     // the loss (a row's logits are overwritten only after its helper has come to its sums).
     long long row = blockIdx.x + h * step, raw = -1;
-    float t0 = 0.0f, z0 = 0.0f, weight = 1.0f;
+    float t0 = 0.0f, z0 = 0.0f, weight = 1.0f, lse0 = 0.0f;
     auto ahead = [&](long long r) {
         raw = -1;
         if (r >= p.rows) return;
         if (MODE & GRAD && p.dloss) weight = p.dloss[r];
+        if (MODE == GRAD) lse0 = p.lse_in[r];
         if (lane < s.top) {
             raw = slot_class(p, r * p.top + lane);
             t0 = slot_logit(p, r * p.top + lane);
@@ -709,7 +725,7 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
     gather(row);
     for (; row < p.rows; row += H * step) {
         const T* zrow = z + row * p.pitch;
-        const float g_row = weight;
+        const float g_row = weight, lse = lse0;
         if (lane < s.top4) {
             s.id[lane] = slot_id(p, raw, t0);
             s.p[lane] = t0;
@@ -731,20 +747,32 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
                 s.share[k] = s.id[k] >= 0 ? class_share(s, k) : -1.0f;
         }
         const float g = some ? g_row * p.scale : 0.0f;
-        named_bar_sync(1 + h, CT + 32);
-        const float wm = lane < WARPS ? sum_m[buf][lane] : -INFINITY, m = lanes_max(wm, 32);
-        const float sum = lanes_sum(lane < WARPS ? shifted(sum_s[buf][lane], wm, m, p.c) : 0.0f, 32);
-        const float inv_s = 1.0f / sum;
-        if (lane == 0) {
-            row_m[h] = m;
-            row_f[h] = g == 0.0f ? 0.0f : g * inv_s;
-        }
-        __syncwarp();
-        named_bar_arrive(1 + H + h, CT + 32);
-        const float ln_s = logf(sum), loss = slots_loss(s, p, lane, m, ln_s);
-        if (lane == 0) {
-            p.loss[row] = some ? p.t2 * loss : 0.0f;
-            if (p.lse) p.lse[row] = fmaf(m, p.inv_t, ln_s);
+        float m = lse, inv_s = 1.0f;
+        if (MODE & LOSS) {
+            named_bar_sync(1 + h, CT + 32);
+            const float wm = lane < WARPS ? sum_m[buf][lane] : -INFINITY;
+            m = lanes_max(wm, 32);
+            const float sum =
+                lanes_sum(lane < WARPS ? shifted(sum_s[buf][lane], wm, m, p.c) : 0.0f, 32);
+            inv_s = 1.0f / sum;
+            if (lane == 0) {
+                row_m[h] = m;
+                row_f[h] = g == 0.0f ? 0.0f : g * inv_s;
+            }
+            __syncwarp();
+            named_bar_arrive(1 + H + h, CT + 32);
+            const float ln_s = logf(sum), loss = slots_loss(s, p, lane, m, ln_s);
+            if (lane == 0) {
+                p.loss[row] = some ? p.t2 * loss : 0.0f;
+                if (p.lse) p.lse[row] = fmaf(m, p.inv_t, ln_s);
+            }
+        } else {
+            if (lane == 0) {
+                row_m[h] = lse;
+                row_f[h] = g;
+            }
+            __syncwarp();
+            named_bar_arrive(1 + H + h, CT + 32);
         }
         gather(row + H * step);
         if (MODE & GRAD) {
@@ -753,7 +781,9 @@ __global__ void __launch_bounds__(RingCfg<CT>::THREADS,
             for (int k = lane; k < s.top && g != 0.0f; k += 32)
                 if (s.id[k] >= 0 && s.share[k] != -1.0f)
                     put(out + s.id[k],
-                        g * (ex2_approx_ftz((s.z[k] - m) * p.c) * inv_s - s.share[k]));
+                        g * ((MODE & LOSS ? ex2_approx_ftz((s.z[k] - m) * p.c) * inv_s
+                                          : ex2_approx_ftz(fmaf(s.z[k], p.inv_t, -m) * LOG2E)) -
+                             s.share[k]));
         }
         __syncwarp();
         static_assert(H % 2 == 0, "a helper's rows have one buffer of sums");
@@ -769,7 +799,7 @@ int row_chunks(const DistillParams& p, int size) {
 
 template <typename T, int MODE, int CT>
 cudaError_t launch_distill_ring(const DistillParams& p, int num_sms, cudaStream_t stream) {
-    using C = RingCfg<CT>;
+    using C = RingCfg<T, MODE, CT>;
     auto* kern = distill_ring_kernel<T, MODE, CT>;
     static std::atomic<unsigned long long> ready{0};  // once a device: the shared memory
     int dev = 0;
@@ -781,7 +811,7 @@ cudaError_t launch_distill_ring(const DistillParams& p, int num_sms, cudaStream_
         if (e != cudaSuccess) return e;
         if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
     }
-    const long long most = static_cast<long long>(num_sms) * C::blocks((MODE & GRAD) && sizeof(T) == 2);
+    const long long most = static_cast<long long>(num_sms) * C::BLOCKS;
     const dim3 g(static_cast<unsigned>(p.rows < most ? p.rows : most));
     return launch_pdl(kern, g, dim3(C::THREADS), C::smem(p.top), stream, p,
                       row_chunks(p, sizeof(T)));
@@ -1071,8 +1101,13 @@ cudaError_t launch_distill_mode(const DistillParams& p, int num_sms, cudaStream_
                   : parts * p.rows < 2 * num_sms))
         parts *= 2;
     const int per = (n + parts - 1) / parts;
-    if ((MODE & LOSS) && parts == 1 && n <= ROW_THREADS * 8) {
-        if constexpr ((MODE & LOSS) != 0) {
+    if (parts == 1 && n <= ROW_THREADS * 8) {
+        // the gradient alone: rows that keep most of a ring's chunks busy, four a block or more
+        // (4096 x 32768 bf16 84 us, 120 by a block a row; 1300 x 10007 fp32 26 and 21)
+        if constexpr (MODE == GRAD) {
+            if (n > ROW_THREADS * 6 && p.rows >= 4LL * num_sms)
+                return launch_distill_ring<T, MODE, 512>(p, num_sms, stream);
+        } else {
             if (n <= 1024) return launch_distill_ring<T, MODE, 128>(p, num_sms, stream);
             if (n <= 2048) return launch_distill_ring<T, MODE, 256>(p, num_sms, stream);
             return launch_distill_ring<T, MODE, 512>(p, num_sms, stream);
