@@ -462,7 +462,8 @@ __global__ void __launch_bounds__(256) f8_dequant_kernel(const F8Dequant p) {
 // wherever rows and components begin, `group` rows (a multiple of eight) a column of blocks.  PAIR,
 // components of eight channels or more: a thread's elements are a run of one component and perhaps the
 // start of the next, which follows it in memory whatever row it is of, so that two loads of eight bytes
-// hold the run and a third the start, shifted together; at most three scales.  100,352 rows of 244:
+// hold the run and a third the start, shifted together; at most three scales.  Bound by its instructions (80%
+// of the issue slots).  100,352 rows of 244:
 // 22.5 us (39.7 by single bytes, eight rows a block); 4805 of 340: 3.0 (4.9); 401,408 of 20: 13.2 (51.9
 // with blocks of eight rows, 20 threads of 256).
 template <bool PAIR>
