@@ -47,18 +47,23 @@ class Mixer:
         self.quantize()
 
     def quantize(self) -> None:
-        """The letters' 8-bit forms, after the letters changed."""
+        """The letters' 8-bit forms, after the letters changed.  Those of `quantize_4bit` go: they are
+        of the letters before."""
+        self.w4 = None
         self.w = [quan.quantize_f8_weights(*w) for w in self.letters]
         self.wt = [quan.quantize_f8_weights(*w, transpose=True) for w in self.letters]
 
     def quantize_4bit(self, group: int = 64) -> None:
-        """The letters in 4 bits, for `serve`, after they changed."""
+        """The letters in 4 bits, for `serve`; again after each `update` or `quantize`.  (An update
+        that a graph replays changes the letters without this object's knowledge.)"""
         self.w4 = [quan.quantize_w4_weights(*w, group=group) for w in self.letters]
 
     def serve(self, x):
         """The stack on a few pixels, bf16 x [..., channels] (CUDA), without dropout and with the
         letters of quantize_4bit: an eighth of their bytes, which bound a single pixel.  Keeps
         nothing."""
+        if self.w4 is None:
+            raise RuntimeError("the letters are not in 4 bits since they changed: quantize_4bit()")
         _, n = quan.residual_join(x, pre=self.pre[0], groups=self.groups, eps=self.eps)
         y = x
         for l in range(self.depth):
