@@ -602,8 +602,9 @@ quan_status_t quan_qpoint_f8_bwd_data(const void* dy, const void* wq, const floa
  *
  * quan_qpoint_w4_fwd: out = act(iqbn_scale * (x W + bias) + iqbn_shift), the rest as in
  * quan_qpoint_f8_fwd.  Sums are fp32.  x bf16 [rows][Cin], out bf16 [rows][Cout], no overlap with an
- * input.  rows = 0 is a no-op; more than 2^20 rows or channels return QUAN_ERR_UNSUPPORTED (past about
- * 64 rows quan_qpoint_f8_fwd is faster).
+ * input.  rows = 0 is a no-op; more than 2^20 rows or channels return QUAN_ERR_UNSUPPORTED.
+ * quan_qpoint_f8_fwd is faster from some number of rows on: between 16 and 32 for 8192 -> 8192, 32 and 49
+ * for 4096 -> 4096, 64 and 96 for 2048 -> 2048, 256 and 512 for 512 -> 1024.
  */
 size_t quan_w4_weights_bytes(int Cin, int Cout);
 size_t quan_w4_weights_scales(int Cin, int Cout, int group);

@@ -8,16 +8,18 @@
 // bf16 holds q and x exactly and the tensor cores add their products in fp32; a group's sum is
 // multiplied by its scale in fp32, so nothing is rounded to fewer bits but the output.
 //
-// Bound by the letters' bytes (half a byte for the 16 products that a letter's element has a row), and
+// Bound by the letters' bytes (half a byte for the four products that a letter's element has a row), and
 // with one pixel by the trip to memory.  A warp-level MMA (m16n8k16) takes 16 output channels of one
 // letter as its rows; its 8 columns are the four output components of two pixels, column (m, co)
 // holding component co xor L of pixel m with Eq. 6's sign.  So an element of a letter is read and
 // widened once for all four components, and the quaternion product needs no other arithmetic.
 //
-// Device time: one pixel 512 -> 1024 1.7 us, 8192 -> 8192 7.0 us (8.9 MB of letters and scales: 1.3 us at
-// HBM's rate, which two rounds of loads, the join of the warps and a cluster's two barriers follow: with
-// the inputs over four blocks instead of two 11.2 us); 49 pixels 2048 -> 2048 8.5 us, 13 pixels
-// 1172 -> 2804 6.3 us.
+// Device time: one pixel 512 -> 1024 1.7 us; 8192 -> 8192 8.3 us with the letters in memory (8.9 MB with
+// their scales: 1.3 us at HBM's rate), 7.1 with them in L2; 49 pixels 2048 -> 2048 8.1 us (8.5 with SiLU and
+// vectors), 13 pixels 1172 -> 2804 6.3 us.  At 8192 -> 8192 clusters of four blocks share a tile's inputs:
+// 512 blocks with 98 registers a thread, 304 at once, so that a second wave's letters wait for the
+// first's joins.  Other clusters there, from memory and L2: one block 9.5 and 8.2, two 6.7 and 5.5, eight
+// 13.2 and 11.4.
 //
 // Layout of the letters: [L][16 output channels][64 input channels] blocks of 512 bytes, a lane's 16
 // bytes side by side: word s of lane 4 g + t has q + 8 of channels g and g + 8, inputs
@@ -415,8 +417,8 @@ cudaError_t launch_w4_form(W4Params p, int num_sms, cudaStream_t stream) {
     // staged for more than four pixels, or channels that are not loaded eight at a time
     constexpr bool STAGED = NT > 2 || LV != 8;
     const long long tiles = (p.rows + 2 * NT - 1) / (2 * NT);
-    // the inputs are split while the blocks are fewer than the SMs' and a warp keeps two blocks
-    // of letters
+    // the inputs are split in two, and again, while the blocks are fewer than the SMs (without a stage,
+    // than two an SM) and a warp keeps two blocks of letters
     p.split = 1;
     while (p.split < 8 && tiles * p.ntiles * p.split < (STAGED ? 1 : 2) * num_sms &&
            4 * p.ktiles >= 4 * W4_WARPS * p.split)

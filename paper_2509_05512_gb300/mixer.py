@@ -60,8 +60,8 @@ class Mixer:
 
     def serve(self, x):
         """The stack on a few pixels, bf16 x [..., channels] (CUDA), without dropout and with the
-        letters of quantize_4bit: an eighth of their bytes, which bound a single pixel.  Keeps
-        nothing."""
+        letters of quantize_4bit: about a quarter of the bf16 letters' bytes, which bound a single
+        pixel.  Keeps nothing."""
         if self.w4 is None:
             raise RuntimeError("the letters are not in 4 bits since they changed: quantize_4bit()")
         _, n = quan.residual_join(x, pre=self.pre[0], groups=self.groups, eps=self.eps)

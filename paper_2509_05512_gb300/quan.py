@@ -999,8 +999,9 @@ def qpointwise_w4(x, w, *, bias=None, scale=None, shift=None, act=QUAN_ACT_NONE,
                   stream=None):
     """Pointwise quaternion convolution of a few pixels with 4-bit letters: bf16 x [..., Cin] (CUDA)
     and w = quantize_w4_weights(...) -> bf16 [..., Cout], act(scale * (x W + bias) + shift) with
-    fp32 vectors [Cout] as in qconv2d.  An eighth of the bytes of bf16 letters, for serving: past
-    about 64 pixels qpointwise_f8 is faster."""
+    fp32 vectors [Cout] as in qconv2d.  About a quarter of the bytes of bf16 letters (0.27 with
+    groups of 64), for serving.  qpointwise_f8 is faster from some number of pixels on: between 16 and 32
+    for 8192 -> 8192, 32 and 49 for 4096 -> 4096, 64 and 96 for 2048 -> 2048, 256 and 512 for 512 -> 1024."""
     torch = _torch or _get_torch()
     q, wscale, Cin, Cout, group = w
     dev, shape, bf16 = _device("x", x), tuple(x.shape), torch.bfloat16
