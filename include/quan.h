@@ -627,7 +627,11 @@ quan_status_t quan_qpoint_w4_fwd(const void* x, const void* wq, const void* wsca
  * stand in several slots.  A logit of -infinity is a class that cannot be (q = 0; a slot with p > 0 of
  * it makes the loss infinite).  +infinity, NaN, or no finite logit in a row that counts give NaN (a
  * teacher's in the loss and the slots' classes).  z / T and t / T have to stay within fp32.
- * Arithmetic is fp32; the gradient is rounded once.  Repeated calls give the same bits.
+ * Arithmetic is fp32; the gradient is rounded once.  Repeated calls give the same bits.  quan_distill_bwd
+ * takes q from e^(z / T - lse), which carries the rounding of lse into the row: q is off by about
+ * 2^-23 (|z| / T + |lse|) of itself, 1e-3 where those are 5000, and nothing is left of it near 1e7.
+ * quan_distill_fwd_bwd has the row's maximum and no such error: it is the call for logits far from 0 or
+ * a small T.
  *   z, dz     [rows][pitch] of dtype (quan_dtype_t), the row's first `classes` elements its logits;
  *             dz's others become 0.  dz may be z itself (in place), no other overlap
  *   index     [rows][top] classes, index_bits (32 or 64) wide, signed
