@@ -81,20 +81,22 @@ class Mixer:
         """bf16 x [N, H, W, channels] (CUDA) -> the last norm's output; keeps what `backward`
         needs."""
         self.training = training
-        _, n, rows = self._norm(0, x, None, dict(pre=self.pre[0], groups=self.groups, eps=self.eps))
+        _, n, rows = self._norm(0, x, None, None,
+                                dict(pre=self.pre[0], groups=self.groups, eps=self.eps))
         self.y, self.h, self.n = [x], [], [n]
         for l in range(self.depth):
             h = quan.qpointwise_f8(rows, self.w[l])
-            y, n, rows = self._norm(l + 1, self.y[l], h, self._join(l, x.numel(), training))
+            y, n, rows = self._norm(l + 1, self.y[l], h, rows, self._join(l, x.numel(), training))
             self.h.append(h)
             self.y.append(y)
             self.n.append(n)
         return self.n[-1]
 
-    def _norm(self, l: int, x, h, args):
-        """A join, and what block l's product reads: the norm in 8 bits, or in bf16."""
+    def _norm(self, l: int, x, h, rows, args):
+        """A join, and what block l's product reads: the norm in 8 bits (in the place of the block
+        before's rows, which its product has read), or in bf16."""
         if self.groups == 4 and l < self.depth:
-            return quan.residual_join_f8(x, h, keep=True, **args)
+            return quan.residual_join_f8(x, h, keep=True, n8=rows, **args)
         y, n = quan.residual_join(x, h, **args)
         return y, n, n
 
