@@ -514,7 +514,13 @@ __device__ __forceinline__ void named_bar_arrive(int id, int count) {
 // 4096 x 32768 bf16, loss and gradient: 89.7 us, 89% of the bytes' floor (101 where the threads wait
 // for the joined sums with nothing else to do, 156 with two powers an element and bounds at every
 // chunk).  Rows that fill fewer threads take blocks of 256 or 128, two to four an SM; of those one
-// helper a block was the slower side (20,000 x 3000, loss: 90 us; 47 with two).
+// helper a block was the slower side (20,000 x 3000, loss: 90 us; 45 with two, in bf16 as in fp32).
+//
+// A helper's time grows with the slots, and past its rows' share of the threads' it bounds the row: loss
+// of 20,000 x 3000 bf16 47 us with 16 slots, 61 with 64, 87 with 128, 112 with 192; loss and gradient of
+// 4096 x 16,000 bf16 47, 60, 86 and 119, where each slot is compared with every other.  Past about 200
+// slots the loss of rows that fill 128 threads has blocks of too much shared memory for four an SM, which
+// its grid counts on: the fourth quarter runs as a second wave (267 us with 256).
 template <typename T, int MODE, int CT_>
 struct RingCfg {
     // Helper warps: fp32 keeps half the powers, which leaves four room beside fewer threads too

@@ -139,9 +139,12 @@ __device__ __forceinline__ void times8(float (&v)[8], float f, const float (&w)[
 // F8: the norm in 8 bits, and in bf16 where out_n is given.  A row is cut into its four components
 // whatever its statistics are, so that a block of 128 is 16 neighbouring lanes; a statistic of the
 // whole row takes the lanes of all four.  Elementwise by twos, without a mask where nothing is dropped, and
-// three blocks an SM: 100,352 rows of 244 bf16 55 us (59 one by one, two blocks); bound by the accesses of
-// single elements.  The other forms ask for no number of blocks (0: the compiler's choice): asked for
-// one, it takes the registers of the third (78 to 95; 32 x 56 x 56 x 256 bf16 42 us, 38 with three).
+// three blocks an SM: 100,352 rows of 244 bf16 55 us (59 one by one, two blocks).  There every access is of
+// one element, as wherever components are not in fours (248 channels: 55 us too): 404 instructions a warp
+// and row at 64% of the issue slots and 29% of HBM's time.  Pairs, which 62 channels a component would
+// allow, have not been tried.
+// The other forms ask for no number of blocks (0: the compiler's choice): asked for one, it takes the
+// registers of the third (78 to 95; 32 x 56 x 56 x 256 bf16 42 us, 38 with three).
 template <typename T, int LV, int NC, bool CROSS, bool F8>
 __global__ void __launch_bounds__(CROSS ? 512 : 256, F8 && !CROSS ? 3 : 0)
     join_fwd_kernel(const JoinParams p) {
