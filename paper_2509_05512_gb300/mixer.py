@@ -47,9 +47,9 @@ class Mixer:
         self.quantize()
 
     def quantize(self) -> None:
-        """The letters' 8-bit forms, after the letters changed.  Those of `quantize_4bit` go: they are
-        of the letters before."""
-        self.w4 = None
+        """The letters' 8-bit forms, after the letters changed.  Those of `quantize_4bit` are of the
+        letters before then (and stay allocated, for a graph that was captured with them)."""
+        self.w4_current = False
         self.w = [quan.quantize_f8_weights(*w) for w in self.letters]
         self.wt = [quan.quantize_f8_weights(*w, transpose=True) for w in self.letters]
 
@@ -57,12 +57,13 @@ class Mixer:
         """The letters in 4 bits, for `serve`; again after each `update` or `quantize`.  (An update
         that a graph replays changes the letters without this object's knowledge.)"""
         self.w4 = [quan.quantize_w4_weights(*w, group=group) for w in self.letters]
+        self.w4_current = True
 
     def serve(self, x):
         """The stack on a few pixels, bf16 x [..., channels] (CUDA), without dropout and with the
         letters of quantize_4bit: about a quarter of the bf16 letters' bytes, which bound a single
         pixel.  Keeps nothing."""
-        if self.w4 is None:
+        if not self.w4_current:
             raise RuntimeError("the letters are not in 4 bits since they changed: quantize_4bit()")
         _, n = quan.residual_join(x, pre=self.pre[0], groups=self.groups, eps=self.eps)
         y = x

@@ -43,6 +43,14 @@ def test_letters_served_are_those_of_the_last_update(model):
     assert all(torch.equal(a, b) for s, l in zip(served, model.letters) for a, b in zip(s, l))
 
 
+def test_an_update_leaves_what_a_captured_pass_reads(model):
+    # a graph of serve holds the letters' addresses: the tensors stay until quantize_4bit makes others
+    model.quantize_4bit()
+    before = model.w4
+    model.update(gradients(model), 0.5)
+    assert model.w4 is before
+
+
 def test_letters_have_to_be_quantised_before_they_are_served(model):
     with pytest.raises(RuntimeError, match="quantize_4bit"):
         model.serve(torch.zeros(1, 16, dtype=torch.bfloat16))
